@@ -265,6 +265,131 @@ mkv_status paged_attn_decode_append(mkv_pool* pool, int32_t layer, int32_t n_req
                                     float* out, float* lse, void* ws, size_t ws_bytes,
                                     hipStream_t stream);
 
+/* Rotary positions.  A kv_rope turns pair i of every head of a row by the angle
+ * th_i = pos[axis_i] * f_i (fp64, one rounding):
+ *     (x0, x1) -> scale * (x0 cos th_i - x1 sin th_i, x1 cos th_i + x0 sin th_i),
+ * evaluated in fp64 and rounded once to bf16 (to nearest even); channels at or
+ * past rot_dim stay as they are (scale does not touch them).  Pair i is channels
+ * (i, i + rot_dim / 2), or (2i, 2i + 1) with interleaved != 0.  With several
+ * axes (time, row and column of an image token, say) each frequency follows the
+ * axis its entry names; positions are int32 [n_axes][n rows], any value.
+ *  - kv_rope_bytes: size of the device table of a rot_dim (even, 2 .. 256).
+ *  - kv_rope_create fills the caller-owned table synchronously; the handle owns
+ *    only host metadata, and the table must stay as long as the handle is used.
+ *    Errors: EINVAL, EUNSUP (head_dim, n_axes over 4), ERANGE (|f_i| over 4 or not
+ *    a number, an axis >= n_axes, scale outside (0, 1e6]), ENOMEM, EHIP.
+ *  - kv_rope_apply rotates the rows of n_tokens tokens, [n_heads][head_dim] each,
+ *    x_stride elements from one token to the next (queries inside packed q/k/v
+ *    rows, say), into out.  In place (out == x, same stride) is allowed, any other
+ *    overlap of the two ranges is refused.  x and out: 8-byte aligned, strides a
+ *    multiple of 4 and at least n_heads * head_dim (MKV_EINVAL otherwise).
+ *    n_tokens = 0 does nothing. */
+typedef struct kv_rope kv_rope; /* opaque host handle */
+typedef struct kv_rope_desc {
+  int32_t head_dim;       /* 128 or 256 */
+  int32_t rot_dim;        /* rotated channels, even, 2 .. head_dim */
+  int32_t n_axes;         /* 1 .. 4 */
+  int32_t interleaved;    /* 0: pairs (i, i + rot_dim/2); else (2i, 2i+1) */
+  double scale;           /* factor on the rotated channels (1: none) */
+  const double* inv_freq; /* host [rot_dim / 2] */
+  const uint8_t* axis;    /* host [rot_dim / 2], or NULL: all axis 0 */
+  void* table;            /* device, 16-byte aligned */
+  size_t table_bytes;
+} kv_rope_desc;
+mkv_status kv_rope_bytes(int32_t rot_dim, size_t* bytes);
+mkv_status kv_rope_create(const kv_rope_desc* desc, kv_rope** out);
+mkv_status kv_rope_destroy(kv_rope* rope);
+mkv_status kv_rope_apply(const kv_rope* rope, int32_t n_tokens, int32_t n_heads, const uint16_t* x,
+                         int64_t x_stride, const int32_t* positions, uint16_t* out,
+                         int64_t out_stride, hipStream_t stream);
+
+/* kv_append_fp8 of keys that come unrotated: every key row is rotated by its
+ * token's positions and rounded to bf16 on the way into its page (values are not).
+ * Pages, scales, table, tags and errors equal those of kv_rope_apply on the keys
+ * followed by kv_append_fp8, bit for bit.  positions: device int32 [n_axes]
+ * [n_new_total], or NULL: a token's place in the cache, seq_lens_before[r] + i, on
+ * every axis.  Row i of k starts k_stride elements after row i - 1 (v likewise;
+ * with MKV_ALL_LAYERS layer l's rows follow layer l - 1's); k and v 8-byte
+ * aligned, strides a multiple of 4 and at least n_kv_heads * head_dim.
+ * MKV_EINVAL also when the rope's head_dim is not the pool's. */
+mkv_status kv_append_fp8_rope(mkv_pool* pool, const kv_rope* rope, int32_t layer, int32_t n_req,
+                              int32_t* block_table, uint8_t* tags, int32_t max_pages,
+                              const int32_t* seq_lens_before, const int32_t* cu_new_tokens,
+                              int32_t n_new_total, const int32_t* positions, const uint16_t* k,
+                              int64_t k_stride, const uint16_t* v, int64_t v_stride,
+                              hipStream_t stream);
+
+/* paged_attn_decode_append of a query and key that come unrotated: both are
+ * rotated by their token's positions (device int32 [n_axes][n_req], or NULL:
+ * seq_lens_before[r] on every axis) and rounded to bf16 inside the launch.  State
+ * afterwards as by kv_append_fp8_rope, outputs those of paged_attn_decode on the
+ * rotated query with the error of fp32 arithmetic (2^-22 of a query entry and of a
+ * weight; paged_attn_decode rounds the query to 2^-14 against TQ3 pages).  Buffers,
+ * workspace and errors as paged_attn_decode_append. */
+mkv_status paged_attn_decode_append_rope(mkv_pool* pool, const kv_rope* rope, int32_t layer,
+                                         int32_t n_req, const uint16_t* q, const uint16_t* k_new,
+                                         const uint16_t* v_new, const int32_t* positions,
+                                         int32_t* block_table, uint8_t* tags, int32_t max_pages,
+                                         const int32_t* seq_lens_before, float* out, float* lse,
+                                         void* ws, size_t ws_bytes, hipStream_t stream);
+
+/* Sparse decode attention: per request and KV head a cheap score picks pages and
+ * the attention reads only those.
+ *  - Page bounds: for every (layer, request, KV head, logical page) the largest and
+ *    the smallest code of each key channel over the page's tokens (E4M3, exact) and
+ *    the page's K scale: codes [n_layers][n_req][n_kv_heads][max_pages][2][head_dim]
+ *    bytes (largest, then smallest), scales fp32 [n_layers][n_req][n_kv_heads]
+ *    [max_pages], caller-owned, sizes from kv_page_bounds_bytes.  They follow the
+ *    logical page: Retier and Promote leave them valid as a score, a request that
+ *    takes over another's pages takes over their rows (a copy).
+ *  - kv_page_bounds_update recomputes the pages that hold positions seq_lens_from[r]
+ *    .. seq_lens[r] - 1, and a partly filled first one whole (after an append: the
+ *    lengths before and after it), for one layer or MKV_ALL_LAYERS.  The pages must
+ *    be FP8 (Recent or Anchor), so it comes before the Retier that would encode
+ *    them.  A length out of range: RANGE, that request is left out; a page with
+ *    another tag: BAD_TAG, or with an id out of range: RANGE, that page is left out.
+ *  - paged_attn_select_pages scores page p of request r for KV head h by
+ *        b = s_p * max over the group's heads of sum_c max(q_c hi_c, q_c lo_c),
+ *    which no q.k of the page exceeds, and lists in pages[r][h][0 .. n_select) the
+ *    first n_first pages, the last n_last and the best of the others, n_select in
+ *    all, in ascending order; with at most n_select pages all of them, -1 behind.
+ *    counts[r][h] is how many.  Scores are compared in fp64, equal ones go to the
+ *    lower page, NaN is the lowest.  q: bf16 [n_req][n_q_heads][d], rotated, 16-byte
+ *    aligned; pages: device int32 [n_req][n_kv_heads][n_select]; counts: device int32
+ *    [n_req][n_kv_heads]; ws: >= paged_attn_select_workspace_bytes(), 16-byte
+ *    aligned.  n_first + n_last <= n_select <= 262144.  An invalid length: RANGE,
+ *    count 0 and -1s for that request.
+ *  - paged_attn_decode_sparse is paged_attn_decode over the listed pages only
+ *    (tokens below seq_lens[r]): pages [n_req][n_kv_heads][n_select], strictly
+ *    ascending, counts of them.  A count of 0 gives zero outputs and lse = -inf.  A
+ *    count outside [0, n_select]: RANGE and zero outputs for that KV head's queries;
+ *    an entry that is not above the one before it, or past the sequence's end: RANGE,
+ *    that entry is left out.  Other errors, buffers and the order of sums as
+ *    paged_attn_decode; ws >= paged_attn_workspace_bytes(pool, n_req, n_select, 0)
+ *    (one for more pages serves too).  Outputs carry the error of fp32 arithmetic, as
+ *    paged_attn_decode_append_rope's do. */
+mkv_status kv_page_bounds_bytes(const mkv_pool* pool, int32_t n_req, int32_t max_pages,
+                                size_t* code_bytes, size_t* scale_bytes);
+mkv_status kv_page_bounds_update(mkv_pool* pool, int32_t layer, int32_t n_req,
+                                 const int32_t* block_table, const uint8_t* tags,
+                                 int32_t max_pages, const int32_t* seq_lens_from,
+                                 const int32_t* seq_lens, uint8_t* codes, size_t code_bytes,
+                                 float* scales, size_t scale_bytes, hipStream_t stream);
+mkv_status paged_attn_select_workspace_bytes(const mkv_pool* pool, int32_t n_req,
+                                             int32_t max_pages, size_t* bytes);
+mkv_status paged_attn_select_pages(mkv_pool* pool, int32_t layer, int32_t n_req,
+                                   const uint16_t* q, const int32_t* seq_lens, int32_t max_pages,
+                                   const uint8_t* codes, size_t code_bytes, const float* scales,
+                                   size_t scale_bytes, int32_t n_select, int32_t n_first,
+                                   int32_t n_last, int32_t* pages, int32_t* counts, void* ws,
+                                   size_t ws_bytes, hipStream_t stream);
+mkv_status paged_attn_decode_sparse(mkv_pool* pool, int32_t layer, int32_t n_req,
+                                    const uint16_t* q, const int32_t* block_table,
+                                    const uint8_t* tags, int32_t max_pages,
+                                    const int32_t* seq_lens, int32_t n_select,
+                                    const int32_t* pages, const int32_t* counts, float* out,
+                                    float* lse, void* ws, size_t ws_bytes, hipStream_t stream);
+
 /* paged_attn_decode for callers that cannot allocate device memory (code
  * under HIP graph capture, tight serving loops, harnesses that forbid
  * hipMalloc): the same attention, with the split partials held in a fixed

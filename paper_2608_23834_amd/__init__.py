@@ -33,6 +33,9 @@ EXPORTS = ["kv_pool_bytes", "kv_pool_create", "kv_pool_destroy", "kv_append_fp8"
            "paged_attn_decode_noalloc", "mkv_fp64_probe", "mkv_control_bf16_write",
            "mkv_control_bf16_workspace_bytes", "mkv_control_bf16_decode",
            "paged_attn_decode_cohort_key", "paged_attn_decode_scores", "kv_page_scores_update",
+           "kv_rope_bytes", "kv_rope_create", "kv_rope_destroy", "kv_rope_apply", "kv_append_fp8_rope",
+           "paged_attn_decode_append_rope", "kv_page_bounds_bytes", "kv_page_bounds_update",
+           "paged_attn_select_workspace_bytes", "paged_attn_select_pages", "paged_attn_decode_sparse",
            "mkv_status_string"]
 
 _lib = None
@@ -55,6 +58,12 @@ class PoolDesc(ctypes.Structure):
                 ("fp8_scales", ctypes.c_void_p), ("fp8_scales_bytes", ctypes.c_size_t),
                 ("tq3_data", ctypes.c_void_p), ("tq3_data_bytes", ctypes.c_size_t),
                 ("ctrl", ctypes.c_void_p), ("ctrl_bytes", ctypes.c_size_t)]
+
+
+class RopeDesc(ctypes.Structure):
+    _fields_ = [("head_dim", ctypes.c_int32), ("rot_dim", ctypes.c_int32), ("n_axes", ctypes.c_int32),
+                ("interleaved", ctypes.c_int32), ("scale", ctypes.c_double), ("inv_freq", ctypes.c_void_p),
+                ("axis", ctypes.c_void_p), ("table", ctypes.c_void_p), ("table_bytes", ctypes.c_size_t)]
 
 
 class Counters(ctypes.Structure):
@@ -107,6 +116,20 @@ def lib() -> ctypes.CDLL:
                                                vp, vp]
         L.kv_page_scores_update.argtypes = [vp, i32, i32, vp, vp, vp, vp, ctypes.c_float, vp, vp,
                                             vp, vp]
+        i64 = ctypes.c_int64
+        L.kv_rope_bytes.argtypes = [i32, vp]
+        L.kv_rope_create.argtypes = [vp, vp]
+        L.kv_rope_destroy.argtypes = [vp]
+        L.kv_rope_apply.argtypes = [vp, i32, i32, vp, i64, vp, vp, i64, vp]
+        L.kv_append_fp8_rope.argtypes = [vp, vp, i32, i32, vp, vp, i32, vp, vp, i32, vp, vp, i64, vp, i64, vp]
+        L.paged_attn_decode_append_rope.argtypes = [vp, vp, i32, i32, vp, vp, vp, vp, vp, vp, i32, vp, vp, vp,
+                                                    vp, sz, vp]
+        L.kv_page_bounds_bytes.argtypes = [vp, i32, i32, vp, vp]
+        L.kv_page_bounds_update.argtypes = [vp, i32, i32, vp, vp, i32, vp, vp, vp, sz, vp, sz, vp]
+        L.paged_attn_select_workspace_bytes.argtypes = [vp, i32, i32, vp]
+        L.paged_attn_select_pages.argtypes = [vp, i32, i32, vp, vp, i32, vp, sz, vp, sz, i32, i32, i32, vp, vp,
+                                              vp, sz, vp]
+        L.paged_attn_decode_sparse.argtypes = [vp, i32, i32, vp, vp, vp, i32, vp, i32, vp, vp, vp, vp, vp, sz, vp]
         L.mkv_control_bf16_write.argtypes = [vp, i32, i32, i32, i32, i32, i32, vp, i32, vp, vp, i32,
                                              vp, vp, vp]
         L.mkv_control_bf16_workspace_bytes.argtypes = [i32, i32, i32, i32, i32, vp]
@@ -311,6 +334,155 @@ def paged_attn_decode_append(pool: Pool, layer, q, k_new, v_new, block_table, ta
     _check("paged_attn_decode_append", lib().paged_attn_decode_append(
         pool.handle, layer, n_req, _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(block_table),
         _ptr(tags), max_pages, _ptr(seq_lens_before), _ptr(out), _ptr(lse), _ptr(ws),
+        ws.numel() * ws.element_size(), _stream(stream)))
+
+
+class Rope:
+    """Rotary positions (kv_rope): pair i of a head turns by positions[axis[i]] *
+    inv_freq[i].  2 * len(inv_freq) channels are rotated, pairs (i, i + half) or,
+    interleaved, (2i, 2i + 1).  The table lives in a torch tensor of this object."""
+
+    def __init__(self, head_dim, inv_freq, axis=None, n_axes=1, interleaved=False, scale=1.0, device="cuda"):
+        import torch
+        f = np.ascontiguousarray(inv_freq, dtype=np.float64)
+        ax = None if axis is None else np.ascontiguousarray(axis, dtype=np.uint8)
+        if f.ndim != 1 or (ax is not None and ax.shape != f.shape):
+            raise ValueError("inv_freq is a vector and axis, if given, one of the same length")
+        self.head_dim, self.rot_dim, self.n_axes = head_dim, 2 * f.size, n_axes
+        b = ctypes.c_size_t()
+        _check("kv_rope_bytes", lib().kv_rope_bytes(self.rot_dim, ctypes.byref(b)))
+        self.table = torch.zeros(b.value, dtype=torch.uint8, device=device)
+        desc = RopeDesc(head_dim, self.rot_dim, n_axes, int(bool(interleaved)), float(scale), f.ctypes.data,
+                        None if ax is None else ax.ctypes.data, self.table.data_ptr(), b.value)
+        h = ctypes.c_void_p()
+        torch.cuda.synchronize()
+        _check("kv_rope_create", lib().kv_rope_create(ctypes.byref(desc), ctypes.byref(h)))
+        self.handle = h
+
+    def close(self):
+        if getattr(self, "handle", None):
+            lib().kv_rope_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+def _rows(t):
+    """Elements from one row [heads][d] of t to the next; the heads lie together."""
+    d = t.shape[-1]
+    if t.stride(-1) != 1 or (t.shape[-2] > 1 and t.stride(-2) != d):
+        raise ValueError("rows are [heads][head_dim] without gaps")
+    n = t.shape[-3]
+    stride = t.stride(-3) if n > 1 else max(t.shape[-2] * d, t.stride(-3))
+    if t.dim() == 4 and t.shape[0] > 1 and t.stride(0) != n * stride:
+        raise ValueError("one layer's rows follow the other's")
+    return stride
+
+
+def _positions(rope, positions, n):
+    if positions is not None and (tuple(positions.shape) != (rope.n_axes, n) or not positions.is_contiguous()):
+        raise ValueError(f"positions are contiguous int32 [{rope.n_axes}][{n}]")
+    return _ptr(positions)
+
+
+def kv_rope_apply(rope: Rope, x, positions, out, stream=None):
+    """Rotate bf16 rows x [n][heads][head_dim] (int16 bits, tokens may be strided) into out;
+    positions: int32 [n_axes][n]."""
+    n, heads, d = x.shape
+    if tuple(out.shape) != tuple(x.shape) or d != rope.head_dim:
+        raise ValueError("x and out are [n][heads][head_dim]")
+    _check("kv_rope_apply", lib().kv_rope_apply(
+        rope.handle, n, heads, _ptr(x), _rows(x), _positions(rope, positions, n), _ptr(out), _rows(out),
+        _stream(stream)))
+
+
+def kv_append_fp8_rope(pool: Pool, rope: Rope, layer, block_table, tags, seq_lens_before, cu_new_tokens,
+                       positions, k, v, stream=None):
+    """kv_append_fp8 with the keys rotated on the way; k, v: [n][H][d] of one layer or
+    [n_layers][n][H][d], tokens may be strided; positions: int32 [n_axes][n] or None."""
+    n_req, max_pages = block_table.shape
+    n = int(k.shape[-3])
+    _check("kv_append_fp8_rope", lib().kv_append_fp8_rope(
+        pool.handle, rope.handle, layer, n_req, _ptr(block_table), _ptr(tags), max_pages, _ptr(seq_lens_before),
+        _ptr(cu_new_tokens), n, _positions(rope, positions, n), _ptr(k), _rows(k), _ptr(v), _rows(v),
+        _stream(stream)))
+
+
+def paged_attn_decode_append_rope(pool: Pool, rope: Rope, layer, q, k_new, v_new, positions, block_table, tags,
+                                  seq_lens_before, out, lse, ws, stream=None):
+    """paged_attn_decode_append with q and k_new rotated in the launch; positions: int32
+    [n_axes][n_req] or None (the token's place in the cache)."""
+    n_req, max_pages = block_table.shape
+    _check("paged_attn_decode_append_rope", lib().paged_attn_decode_append_rope(
+        pool.handle, rope.handle, layer, n_req, _ptr(q), _ptr(k_new), _ptr(v_new),
+        _positions(rope, positions, n_req), _ptr(block_table), _ptr(tags), max_pages, _ptr(seq_lens_before),
+        _ptr(out), _ptr(lse), _ptr(ws), ws.numel() * ws.element_size(), _stream(stream)))
+
+
+class PageBounds:
+    """Channelwise extremes of the keys of every logical page, for page selection:
+    codes uint8 (E4M3) [n_layers][n_req][H][max_pages][2][d] (largest, smallest) and
+    scales float32 [n_layers][n_req][H][max_pages]."""
+
+    def __init__(self, pool: Pool, n_req, max_pages, device="cuda"):
+        import torch
+        c, s = ctypes.c_size_t(), ctypes.c_size_t()
+        _check("kv_page_bounds_bytes", lib().kv_page_bounds_bytes(pool.handle, n_req, max_pages,
+                                                                  ctypes.byref(c), ctypes.byref(s)))
+        shape = (pool.n_layers, n_req, pool.n_kv_heads, max_pages)
+        self.n_req, self.max_pages = n_req, max_pages
+        self.codes = torch.zeros((*shape, 2, pool.d), dtype=torch.uint8, device=device)
+        self.scales = torch.zeros(shape, dtype=torch.float32, device=device)
+        assert self.codes.numel() == c.value and self.scales.numel() * 4 == s.value
+
+    def _args(self):
+        return _ptr(self.codes), self.codes.numel(), _ptr(self.scales), 4 * self.scales.numel()
+
+
+def kv_page_bounds_update(pool: Pool, layer, block_table, tags, seq_lens_from, seq_lens, bounds: PageBounds,
+                          stream=None):
+    """Recompute the bounds of the pages that hold tokens [seq_lens_from, seq_lens)."""
+    n_req, max_pages = block_table.shape
+    if (n_req, max_pages) != (bounds.n_req, bounds.max_pages):
+        raise ValueError("the bounds are those of another table shape")
+    _check("kv_page_bounds_update", lib().kv_page_bounds_update(
+        pool.handle, layer, n_req, _ptr(block_table), _ptr(tags), max_pages, _ptr(seq_lens_from), _ptr(seq_lens),
+        *bounds._args(), _stream(stream)))
+
+
+def select_workspace(pool: Pool, n_req, max_pages, device="cuda"):
+    import torch
+    b = ctypes.c_size_t()
+    _check("paged_attn_select_workspace_bytes", lib().paged_attn_select_workspace_bytes(
+        pool.handle, n_req, max_pages, ctypes.byref(b)))
+    return torch.empty(b.value, dtype=torch.uint8, device=device)
+
+
+def paged_attn_select_pages(pool: Pool, layer, q, seq_lens, bounds: PageBounds, n_first, n_last, pages, counts, ws,
+                            stream=None):
+    """Per request and KV head the pages to attend to: pages int32 [n_req][H][n_select]
+    (ascending, -1 behind), counts int32 [n_req][H]; q is the rotated query."""
+    n_req, H, n_select = pages.shape
+    if n_req != bounds.n_req or H != pool.n_kv_heads or tuple(counts.shape) != (n_req, H):
+        raise ValueError("pages are [n_req][H][n_select], counts [n_req][H]")
+    _check("paged_attn_select_pages", lib().paged_attn_select_pages(
+        pool.handle, layer, n_req, _ptr(q), _ptr(seq_lens), bounds.max_pages, *bounds._args(), n_select, n_first,
+        n_last, _ptr(pages), _ptr(counts), _ptr(ws), ws.numel() * ws.element_size(), _stream(stream)))
+
+
+def paged_attn_decode_sparse(pool: Pool, layer, q, block_table, tags, seq_lens, pages, counts, out, lse, ws,
+                             stream=None):
+    """paged_attn_decode over the listed logical pages of each request and KV head."""
+    n_req, max_pages = block_table.shape
+    if pages.dim() != 3 or tuple(pages.shape[:2]) != (n_req, pool.n_kv_heads) or tuple(counts.shape) != tuple(pages.shape[:2]):
+        raise ValueError("pages are [n_req][H][n_select], counts [n_req][H]")
+    _check("paged_attn_decode_sparse", lib().paged_attn_decode_sparse(
+        pool.handle, layer, n_req, _ptr(q), _ptr(block_table), _ptr(tags), max_pages, _ptr(seq_lens),
+        int(pages.shape[2]), _ptr(pages), _ptr(counts), _ptr(out), _ptr(lse), _ptr(ws),
         ws.numel() * ws.element_size(), _stream(stream)))
 
 

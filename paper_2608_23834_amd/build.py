@@ -23,14 +23,14 @@ COMMON = [
     "-I", os.path.join(ROOT, "include"),
 ]
 # TUs whose bit-exact outputs must follow single IEEE operations in order
-EXACT = {"mkv_pool_kernels.hip"}
+EXACT = {"mkv_pool_kernels.hip", "mkv_rope.hip", "mkv_sparse.hip"}
 # Per-TU extra flags.  The chunk kernel keeps its MFMA accumulators in
 # ordinary VGPRs: with the accumulator-register form the compiler copied all
 # 128 output accumulators into VGPRs on every pass of the stage loop (for the
 # rarely taken rescale branch).
 EXTRA = {"mkv_chunk.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
 SOURCES = ["mkv_api.hip", "mkv_pool_kernels.hip", "mkv_decode.hip", "mkv_chunk.hip", "mkv_probe.hip",
-           "mkv_control.hip"]
+           "mkv_control.hip", "mkv_rope.hip", "mkv_sparse.hip"]
 
 
 def _compile(src: str) -> str:

@@ -53,6 +53,11 @@ bool is_permutation(const int32_t* o, int n) {
   return true;
 }
 
+// rows of `width` elements, `stride` apart, read and written in 8-byte pieces
+bool good_rows(const void* p, int64_t stride, int64_t width) {
+  return (reinterpret_cast<uintptr_t>(p) & 7) == 0 && stride % 4 == 0 && stride >= width;
+}
+
 mkv_status hip_status(hipError_t e) { return e == hipSuccess ? MKV_OK : MKV_EHIP; }
 
 }  // namespace
@@ -346,6 +351,193 @@ mkv_status paged_attn_decode_append(mkv_pool* pool, int32_t layer, int32_t n_req
     if (pool->timing) pool->timed = 1;
   }
   return st;
+}
+
+mkv_status paged_attn_decode_append_rope(mkv_pool* pool, const kv_rope* rope, int32_t layer, int32_t n_req,
+                                         const uint16_t* q, const uint16_t* k_new, const uint16_t* v_new,
+                                         const int32_t* positions, int32_t* block_table, uint8_t* tags,
+                                         int32_t max_pages, const int32_t* seq_lens_before, float* out,
+                                         float* lse, void* ws, size_t ws_bytes, hipStream_t stream) {
+  if (!pool || !rope || !q || !k_new || !v_new || !block_table || !tags || !seq_lens_before || !out || !ws)
+    return MKV_EINVAL;
+  if (n_req < 1 || max_pages < 1 || rope->head_dim != pool->d) return MKV_EINVAL;
+  if (!aligned16(q) || !aligned16(out) || !aligned16(ws)) return MKV_EINVAL;
+  if ((reinterpret_cast<uintptr_t>(k_new) | reinterpret_cast<uintptr_t>(v_new)) & 7) return MKV_EINVAL;
+  if (layer < 0 || layer >= pool->n_layers) return MKV_ERANGE;
+  if (n_req > 65535 || max_pages > 1024 * 256) return MKV_ERANGE;
+  if (ws_bytes < decode_ws_bytes(n_req, max_pages, pool->n_kv_heads, pool->group, pool->d, pool->recent))
+    return MKV_ENOMEM;
+  mkv_status st = hip_status(launch_decode(view_of(pool), layer, n_req, q, block_table, tags,
+                                           max_pages, seq_lens_before, out, lse, ws, stream,
+                                           pool->timing ? pool->timing_ev : nullptr, k_new, v_new,
+                                           block_table, tags, nullptr, &rope->view, positions));
+  if (st == MKV_OK) {
+    pool->decode_routes++;
+    if (pool->timing) pool->timed = 1;
+  }
+  return st;
+}
+
+mkv_status paged_attn_decode_sparse(mkv_pool* pool, int32_t layer, int32_t n_req, const uint16_t* q,
+                                    const int32_t* block_table, const uint8_t* tags, int32_t max_pages,
+                                    const int32_t* seq_lens, int32_t n_select, const int32_t* pages,
+                                    const int32_t* counts, float* out, float* lse, void* ws, size_t ws_bytes,
+                                    hipStream_t stream) {
+  if (!pool || !q || !block_table || !tags || !seq_lens || !pages || !counts || !out || !ws) return MKV_EINVAL;
+  if (n_req < 1 || max_pages < 1 || n_select < 1) return MKV_EINVAL;
+  if (!aligned16(q) || !aligned16(out) || !aligned16(ws)) return MKV_EINVAL;
+  if (layer < 0 || layer >= pool->n_layers) return MKV_ERANGE;
+  if (n_req > 65535 || max_pages > 1024 * 256 || n_select > 1024 * 256) return MKV_ERANGE;
+  if (ws_bytes < decode_ws_bytes(n_req, n_select, pool->n_kv_heads, pool->group, pool->d, 0)) return MKV_ENOMEM;
+  mkv_status st = hip_status(launch_decode(view_of(pool), layer, n_req, q, block_table, tags, max_pages, seq_lens,
+                                           out, lse, ws, stream, pool->timing ? pool->timing_ev : nullptr, nullptr,
+                                           nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, pages, counts,
+                                           n_select));
+  if (st == MKV_OK) {
+    pool->decode_routes++;
+    if (pool->timing) pool->timed = 1;
+  }
+  return st;
+}
+
+mkv_status kv_rope_bytes(int32_t rot_dim, size_t* bytes) {
+  if (!bytes || rot_dim < 2 || rot_dim % 2 || rot_dim > 256) return MKV_EINVAL;
+  *bytes = (size_t)(rot_dim / 2) * sizeof(RopeEntry);
+  return MKV_OK;
+}
+
+mkv_status kv_rope_create(const kv_rope_desc* desc, kv_rope** out) {
+  if (!out) return MKV_EINVAL;
+  *out = nullptr;
+  if (!desc || !desc->inv_freq || !desc->table) return MKV_EINVAL;
+  if (desc->head_dim != 128 && desc->head_dim != 256) return MKV_EUNSUP;
+  if (desc->rot_dim < 2 || desc->rot_dim % 2 || desc->rot_dim > desc->head_dim) return MKV_EINVAL;
+  if (desc->n_axes < 1 || desc->n_axes > ROPE_MAX_AXES) return MKV_EUNSUP;
+  if (!(desc->scale > 0.0 && desc->scale <= 1e6)) return MKV_ERANGE;
+  const int m = desc->rot_dim / 2;
+  std::vector<RopeEntry> tab((size_t)m);
+  for (int i = 0; i < m; ++i) {
+    const double f = desc->inv_freq[i];
+    if (!(f >= -4.0 && f <= 4.0)) return MKV_ERANGE;  // (NaN too)
+    const int ax = desc->axis ? desc->axis[i] : 0;
+    if (ax >= desc->n_axes) return MKV_ERANGE;
+    tab[(size_t)i] = {f, ax, 0};
+  }
+  if (desc->table_bytes < (size_t)m * sizeof(RopeEntry)) return MKV_ENOMEM;
+  if (!aligned16(desc->table)) return MKV_EINVAL;
+  if (hipMemcpy(desc->table, tab.data(), tab.size() * sizeof(RopeEntry), hipMemcpyHostToDevice) != hipSuccess)
+    return MKV_EHIP;
+  kv_rope* r = new (std::nothrow) kv_rope;
+  if (!r) return MKV_ENOMEM;
+  r->head_dim = desc->head_dim;
+  r->view.tab = static_cast<const RopeEntry*>(desc->table);
+  r->view.scale = desc->scale;
+  r->view.rot = desc->rot_dim;
+  r->view.n_axes = desc->n_axes;
+  r->view.interleaved = desc->interleaved != 0;
+  *out = r;
+  return MKV_OK;
+}
+
+mkv_status kv_rope_destroy(kv_rope* rope) {
+  if (!rope) return MKV_EINVAL;
+  delete rope;
+  return MKV_OK;
+}
+
+mkv_status kv_rope_apply(const kv_rope* rope, int32_t n_tokens, int32_t n_heads, const uint16_t* x,
+                         int64_t x_stride, const int32_t* positions, uint16_t* out, int64_t out_stride,
+                         hipStream_t stream) {
+  if (!rope || n_tokens < 0 || n_heads < 1) return MKV_EINVAL;
+  if (n_tokens == 0) return MKV_OK;
+  if (!x || !positions || !out) return MKV_EINVAL;
+  if ((int64_t)n_heads * rope->head_dim > ((int64_t)1 << 30) || x_stride > ((int64_t)1 << 31) ||
+      out_stride > ((int64_t)1 << 31))
+    return MKV_ERANGE;
+  const int64_t width = (int64_t)n_heads * rope->head_dim;
+  if (!good_rows(x, x_stride, width) || !good_rows(out, out_stride, width)) return MKV_EINVAL;
+  if (!(x == out && x_stride == out_stride)) {  // in place, or apart
+    const uintptr_t a = reinterpret_cast<uintptr_t>(x), b = reinterpret_cast<uintptr_t>(out);
+    const uintptr_t na = 2 * (uintptr_t)((n_tokens - 1) * x_stride + width);
+    const uintptr_t nb = 2 * (uintptr_t)((n_tokens - 1) * out_stride + width);
+    if (a < b + nb && b < a + na) return MKV_EINVAL;
+  }
+  return hip_status(launch_rope_apply(rope->view, rope->head_dim, n_tokens, n_heads, x, x_stride, positions, out,
+                                      out_stride, stream));
+}
+
+mkv_status kv_append_fp8_rope(mkv_pool* pool, const kv_rope* rope, int32_t layer, int32_t n_req,
+                              int32_t* block_table, uint8_t* tags, int32_t max_pages,
+                              const int32_t* seq_lens_before, const int32_t* cu_new_tokens, int32_t n_new_total,
+                              const int32_t* positions, const uint16_t* k, int64_t k_stride, const uint16_t* v,
+                              int64_t v_stride, hipStream_t stream) {
+  if (!pool || !rope || !block_table || !tags || !seq_lens_before || !cu_new_tokens) return MKV_EINVAL;
+  if (n_req < 1 || max_pages < 1 || n_new_total < 0 || rope->head_dim != pool->d) return MKV_EINVAL;
+  if (n_new_total > 0) {
+    if (!k || !v) return MKV_EINVAL;
+    const int64_t width = (int64_t)pool->n_kv_heads * pool->d;
+    if (k_stride > ((int64_t)1 << 31) || v_stride > ((int64_t)1 << 31)) return MKV_ERANGE;
+    if (!good_rows(k, k_stride, width) || !good_rows(v, v_stride, width)) return MKV_EINVAL;
+  }
+  if (layer != MKV_ALL_LAYERS && (layer < 0 || layer >= pool->n_layers)) return MKV_ERANGE;
+  return hip_status(launch_append_rope(view_of(pool), rope->view, layer, n_req, block_table, tags, max_pages,
+                                       seq_lens_before, cu_new_tokens, n_new_total, positions, k, k_stride, v,
+                                       v_stride, stream));
+}
+
+mkv_status kv_page_bounds_bytes(const mkv_pool* pool, int32_t n_req, int32_t max_pages, size_t* code_bytes,
+                                size_t* scale_bytes) {
+  if (!pool || n_req < 1 || max_pages < 1) return MKV_EINVAL;
+  const size_t rows = (size_t)pool->n_layers * n_req * pool->n_kv_heads * max_pages;
+  if (code_bytes) *code_bytes = rows * 2 * pool->d;
+  if (scale_bytes) *scale_bytes = rows * sizeof(float);
+  return MKV_OK;
+}
+
+static mkv_status check_bounds(const mkv_pool* pool, int32_t n_req, int32_t max_pages, const void* codes,
+                               size_t code_bytes, const void* scales, size_t scale_bytes) {
+  if (!codes || !scales || !aligned16(codes) || (reinterpret_cast<uintptr_t>(scales) & 3)) return MKV_EINVAL;
+  if (n_req > 65535 || max_pages > 1024 * 256) return MKV_ERANGE;
+  size_t c, s;
+  mkv_status st = kv_page_bounds_bytes(pool, n_req, max_pages, &c, &s);
+  if (st != MKV_OK) return st;
+  return code_bytes < c || scale_bytes < s ? MKV_ENOMEM : MKV_OK;
+}
+
+mkv_status kv_page_bounds_update(mkv_pool* pool, int32_t layer, int32_t n_req, const int32_t* block_table,
+                                 const uint8_t* tags, int32_t max_pages, const int32_t* seq_lens_from,
+                                 const int32_t* seq_lens, uint8_t* codes, size_t code_bytes, float* scales,
+                                 size_t scale_bytes, hipStream_t stream) {
+  if (!pool || !block_table || !tags || !seq_lens_from || !seq_lens || n_req < 1 || max_pages < 1) return MKV_EINVAL;
+  if (layer != MKV_ALL_LAYERS && (layer < 0 || layer >= pool->n_layers)) return MKV_ERANGE;
+  mkv_status st = check_bounds(pool, n_req, max_pages, codes, code_bytes, scales, scale_bytes);
+  if (st != MKV_OK) return st;
+  return hip_status(launch_page_bounds(view_of(pool), layer, n_req, block_table, tags, max_pages, seq_lens_from,
+                                       seq_lens, codes, scales, stream));
+}
+
+mkv_status paged_attn_select_workspace_bytes(const mkv_pool* pool, int32_t n_req, int32_t max_pages, size_t* bytes) {
+  if (!pool || !bytes || n_req < 1 || max_pages < 1) return MKV_EINVAL;
+  *bytes = select_ws_bytes(n_req, max_pages, pool->n_kv_heads);
+  return MKV_OK;
+}
+
+mkv_status paged_attn_select_pages(mkv_pool* pool, int32_t layer, int32_t n_req, const uint16_t* q,
+                                   const int32_t* seq_lens, int32_t max_pages, const uint8_t* codes,
+                                   size_t code_bytes, const float* scales, size_t scale_bytes, int32_t n_select,
+                                   int32_t n_first, int32_t n_last, int32_t* pages, int32_t* counts, void* ws,
+                                   size_t ws_bytes, hipStream_t stream) {
+  if (!pool || !q || !seq_lens || !pages || !counts || !ws) return MKV_EINVAL;
+  if (n_req < 1 || max_pages < 1 || n_select < 1 || n_first < 0 || n_last < 0) return MKV_EINVAL;
+  if ((int64_t)n_first + n_last > n_select) return MKV_EINVAL;
+  if (!aligned16(q) || !aligned16(ws)) return MKV_EINVAL;
+  if (layer < 0 || layer >= pool->n_layers || n_select > 1024 * 256) return MKV_ERANGE;
+  mkv_status st = check_bounds(pool, n_req, max_pages, codes, code_bytes, scales, scale_bytes);
+  if (st != MKV_OK) return st;
+  if (pool->n_kv_heads > 65535) return MKV_EUNSUP;
+  if (ws_bytes < select_ws_bytes(n_req, max_pages, pool->n_kv_heads)) return MKV_ENOMEM;
+  return hip_status(launch_select(view_of(pool), layer, n_req, q, seq_lens, max_pages, codes, scales, n_select,
+                                  n_first, n_last, pages, counts, ws, stream));
 }
 
 mkv_status paged_attn_set_deterministic(mkv_pool* pool, int32_t enable) {

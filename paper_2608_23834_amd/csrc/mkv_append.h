@@ -11,6 +11,7 @@
 
 #include "mkv_device.h"
 #include "mkv_internal.h"
+#include "mkv_rope.h"
 
 namespace mkv {
 
@@ -33,13 +34,14 @@ struct SmallTask {
   bool have_old;
 };
 
+// the task's new rows; row i of layer li of k (v) is at k + (li n_new_total + i) kts
 template <int D>
-__device__ __forceinline__ void small_task_load_x(SmallTask<D>& T, int H, int n_new_total,
+__device__ __forceinline__ void small_task_load_x(SmallTask<D>& T, int64_t kts, int64_t vts, int n_new_total,
                                                   const uint16_t* k, const uint16_t* v, int lane) {
   constexpr int D4 = SmallTask<D>::D4;
-  const uint16_t* src = (T.kv ? v : k) + (int64_t)T.li * n_new_total * H * D;
-  const uint16_t* srow = src + ((int64_t)T.row0 * H + T.h) * D;  // token t at srow[t * H * D + c]
-  const int64_t tstride = (int64_t)H * D;
+  const int64_t tstride = T.kv ? vts : kts;
+  const uint16_t* src = (T.kv ? v : k) + (int64_t)T.li * n_new_total * tstride;
+  const uint16_t* srow = src + T.row0 * tstride + (int64_t)T.h * D;  // token t at srow[t * tstride + c]
   const int n4 = (T.t1 - T.t0) * D4;
 #pragma unroll
   for (int j = 0; j < SmallTask<D>::NC; ++j) {
@@ -51,6 +53,41 @@ __device__ __forceinline__ void small_task_load_x(SmallTask<D>& T, int H, int n_
     }
   }
   (void)lane;
+}
+
+// Rotate a key task's rows (x as loaded) by their positions, through an LDS block of the
+// rows [token][channel] (xs, at least (t1 - t0) D bf16): one lane per (token, pair), so an
+// angle is evaluated once and any pairing is the same code.
+template <int D>
+__device__ __forceinline__ void small_task_rotate(SmallTask<D>& T, const RopeView& R, const int32_t* pos,
+                                                  int n_pos, uint16_t* xs, int lane) {
+  constexpr int D4 = SmallTask<D>::D4;
+  const int nt = T.t1 - T.t0, n4 = nt * D4, m = R.rot / 2;
+#pragma unroll
+  for (int j = 0; j < SmallTask<D>::NC; ++j) {
+    const int idx = lane + 64 * j;
+    if (idx < n4) reinterpret_cast<uint2*>(xs)[idx] = T.x[j];
+  }
+  __builtin_amdgcn_wave_barrier();
+  for (int it = lane; it < nt * m; it += 64) {
+    const int t = it / m, i = it - t * m;
+    const RopeEntry e = R.tab[i];
+    const double th = rope_pos(pos, n_pos, (int64_t)T.row0 + T.t0 + t, e.axis, T.p * PAGE + T.t0 + t) * e.freq;
+    double c, s, y0, y1;
+    rope_cos_sin(th, R.scale, c, s);
+    const int2 pr = rope_pair(R, i);
+    uint16_t* x = xs + t * D;
+    rope_rotate((double)bf16_to_f32(x[pr.x]), (double)bf16_to_f32(x[pr.y]), c, s, y0, y1);
+    x[pr.x] = (uint16_t)f64_to_bf16(y0);
+    x[pr.y] = (uint16_t)f64_to_bf16(y1);
+  }
+  __builtin_amdgcn_wave_barrier();
+#pragma unroll
+  for (int j = 0; j < SmallTask<D>::NC; ++j) {
+    const int idx = lane + 64 * j;
+    if (idx < n4) T.x[j] = reinterpret_cast<const uint2*>(xs)[idx];
+  }
+  __builtin_amdgcn_wave_barrier();  // xs is free
 }
 
 // codes and scale of page-head (T.layer, id, T.h), part T.kv; only a page with

@@ -46,6 +46,7 @@
 #include "mkv_append.h"
 #include "mkv_attn.h"
 #include "mkv_internal.h"
+#include "mkv_rope.h"
 #include "../../include/minima_kv.h"
 
 namespace mkv {
@@ -107,6 +108,15 @@ struct DecodeArgs {
   // softmax mass sum_i 2^(s_i - m) and the reference exponent m it was taken
   // against (base 2, units of the scaled scores)
   float2* page_mass;
+  // ROPE instance (with APP): q and k_new come unrotated and are turned by their token's
+  // positions [n_axes][n_req], or by its place in the cache where pos is null
+  RopeView rope;
+  const int32_t* pos;
+  // SPARSE instance: per (request, KV head) the logical pages to attend to, strictly
+  // ascending, sel_count of n_sel
+  const int32_t* sel;
+  const int32_t* sel_count;
+  int n_sel;
 };
 
 // Cost of a request's pages: n_old pages wholly outside the Recent window and
@@ -207,6 +217,17 @@ constexpr float M_INIT = -1.0e30f;
 // its four significant bits) or 2^-10, half E4M3's smallest step: 2^-15 of the head's
 // largest entry at most, and down to 2^-18 for small ones.
 constexpr int QF8_TERMS = 3;
+// The rotating and sparse instances (FINE) are as exact as fp32 attention instead: their
+// rotated query is an fp16 hi + lo pair (22 bits of each entry, under a power-of-two head
+// scale that puts the largest in [2^14, 2^15)) on the f16 MFMA.  More E4M3 terms would not
+// do: the fp8 product keeps little below a group's largest term (random operands of 14
+// octaves came out 5e-5 off, f16 ones rounded like fp32).  The plain query gets a scale
+// of the same kind, so that no bf16 entry that matters leaves fp16's range.
+// bytes of the query operands in LDS: the rotated query, then the plain one
+__host__ __device__ constexpr int rot_query_bytes(bool fine, int d) {
+  return fine ? 2 * (d / 32) * 64 * 16 : QF8_TERMS * (d / 128) * 64 * 32;
+}
+__host__ __device__ constexpr int query_bytes(bool fine, int d) { return rot_query_bytes(fine, d) + (d / 32) * 64 * 16; }
 
 // Column layout of a score tile (and row layout of the PV accumulator).  With
 // at most six heads per KV head, heads sit in columns 4 k + i, i < 3, so that
@@ -221,13 +242,18 @@ __device__ __forceinline__ int head_of_col(int c) {
 // the page that owns column ln).  Weights are returned in place.  The
 // accumulator rows 4*lg + i belong to columns 4*lg + i, whose rescale factors
 // are fetched from those lanes when the reference max moves.
-template <int D, int NI>
+// FINE: the reference is set 2^-7 below the max and kept up to 2^15, so that the largest
+// weights are 2^7 to 2^15 and the fp16 pair of one (p_operand), which cannot hold less than
+// 2^-25, cuts off 2^-32 of them instead of 2^-25 (with it weights of 2^-10 of the largest
+// were off by 2^-15: the output of one 2,048-token request by 1.3e-5, now 1e-6).
+template <int D, int NI, bool FINE>
 __device__ __forceinline__ void softmax_step(WaveState<D>& st, float* sc, int lg) {
+  constexpr float BELOW = FINE ? 7.0f : 0.0f;
   const float mx = max4rows(fmaxf(fmaxf(sc[0], sc[1]), fmaxf(sc[2], sc[3])));
   // lazy rescale: keep the reference max while new scores stay within 2^8
-  const bool need = mx > st.m_run + 8.0f;
+  const bool need = mx > st.m_run + (8.0f + BELOW);
   if (__any(need)) {
-    const float m_new = need ? mx : st.m_run;
+    const float m_new = need ? mx - BELOW : st.m_run;
     const float alpha = __builtin_amdgcn_exp2f(st.m_run - m_new);
     st.l_run *= alpha;
     st.m_run = m_new;
@@ -275,9 +301,13 @@ __device__ __forceinline__ void p_operand(const float* p, bool row_is_b, half8& 
 // PAIR (query group of at most 8 heads): two pages share one score tile,
 // columns [0, 8) scoring page a and [8, 16) page b.  G6: at most six heads
 // (see head_of_col).
-template <int D, bool PAIR, bool G6, bool APP, bool SCORE = false>
+// ROPE, SPARSE: see DecodeArgs.
+template <int D, bool PAIR, bool G6, bool APP, bool SCORE = false, bool ROPE = false, bool SPARSE = false>
 __global__ __launch_bounds__(DecodeCfg<PAIR>::NT, PAIR && D == 128 ? 4 : 2) void decode_kernel(DecodeArgs a) {
   static_assert(!(APP && SCORE), "the scoring instance has no fused append");
+  static_assert(APP || !ROPE, "rotation comes with the append");
+  static_assert(!SPARSE || (!APP && !SCORE), "a page list comes with neither");
+  constexpr bool FINE = ROPE || SPARSE;  // outputs as exact as fp32 attention's
   constexpr int NW = DecodeCfg<PAIR>::NW, NT = DecodeCfg<PAIR>::NT, SLOTS = DecodeCfg<PAIR>::SLOTS;
   constexpr int NCH = NCH_OF(PAIR);  // query heads a score tile holds
   constexpr int CL = D / 16, NDW = 3 * D / 128, CB = 3 * D / 32, NS = D / 32, QV = D / 64;
@@ -314,8 +344,11 @@ __global__ __launch_bounds__(DecodeCfg<PAIR>::NT, PAIR && D == 128 ? 4 : 2) void
                "s"(P.recent), "s"(mp), "s"(a.n_req), "s"(P.tq3), "s"(P.fp8), "s"(a.partials));
   // LDS: [rotated query as E4M3 terms][plain-query operand][page ring | wave merge]
   uint8_t* qf8 = smem;  // [term][step][lane][32 bytes], see the query build below
-  half8* qpl = reinterpret_cast<half8*>(smem + QF8_TERMS * NK8 * 64 * 32);  // plain query (bf16 -> fp16 is exact)
-  uint8_t* ring = smem + QF8_TERMS * NK8 * 64 * 32 + NS * 64 * 16;
+  half8* qpl = reinterpret_cast<half8*>(smem + rot_query_bytes(FINE, D));  // plain query (bf16 -> fp16 is exact)
+  half8* qrh = reinterpret_cast<half8*>(smem);  // FINE: rotated query, hi then lo, laid out as qpl
+  half8* qrl = qrh + NS * 64;
+  uint8_t* ring = smem + query_bytes(FINE, D);
+  __shared__ float s_pinv[FINE ? 16 : 1];  // FINE: 1 / the plain query's scale
   __shared__ float s_qinv[16];  // per score column: 1 / the power-of-two scale of its terms
 
   // ---- 1. queries: wave w owns score columns w and w + NW below NCH (the
@@ -338,16 +371,33 @@ __global__ __launch_bounds__(DecodeCfg<PAIR>::NT, PAIR && D == 128 ? 4 : 2) void
   }
 #pragma unroll
   for (int i = 0; i < QV; ++i) sg[i] = P.sigma[QV * lane + i];
+  // ROPE: the angles of the request's token, one lane each (rot / 2 <= 128 of the 512 lanes)
+  [[maybe_unused]] double turn_f = 0.0;
+  [[maybe_unused]] int turn_axis = 0, turn_pos[ROPE_MAX_AXES] = {0, 0, 0, 0};
+  if constexpr (ROPE) {
+    if (tid < a.rope.rot / 2) {
+      const RopeEntry e = a.rope.tab[tid];
+      turn_f = e.freq;
+      turn_axis = e.axis;
+    }
+    if (a.pos) {
+#pragma unroll
+      for (int i = 0; i < ROPE_MAX_AXES; ++i)
+        turn_pos[i] = a.pos[(int64_t)min(i, a.rope.n_axes - 1) * a.n_req + r];
+    }
+  }
 
   float* part = a.partials + (((int64_t)r * H + h) * a.max_chunks + chunk) * part_stride(G, D);
   // ---- chunk -> logical page range: equal-cost ranges over the table width,
   // known before any load, so the sequence length and the chunk's tags and
   // ids are loaded together; pages at or past the request's end are dropped
   // once the length is in (chunk < max_chunks, so the range is not empty)
-  const int n_old_t = (int)old_pages((int64_t)mp * PAGE, P.recent);
+  // (a page list: ranges of its entries, all at the cost of an old page)
+  const int n_ent = SPARSE ? a.n_sel : mp;
+  const int n_old_t = SPARSE ? a.n_sel : (int)old_pages((int64_t)mp * PAGE, P.recent);
   const int64_t c0 = (int64_t)chunk * a.cunits;
   const int p0 = page_at_cost(c0, n_old_t);
-  const int p1 = page_at_cost(min(request_cost(mp, n_old_t), c0 + a.cunits), n_old_t);
+  const int p1 = page_at_cost(min(request_cost(n_ent, n_old_t), c0 + a.cunits), n_old_t);
   const int n_pr = p1 - p0;
   // ---- 2. per-format compact lists of the chunk (logical order) -> stages.
   // Every wave reads the tags and ids of the whole chunk (lane l holds pages
@@ -360,9 +410,24 @@ __global__ __launch_bounds__(DecodeCfg<PAIR>::NT, PAIR && D == 128 ? 4 : 2) void
   uint64_t m3w[PW], m8w[PW];
   int n3 = 0, n8 = 0;
   int tg_w[PW];
+  int n_list = 0;
+  bool up_w[PW];  // the list's entry is above the one before it
+  if constexpr (SPARSE) {
+    const int64_t l0 = ((int64_t)r * H + h) * a.n_sel;
+    int before[PW];
+#pragma unroll
+    for (int k = 0; k < PW; ++k) {
+      const int i = p0 + min(lane + 64 * k, n_pr - 1);
+      pg_lp[k] = a.sel[l0 + i];
+      before[k] = i > 0 ? a.sel[l0 + i - 1] : -1;
+    }
+    n_list = a.sel_count[(int64_t)r * H + h];
+#pragma unroll
+    for (int k = 0; k < PW; ++k) up_w[k] = pg_lp[k] > before[k];
+  }
 #pragma unroll
   for (int k = 0; k < PW; ++k) {  // all loads in flight together (clamped to the chunk)
-    const int64_t pi = (int64_t)r * mp + p0 + min(lane + 64 * k, n_pr - 1);
+    const int64_t pi = (int64_t)r * mp + (SPARSE ? min(max(pg_lp[k], 0), mp - 1) : p0 + min(lane + 64 * k, n_pr - 1));
     tg_w[k] = a.tags[pi];
     pg_id[k] = a.bt[pi];
   }
@@ -378,10 +443,51 @@ __global__ __launch_bounds__(DecodeCfg<PAIR>::NT, PAIR && D == 128 ? 4 : 2) void
     if (tid < G) part[G * D + G + tid] = 0.0f;  // empty partial: the merge writes zeros
     return;
   }
-  const int n_pg = min(p1, (S + PAGE - 1) / PAGE) - p0;  // pages of the chunk before the end
+  if (SPARSE && (n_list < 0 || n_list > a.n_sel)) {  // no list: zero outputs
+    if (chunk == 0 && tid == 0) atomicOr(&P.ctrl[CTRL_ERR], (int)MKV_DEVERR_RANGE);
+    n_list = 0;
+  }
+  // pages of the chunk before the end (a page list: its entries)
+  const int n_pg = min(p1, SPARSE ? n_list : (S + PAGE - 1) / PAGE) - p0;
   if (n_pg <= 0) {
     if (tid < G) part[G * D + G + tid] = 0.0f;  // slot past the request's end
     return;
+  }
+  if constexpr (ROPE) {
+    // cosine and sine per frequency, in the last wave's ring slot: its first copy is issued
+    // behind the barrier that follows the query build
+    double2* s_turn = reinterpret_cast<double2*>(ring + (NW - 1) * SLOTS * STAGE);
+    static_assert(NW - 1 >= 4 && D / 2 * (int)sizeof(double2) <= SLOTS * STAGE, "the table fits a slot not yet in use");
+    if (tid < a.rope.rot / 2) {
+      int at = turn_pos[0];
+#pragma unroll
+      for (int i = 1; i < ROPE_MAX_AXES; ++i) at = turn_axis == i ? turn_pos[i] : at;
+      double c, s;
+      rope_cos_sin((double)(a.pos ? at : s_in) * turn_f, a.rope.scale, c, s);
+      s_turn[tid] = make_double2(c, s);
+    }
+    __syncthreads();
+    // (the other half of each pair is loaded here: the first load has brought its line)
+#pragma unroll
+    for (int ps = 0; ps < 2; ++ps) {
+      const int hd = head_of_col<G6>(wid + NW * ps);
+      if (hd < 0 || hd >= G) continue;  // wave-uniform
+      const uint16_t* qh = a.q + ((int64_t)r * Hq + h * G + hd) * D;
+#pragma unroll
+      for (int i = 0; i < QV; ++i) {
+        const int ch = QV * lane + i;
+        if (ch < a.rope.rot) {
+          int f, pc;
+          bool up;
+          rope_of_channel(a.rope, ch, f, pc, up);
+          const double x = (double)qx[ps][i], xp = (double)bf16_to_f32(qh[pc]);
+          const double2 cs = s_turn[f];
+          double y0, y1;
+          rope_rotate(up ? xp : x, up ? x : xp, cs.x, cs.y, y0, y1);
+          qx[ps][i] = bf16_to_f32((uint16_t)f64_to_bf16(up ? y1 : y0));
+        }
+      }
+    }
   }
   // ---- query operands, built while the page-table loads are in flight, in MFMA
   // lane order (ln = lane % 16 the score column, lg = lane / 16):
@@ -442,31 +548,63 @@ __global__ __launch_bounds__(DecodeCfg<PAIR>::NT, PAIR && D == 128 ? 4 : 2) void
       amax = fmaxf(amax, lane_xor<32>(amax, lane));
       int ex = 0;
       (void)frexpf(amax, &ex);  // amax in [2^(ex-1), 2^ex)
-      const float qsc = (ok && amax > 0.0f) ? ldexpf(1.0f, 7 - ex + 1) : 1.0f;
+      // (FINE: a scale below 2^126, whose inverse is no subnormal)
+      const float qsc = (ok && amax > 0.0f) ? (FINE ? ldexpf(1.0f, min(15 - ex, 126)) : ldexpf(1.0f, 7 - ex + 1)) : 1.0f;
       if (lane == 0) {
         s_qinv[n] = 1.0f / qsc;
         if (pair) s_qinv[n + 8] = 1.0f / qsc;
+      }
+      float psc = 1.0f;
+      if constexpr (FINE) {
+        float pmax = 0.0f;
+#pragma unroll
+        for (int i = 0; i < QV; ++i) pmax = fmaxf(pmax, fabsf(qx[ps][i]));
+        pmax = fmaxf(pmax, lane_xor<1>(pmax, lane));
+        pmax = fmaxf(pmax, lane_xor<2>(pmax, lane));
+        pmax = fmaxf(pmax, lane_xor<4>(pmax, lane));
+        pmax = fmaxf(pmax, lane_xor<8>(pmax, lane));
+        pmax = fmaxf(pmax, lane_xor<16>(pmax, lane));
+        pmax = fmaxf(pmax, lane_xor<32>(pmax, lane));
+        int px = 0;
+        (void)frexpf(pmax, &px);
+        psc = (ok && pmax > 0.0f) ? ldexpf(1.0f, min(15 - px, 126)) : 1.0f;
+        if (lane == 0) {
+          s_pinv[n] = 1.0f / psc;
+          if (pair) s_pinv[n + 8] = 1.0f / psc;
+        }
       }
       // the lane's QV channels are neighbours in both operands: one store each
       const int c = QV * lane, lgc = c / (D / 4), cc = c % (D / 4);
       typedef _Float16 hvec __attribute__((ext_vector_type(QV)));
       hvec vp;
 #pragma unroll
-      for (int i = 0; i < QV; ++i) vp[i] = (_Float16)(ok ? qx[ps][i] : 0.0f);
+      for (int i = 0; i < QV; ++i) vp[i] = (_Float16)(ok ? (FINE ? qx[ps][i] * psc : qx[ps][i]) : 0.0f);
       *reinterpret_cast<hvec*>(qp + ((cc / 8 * 64) + lgc * 16 + n) * 8 + c % 8) = vp;
       // rotated query times its scale as three E4M3 terms (exact residuals)
       float x[QV];
 #pragma unroll
       for (int i = 0; i < QV; ++i) x[i] = ok ? xr[i] * qscale * qsc : 0.0f;
-      uint8_t* q8 = qf8 + ((cc / 32 * 64) + lgc * 16 + n) * 32 + c % 32;
+      if constexpr (FINE) {
+        hvec hi, lo;
 #pragma unroll
-      for (int t = 0; t < QF8_TERMS; ++t) {
-        uint32_t w = f32_to_e4m3(x[0]) | f32_to_e4m3(x[1]) << 8;
-        if constexpr (QV == 4) w |= f32_to_e4m3(x[2]) << 16 | f32_to_e4m3(x[3]) << 24;
+        for (int i = 0; i < QV; ++i) {
+          hi[i] = (_Float16)x[i];
+          lo[i] = (_Float16)(x[i] - (float)hi[i]);
+        }
+        const int at = ((cc / 8 * 64) + lgc * 16 + n) * 8 + c % 8;
+        *reinterpret_cast<hvec*>(reinterpret_cast<_Float16*>(qrh) + at) = hi;
+        *reinterpret_cast<hvec*>(reinterpret_cast<_Float16*>(qrl) + at) = lo;
+      } else {
+        uint8_t* q8 = qf8 + ((cc / 32 * 64) + lgc * 16 + n) * 32 + c % 32;
 #pragma unroll
-        for (int i = 0; i < QV; ++i) x[i] -= e4m3_to_f32(w >> (8 * i) & 0xFFu);
-        if constexpr (QV == 4) *reinterpret_cast<uint32_t*>(q8 + t * NK8 * 64 * 32) = w;
-        else *reinterpret_cast<uint16_t*>(q8 + t * NK8 * 64 * 32) = (uint16_t)w;
+        for (int t = 0; t < QF8_TERMS; ++t) {
+          uint32_t w = f32_to_e4m3(x[0]) | f32_to_e4m3(x[1]) << 8;
+          if constexpr (QV == 4) w |= f32_to_e4m3(x[2]) << 16 | f32_to_e4m3(x[3]) << 24;
+#pragma unroll
+          for (int i = 0; i < QV; ++i) x[i] -= e4m3_to_f32(w >> (8 * i) & 0xFFu);
+          if constexpr (QV == 4) *reinterpret_cast<uint32_t*>(q8 + t * NK8 * 64 * 32) = w;
+          else *reinterpret_cast<uint16_t*>(q8 + t * NK8 * 64 * 32) = (uint16_t)w;
+        }
       }
     }
   }
@@ -486,15 +624,20 @@ __global__ __launch_bounds__(DecodeCfg<PAIR>::NT, PAIR && D == 128 ? 4 : 2) void
       tg = TAG_R;
       if (id < 0) id = 0;  // fresh: placeholder until the append wave has popped the id
     }
+    if (SPARSE && pi < n_pg && !(up_w[k] && pg_lp[k] < (S + PAGE - 1) / PAGE)) {
+      // not above the entry before it, or past the end: left out
+      if (wid == 0) atomicOr(&P.ctrl[CTRL_ERR], (int)MKV_DEVERR_RANGE);
+      tg = -2;
+    }
     bool is3 = tg == TAG_S, is8 = (tg == TAG_R || tg == TAG_A);
-    if (wid == 0 && pi < n_pg && !is3 && !is8) atomicOr(&P.ctrl[CTRL_ERR], (int)MKV_DEVERR_BAD_TAG);
+    if (wid == 0 && pi < n_pg && !is3 && !is8 && tg != -2) atomicOr(&P.ctrl[CTRL_ERR], (int)MKV_DEVERR_BAD_TAG);
     if ((is3 || is8) && (id < 0 || id >= (is3 ? P.n_tq3 : P.n_fp8))) {
       // out-of-range physical id: left out (no page can stand in where the pool has none).
       // The page of the new token among them: the append then fails, and with it the call
       if (wid == 0) atomicOr(&P.ctrl[CTRL_ERR], (int)MKV_DEVERR_RANGE);
       is3 = is8 = false;
     }
-    pg_lp[k] = p0 + pi;
+    if (!SPARSE) pg_lp[k] = p0 + pi;
     pg_id[k] = id;
     m3w[k] = __ballot(is3);
     m8w[k] = __ballot(is8);
@@ -710,7 +853,9 @@ __global__ __launch_bounds__(DecodeCfg<PAIR>::NT, PAIR && D == 128 ? 4 : 2) void
       T.layer = a.layer;
       T.li = 0;
       T.h = h;
-      small_task_load_x<D>(T, H, a.n_req, a.k_new, a.v_new, lane);
+      small_task_load_x<D>(T, (int64_t)H * D, (int64_t)H * D, a.n_req, a.k_new, a.v_new, lane);
+      if constexpr (ROPE)
+        if (!kv) small_task_rotate<D>(T, a.rope, a.pos, a.n_req, reinterpret_cast<uint16_t*>(own), lane);
       small_task_load_old<D>(T, P, id, lane);
       small_task_run<D>(T, P, id, reinterpret_cast<uint32_t*>(own), own + PAGE * D, lane);
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the token's codes and scale are stored
@@ -738,6 +883,7 @@ __global__ __launch_bounds__(DecodeCfg<PAIR>::NT, PAIR && D == 128 ? 4 : 2) void
 
   __syncthreads();  // query operands and the stage list visible to every wave
   const float qinv = s_qinv[ln];  // undoes the query-term scale of this lane's column
+  const float pinv = FINE ? s_pinv[ln % (FINE ? 16 : 1)] : 1.0f;
   if (APP && holds && wid >= NW - 2) {
     // an append wave with two slots copies its first stage before the task
     // (unless that stage is the appended page's), so the copy's latency
@@ -812,6 +958,32 @@ __global__ __launch_bounds__(DecodeCfg<PAIR>::NT, PAIR && D == 128 ? 4 : 2) void
     // 16x16x128 fp8 MFMA: the 3-bit codes become E4M3 codebook bytes (one
     // v_perm per 4 codes) and meet the query's E4M3 terms directly
     float4v sa = zero4, sb = zero4;
+    if constexpr (FINE) {
+      // on the f16 MFMA: codebook values by the same v_perm and a conversion, hi and lo
+      // products in sums of their own, two each
+      float4v pa[4], pb[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) pa[i] = pb[i] = zero4;
+      auto keys = [&](const uint32_t* k, int s) {
+        const uint32_t u = __builtin_amdgcn_perm(KLUT_HI, KLUT_LO, quad_sel<NDW>(k, 2 * s));
+        const uint32_t w = __builtin_amdgcn_perm(KLUT_HI, KLUT_LO, quad_sel<NDW>(k, 2 * s + 1));
+        return h8(cvt_lo(u), cvt_hi(u), cvt_lo(w), cvt_hi(w));
+      };
+#pragma unroll
+      for (int s = 0; s < NS; ++s) {
+        const half8 qh = qrh[s * 64 + qlane], ql = qrl[s * 64 + qlane];
+        const half8 ka = keys(kA, s);
+        pa[s & 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ka, qh, pa[s & 1], 0, 0, 0);
+        pa[2 + (s & 1)] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ka, ql, pa[2 + (s & 1)], 0, 0, 0);
+        if (pair) {
+          const half8 kb = keys(kB, s);
+          pb[s & 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kb, qh, pb[s & 1], 0, 0, 0);
+          pb[2 + (s & 1)] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kb, ql, pb[2 + (s & 1)], 0, 0, 0);
+        }
+      }
+      sa = (pa[0] + pa[1]) + (pa[2] + pa[3]);
+      if (pair) sb = (pb[0] + pb[1]) + (pb[2] + pb[3]);
+    } else {
 #pragma unroll
     for (int S = 0; S < NK8; ++S) {
       v8i Ka, Kb;
@@ -826,6 +998,7 @@ __global__ __launch_bounds__(DecodeCfg<PAIR>::NT, PAIR && D == 128 ? 4 : 2) void
         sa = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(Ka, qv, sa, 0, 0, 0, 0, 0, 0);
         if (pair) sb = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(Kb, qv, sb, 0, 0, 0, 0, 0, 0);
       }
+    }
     }
     float sc[4];
     {
@@ -842,7 +1015,7 @@ __global__ __launch_bounds__(DecodeCfg<PAIR>::NT, PAIR && D == 128 ? 4 : 2) void
       }
     }
     STAGE_PRIO(2);
-    softmax_step<D, NI>(st, sc, lg);
+    softmax_step<D, NI, FINE>(st, sc, lg);
     if constexpr (SCORE) record_mass(sc, col_b ? e.z : e.x);
     STAGE_PRIO(3);
     half8 pT, pTl;
@@ -851,6 +1024,34 @@ __global__ __launch_bounds__(DecodeCfg<PAIR>::NT, PAIR && D == 128 ? 4 : 2) void
     // subnormal is c * 2^-9; the converter's power-of-two scale 2^9 makes it
     // c); v = zero + scale * code is applied in fp32 to the MFMA output,
     // the zero term through the rows' weight sums PS (MFMAs against ones)
+    if constexpr (FINE) {
+      // the products with the weights' low parts apart: added to the high parts' sum inside
+      // the matrix unit they lose their last bits, always downwards, and zero + scale *
+      // code, two sums of one sign each that nearly cancel, would not forgive it
+      const float4v PS = __builtin_amdgcn_mfma_f32_16x16x32_f16(pT, ones8, zero4, 0, 0, 0) +
+                         __builtin_amdgcn_mfma_f32_16x16x32_f16(pTl, ones8, zero4, 0, 0, 0);
+      auto codes_of = [&](int m) {
+        const uint32_t ua = quad_sel<NDW>(vA, m), ub = quad_sel<NDW>(vB, m);
+        return h8(cvt_code<false>(ua), cvt_code<true>(ua), cvt_code<false>(ub), cvt_code<true>(ub));
+      };
+      auto pv2 = [&](int m, float4v& hi, float4v& lo) {
+        const half8 c = codes_of(m);
+        hi = __builtin_amdgcn_mfma_f32_16x16x32_f16(pT, c, zero4, 0, 0, 0);
+        lo = __builtin_amdgcn_mfma_f32_16x16x32_f16(pTl, c, zero4, 0, 0, 0);
+      };
+      float4v X, Xl;
+      pv2(0, X, Xl);
+#pragma unroll
+      for (int m = 0; m < CL; ++m) {
+        float4v Xn = X, Xln = Xl;
+        if (m + 1 < CL) pv2(m + 1, Xn, Xln);
+        const float sm = (float)sO[m >> 1][m & 1], zm = (float)zO[m >> 1][m & 1];
+#pragma unroll
+        for (int i = 0; i < NI; ++i) st.acc[m][i] += fmaf(sm, Xl[i], fmaf(sm, X[i], zm * PS[i]));
+        X = Xn;
+        Xl = Xln;
+      }
+    } else {
     const float4v PS = __builtin_amdgcn_mfma_f32_16x16x32_f16(
         pTl, ones8, __builtin_amdgcn_mfma_f32_16x16x32_f16(pT, ones8, zero4, 0, 0, 0), 0, 0, 0);
     auto pv = [&](int m) {
@@ -870,6 +1071,7 @@ __global__ __launch_bounds__(DecodeCfg<PAIR>::NT, PAIR && D == 128 ? 4 : 2) void
       for (int i = 0; i < NI; ++i)
         st.acc[m][i] = fmaf((float)zm, PS[i], fmaf((float)sm, X[i], st.acc[m][i]));
       X = Xn;
+    }
     }
     if (SLOTS == 1) {
       jc = jr;
@@ -909,15 +1111,21 @@ __global__ __launch_bounds__(DecodeCfg<PAIR>::NT, PAIR && D == 128 ? 4 : 2) void
     const float2 ksv = *reinterpret_cast<const float2*>(ra + R8);
     wait_lgkm0();  // the stage is in registers: refill its slot
     if (refill) issue(e2, slot);
-    float4v sa = zero4;
+    // (FINE: four sums instead of one: the matrix unit rounds every eight products to the sum)
+    constexpr int NSUM = FINE ? 4 : 1;
+    float4v part4[NSUM];
+#pragma unroll
+    for (int s = 0; s < NSUM; ++s) part4[s] = zero4;
 #pragma unroll
     for (int s = 0; s < NS; ++s)
-      sa = __builtin_amdgcn_mfma_f32_16x16x32_f16(
+      part4[s % NSUM] = __builtin_amdgcn_mfma_f32_16x16x32_f16(
           h8(cvt_lo(kA[2 * s]), cvt_hi(kA[2 * s]), cvt_lo(kA[2 * s + 1]), cvt_hi(kA[2 * s + 1])),
-          qpl[s * 64 + qlane], sa, 0, 0, 0);
+          qpl[s * 64 + qlane], part4[s % NSUM], 0, 0, 0);
+    float4v sa = part4[0];
+    if constexpr (FINE) sa = (sa + part4[1]) + (part4[2] + part4[3]);
     float sc[4];
     {
-      const float kk = ksv.x * smk;
+      const float kk = FINE ? ksv.x * smk * pinv : ksv.x * smk;
 #pragma unroll
       for (int i = 0; i < 4; ++i) sc[i] = fmaf(sa[i], kk, fp8_bias);
       if ((e.x + 1) * PAGE > S) {
@@ -928,7 +1136,7 @@ __global__ __launch_bounds__(DecodeCfg<PAIR>::NT, PAIR && D == 128 ? 4 : 2) void
       }
     }
     STAGE_PRIO(2);
-    softmax_step<D, NI>(st, sc, lg);
+    softmax_step<D, NI, FINE>(st, sc, lg);
     if constexpr (SCORE) record_mass(sc, col_b ? MASK_LP : e.x);
     STAGE_PRIO(3);
     half8 pT, pTl;
@@ -937,8 +1145,11 @@ __global__ __launch_bounds__(DecodeCfg<PAIR>::NT, PAIR && D == 128 ? 4 : 2) void
 #pragma unroll
     for (int m = 0; m < CL; ++m) {
       const half8 v = h8(cvt_lo(vA[m]), cvt_hi(vA[m]), z2, z2);
-      const float4v X = __builtin_amdgcn_mfma_f32_16x16x32_f16(
-          pTl, v, __builtin_amdgcn_mfma_f32_16x16x32_f16(pT, v, zero4, 0, 0, 0), 0, 0, 0);
+      const float4v X =
+          FINE ? __builtin_amdgcn_mfma_f32_16x16x32_f16(pT, v, zero4, 0, 0, 0) +
+                     __builtin_amdgcn_mfma_f32_16x16x32_f16(pTl, v, zero4, 0, 0, 0)
+               : __builtin_amdgcn_mfma_f32_16x16x32_f16(
+                     pTl, v, __builtin_amdgcn_mfma_f32_16x16x32_f16(pT, v, zero4, 0, 0, 0), 0, 0, 0);
 #pragma unroll
       for (int i = 0; i < NI; ++i) st.acc[m][i] = fmaf(ksv.y, X[i], st.acc[m][i]);
     }
@@ -1244,15 +1455,15 @@ static constexpr size_t lds_limit() {
   return 160 * 1024 - sizeof(int4) * MAX_CHUNK_PAGES - 2 * 16 * NW_MAX * sizeof(float) - 256;
 }
 
-template <bool APP, bool SCORE = false>
+template <bool APP, bool SCORE = false, bool ROPE = false, bool SPARSE = false>
 static const void* decode_instance(int d, bool pair, bool g6) {
   if (d == 256)
-    return g6 ? (const void*)decode_kernel<256, true, true, APP, SCORE>
-                : pair ? (const void*)decode_kernel<256, true, false, APP, SCORE>
-                       : (const void*)decode_kernel<256, false, false, APP, SCORE>;
-  return g6 ? (const void*)decode_kernel<128, true, true, APP, SCORE>
-              : pair ? (const void*)decode_kernel<128, true, false, APP, SCORE>
-                     : (const void*)decode_kernel<128, false, false, APP, SCORE>;
+    return g6 ? (const void*)decode_kernel<256, true, true, APP, SCORE, ROPE, SPARSE>
+                : pair ? (const void*)decode_kernel<256, true, false, APP, SCORE, ROPE, SPARSE>
+                       : (const void*)decode_kernel<256, false, false, APP, SCORE, ROPE, SPARSE>;
+  return g6 ? (const void*)decode_kernel<128, true, true, APP, SCORE, ROPE, SPARSE>
+              : pair ? (const void*)decode_kernel<128, true, false, APP, SCORE, ROPE, SPARSE>
+                     : (const void*)decode_kernel<128, false, false, APP, SCORE, ROPE, SPARSE>;
 }
 
 hipError_t launch_decode(const PoolView& P, int layer, int n_req, const uint16_t* q,
@@ -1260,11 +1471,14 @@ hipError_t launch_decode(const PoolView& P, int layer, int n_req, const uint16_t
                          const int32_t* seq_lens, float* out, float* lse, void* ws,
                          hipStream_t s, hipEvent_t* ev, const uint16_t* k_new,
                          const uint16_t* v_new, int32_t* bt_w, uint8_t* tags_w,
-                         float2* page_mass) {
+                         float2* page_mass, const RopeView* rope, const int32_t* pos, const int32_t* sel,
+                         const int32_t* sel_count, int n_sel) {
   const bool app = k_new != nullptr;
   const bool score = page_mass != nullptr;
-  if (app && score) return hipErrorInvalidValue;
-  const DecodeShape sh = decode_shape(n_req, max_pages, P.n_kv_heads, P.recent, P.group, P.d);
+  const bool turn = rope != nullptr, sparse = sel != nullptr;
+  if ((app && score) || (turn && !app) || (sparse && (app || score))) return hipErrorInvalidValue;
+  const DecodeShape sh = sparse ? decode_shape(n_req, n_sel, P.n_kv_heads, 0, P.group, P.d)
+                                : decode_shape(n_req, max_pages, P.n_kv_heads, P.recent, P.group, P.d);
   DecodeArgs a;
   a.P = P;
   a.layer = layer;
@@ -1285,19 +1499,26 @@ hipError_t launch_decode(const PoolView& P, int layer, int n_req, const uint16_t
   a.bt_w = bt_w;
   a.tags_w = tags_w;
   a.page_mass = page_mass;
+  a.rope = turn ? *rope : RopeView{};
+  a.pos = pos;
+  a.sel = sel;
+  a.sel_count = sel_count;
+  a.n_sel = n_sel;
   a.app_rec = app ? reinterpret_cast<int32_t*>(reinterpret_cast<uint8_t*>(ws) +
                                               decode_part_bytes((int64_t)n_req * P.n_kv_heads * sh.max_chunks, P.group, P.d))
                   : nullptr;
-  // dynamic LDS: three query operands, then the page ring (reused by the wave merge)
+  // dynamic LDS: the query operands, then the page ring (reused by the wave merge)
   const bool pair = P.group <= 8;
   const int nw = pair ? DecodeCfg<true>::NW : DecodeCfg<false>::NW;
   const int slots = pair ? DecodeCfg<true>::SLOTS : DecodeCfg<false>::SLOTS;
-  const size_t qop_b = (size_t)QF8_TERMS * (P.d / 128) * 64 * 32 + (size_t)(P.d / 32) * 64 * 16;
+  const size_t qop_b = (size_t)query_bytes(turn || sparse, P.d);
   const size_t ring_b = (size_t)nw * slots * 2 * tq3_region_bytes(P.d);
   const size_t lds = qop_b + ring_b;  // the epilogue reuses each wave's ring slot
   if (lds > lds_limit()) return hipErrorInvalidValue;
   const bool g6 = pair && P.group <= 6;
-  const void* kern = app     ? decode_instance<true>(P.d, pair, g6)
+  const void* kern = sparse  ? decode_instance<false, false, false, true>(P.d, pair, g6)
+                     : turn  ? decode_instance<true, false, true>(P.d, pair, g6)
+                     : app   ? decode_instance<true>(P.d, pair, g6)
                      : score ? decode_instance<false, true>(P.d, pair, g6)
                              : decode_instance<false>(P.d, pair, g6);
   // the dynamic-LDS limit is raised once per kernel instance and device
@@ -1305,7 +1526,7 @@ hipError_t launch_decode(const PoolView& P, int layer, int n_req, const uint16_t
   int dev = 0;
   hipError_t e = hipGetDevice(&dev);
   if (e != hipSuccess) return e;
-  const uint32_t bit = 1u << ((app ? 6 : score ? 12 : 0) + (P.d == 256 ? 3 : 0) + (g6 ? 2 : pair ? 1 : 0));
+  const uint32_t bit = 1u << ((sparse ? 24 : turn ? 18 : app ? 6 : score ? 12 : 0) + (P.d == 256 ? 3 : 0) + (g6 ? 2 : pair ? 1 : 0));
   if (dev < 0 || dev >= 64 || !(attr_done[dev].load() & bit)) {
     e = hipFuncSetAttribute(kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds_limit());
     if (e != hipSuccess) return e;

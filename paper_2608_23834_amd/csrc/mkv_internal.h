@@ -6,6 +6,12 @@
 #include <stdint.h>
 
 #include "mkv_device.h"
+#include "mkv_rope.h"
+
+struct kv_rope {
+  int head_dim;
+  mkv::RopeView view;
+};
 
 struct mkv_pool {
   int n_layers, n_q_heads, n_kv_heads, d, group, n_fp8, n_tq3, recent;
@@ -72,6 +78,10 @@ inline PoolView view_of(const mkv_pool* p) {
 hipError_t launch_append(const PoolView& P, int layer, int n_req, int32_t* bt, uint8_t* tags,
                          int max_pages, const int32_t* seq_before, const int32_t* cu_new,
                          int n_new_total, const uint16_t* k, const uint16_t* v, hipStream_t s);
+hipError_t launch_append_rope(const PoolView& P, const RopeView& R, int layer, int n_req, int32_t* bt,
+                              uint8_t* tags, int max_pages, const int32_t* sb, const int32_t* cu,
+                              int n_new_total, const int32_t* pos, const uint16_t* k, int64_t kts,
+                              const uint16_t* v, int64_t vts, hipStream_t s);
 hipError_t launch_migrate(const PoolView& P, int n_req, int32_t* bt, uint8_t* tags, int max_pages,
                           const uint8_t* anchor, const int32_t* seq_lens, hipStream_t s);
 hipError_t launch_promote(const PoolView& P, int n_req, int32_t* bt, uint8_t* tags, int max_pages,
@@ -105,11 +115,26 @@ hipError_t launch_decode(const PoolView& P, int layer, int n_req, const uint16_t
                          const int32_t* seq_lens, float* out, float* lse, void* ws,
                          hipStream_t s, hipEvent_t* ev, const uint16_t* k_new = nullptr,
                          const uint16_t* v_new = nullptr, int32_t* bt_w = nullptr,
-                         uint8_t* tags_w = nullptr, float2* page_mass = nullptr);
+                         uint8_t* tags_w = nullptr, float2* page_mass = nullptr,
+                         const RopeView* rope = nullptr, const int32_t* pos = nullptr,
+                         const int32_t* sel = nullptr, const int32_t* sel_count = nullptr, int n_sel = 0);
 hipError_t launch_score_collect(int n_req, int n_q_heads, int max_pages, const int32_t* seq_lens,
                                 const float* lse, const float2* page_mass,
                                 const uint8_t* head_mask, float beta, float* a_io, float* r_out,
                                 float* qn_out, hipStream_t s);
+
+// mkv_rope.hip
+hipError_t launch_rope_apply(const RopeView& R, int d, int n_tokens, int n_heads, const uint16_t* x, int64_t xs,
+                             const int32_t* pos, uint16_t* out, int64_t os, hipStream_t s);
+
+// mkv_sparse.hip
+hipError_t launch_page_bounds(const PoolView& P, int layer, int n_req, const int32_t* bt, const uint8_t* tags,
+                              int max_pages, const int32_t* from, const int32_t* seq, uint8_t* codes, float* scales,
+                              hipStream_t s);
+size_t select_ws_bytes(int n_req, int max_pages, int H);
+hipError_t launch_select(const PoolView& P, int layer, int n_req, const uint16_t* q, const int32_t* seq,
+                         int max_pages, const uint8_t* codes, const float* scales, int n_select, int n_first,
+                         int n_last, int32_t* sel, int32_t* counts, void* ws, hipStream_t s);
 
 // mkv_control.hip (dense bf16 control, measurement only)
 size_t control_bf16_ws_bytes(int n_req, int max_pages, int n_kv_heads, int group, int d);

@@ -210,7 +210,7 @@ __device__ __forceinline__ uint32_t pack_e4m3(float a, float b, float c, float d
 
 // Quantize one tensor (K or V) of one page-head with one wave.  Slots [0, t0)
 // already hold codes with the page's scale; the new bf16 values are rows
-// row0 + t (t in [t0, t1)) of src, [row][H][D].  The scale only grows: when the
+// row0 + t (t in [t0, t1)) of the head, tstride apart from src on.  The scale only grows: when the
 // new amax exceeds 448 * s_old the old codes are re-rounded to the new scale.
 // Lane l holds channels 4 (l % (D/4)) .. + 3 of NT consecutive tokens, so it has
 // every byte of its K dwords (one token, four channels) and of its V dwords (one
@@ -221,11 +221,10 @@ __device__ __forceinline__ uint32_t pack_e4m3(float a, float b, float c, float d
 // byte by byte the launch took 367 us, now 160 us (5.0 TB/s).
 template <int D, bool kv>
 __device__ __forceinline__ void quant_task(uint8_t* reg, float* sc, const uint16_t* src, int64_t row0,
-                                           int t0, int t1, int H, int h, int lane) {
+                                           int t0, int t1, int64_t tstride, int lane) {
   constexpr int CL = D / 16, D4 = D / 4, NT = PAGE * D4 / 64, NG = NT / 4;
   const int cg = lane % D4, tb = (lane / D4) * NT;  // channel group, first token
-  const uint16_t* srow = src + (row0 * H + h) * D + 4 * cg;  // token t at srow[t * H * D]
-  const int64_t tstride = (int64_t)H * D;
+  const uint16_t* srow = src + row0 * tstride + 4 * cg;  // token t at srow[t * tstride]
   uint32_t* rw = reinterpret_cast<uint32_t*>(reg + (kv ? PAGE * D : 0));
   // K: dword of token t at t D4 + cg; V: the dwords of token group g at
   // ((r 4 + g) CL + m), r = 4 cg / CL, m = 4 cg % CL .. + 3
@@ -361,13 +360,13 @@ __device__ __forceinline__ void run_quant_task(const PoolView& P, int64_t task, 
   const int t0 = max(0, s0 - p * PAGE), t1 = min(PAGE, s0 + n - p * PAGE);
   const int64_t ph = ((int64_t)layer * P.n_fp8 + id) * H + h;
   const int64_t row0 = (int64_t)cu[r] + p * PAGE - s0;  // input row of slot t is row0 + t
-  const uint16_t* src = (kv ? v : k) + (int64_t)li * n_new_total * H * D;
+  const uint16_t* src = (kv ? v : k) + ((int64_t)li * n_new_total * H + h) * D;
   uint8_t* reg = P.fp8 + ph * fp8_region_bytes(D);
   float* sc = P.fp8_scales + ph * 2;
   if (kv)
-    quant_task<D, true>(reg, sc, src, row0, t0, t1, H, h, lane);
+    quant_task<D, true>(reg, sc, src, row0, t0, t1, (int64_t)H * D, lane);
   else
-    quant_task<D, false>(reg, sc, src, row0, t0, t1, H, h, lane);
+    quant_task<D, false>(reg, sc, src, row0, t0, t1, (int64_t)H * D, lane);
 }
 
 // Quantize every listed page-head of every requested layer (grid-stride over
@@ -382,6 +381,172 @@ __global__ __launch_bounds__(256) void append_quant_kernel(PoolView P, int layer
   const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   for (int64_t t = (int64_t)blockIdx.x * 4 + wid; t < n_tasks; t += (int64_t)gridDim.x * 4)
     run_quant_task<D>(P, t, layer_sel, n_lcall, sb, cu, n_new_total, k, v, P.list, lane);
+}
+
+// Keys of one page-head rotated and quantized by one wave, as quant_task does the plain
+// ones.  D / 8 lanes share a token, each with the two groups of four channels a and b whose
+// pairs it can turn by itself: 4 j .. and rot / 2 + 4 j .. (halves), 8 j .. and 8 j + 4 ..
+// (neighbours), so cosines and sines are four 16-byte LDS reads a token ([t][i % 4][i / 4]:
+// the lanes of a read are neighbours) and the rows are loaded once, into registers.  VEC
+// needs rot / 2 in fours; otherwise (!VEC) a lane holds channels 8 j .. and loads the other
+// half of each pair again.
+template <int D, bool VEC>
+__device__ __forceinline__ void rope_quant_keys(uint8_t* reg, float* sc, const uint16_t* src, int64_t row0,
+                                                int t0, int t1, int64_t tstride, const RopeView& R,
+                                                const double2* tab, int lane) {
+  constexpr int LT = D / 8, TP = 64 / LT, NP = PAGE / TP, D4 = D / 4;
+  const int j = lane % LT, tl = lane / LT, m = R.rot / 2;
+  const bool turn = VEC ? j < m / 4 : 8 * j < R.rot;
+  int ca = 8 * j, cb = 8 * j + 4;
+  if (VEC && !R.interleaved) {
+    ca = turn ? 4 * j : R.rot + 8 * (j - m / 4);
+    cb = turn ? m + 4 * j : ca + 4;
+  }
+  const uint16_t* srow = src + row0 * tstride;
+  const float s_old = t0 > 0 ? sc[0] : 0.0f;
+  uint2 xa[NP], xb[NP];
+#pragma unroll
+  for (int i = 0; i < NP; ++i) {
+    const int t = TP * i + tl;
+    xa[i] = xb[i] = make_uint2(0u, 0u);
+    if (t >= t0 && t < t1) {
+      xa[i] = *reinterpret_cast<const uint2*>(srow + t * tstride + ca);
+      xb[i] = *reinterpret_cast<const uint2*>(srow + t * tstride + cb);
+    }
+  }
+  float amax = 0.0f;
+#pragma unroll
+  for (int i = 0; i < NP; ++i) {
+    const int t = TP * i + tl;
+    if (turn && t >= t0 && t < t1) {
+      uint32_t h[8] = {xa[i].x & 0xFFFFu, xa[i].x >> 16, xa[i].y & 0xFFFFu, xa[i].y >> 16,
+                       xb[i].x & 0xFFFFu, xb[i].x >> 16, xb[i].y & 0xFFFFu, xb[i].y >> 16};
+      if constexpr (VEC) {
+        const double2* tt = tab + t * m + j;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const double2 cs = tt[q * (m / 4)];
+          double y0, y1;
+          const double x0 = (double)bf16_to_f32((uint16_t)(R.interleaved ? h[2 * q] : h[q]));
+          const double x1 = (double)bf16_to_f32((uint16_t)(R.interleaved ? h[2 * q + 1] : h[q + 4]));
+          rope_rotate(x0, x1, cs.x, cs.y, y0, y1);
+          if (R.interleaved) {
+            h[2 * q] = f64_to_bf16(y0);
+            h[2 * q + 1] = f64_to_bf16(y1);
+          } else {
+            h[q] = f64_to_bf16(y0);
+            h[q + 4] = f64_to_bf16(y1);
+          }
+        }
+      } else {
+#pragma unroll
+        for (int b = 0; b < 8; ++b) {
+          const int c = 8 * j + b;
+          if (c < R.rot) {
+            int f, pc;
+            bool up;
+            rope_of_channel(R, c, f, pc, up);
+            const double2 cs = tab[t * m + f];
+            const double x = (double)bf16_to_f32((uint16_t)h[b]), xp = (double)bf16_to_f32(srow[t * tstride + pc]);
+            double y0, y1;
+            rope_rotate(up ? xp : x, up ? x : xp, cs.x, cs.y, y0, y1);
+            h[b] = f64_to_bf16(up ? y1 : y0);
+          }
+        }
+      }
+      xa[i] = make_uint2(h[0] | h[1] << 16, h[2] | h[3] << 16);
+      xb[i] = make_uint2(h[4] | h[5] << 16, h[6] | h[7] << 16);
+    }
+    amax = fmaxf(amax, fmaxf(fmaxf(fmaxf(fabsf(__uint_as_float(xa[i].x << 16)), fabsf(__uint_as_float(xa[i].x & 0xFFFF0000u))),
+                                   fmaxf(fabsf(__uint_as_float(xa[i].y << 16)), fabsf(__uint_as_float(xa[i].y & 0xFFFF0000u)))),
+                             fmaxf(fmaxf(fabsf(__uint_as_float(xb[i].x << 16)), fabsf(__uint_as_float(xb[i].x & 0xFFFF0000u))),
+                                   fmaxf(fabsf(__uint_as_float(xb[i].y << 16)), fabsf(__uint_as_float(xb[i].y & 0xFFFF0000u))))));
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor(amax, o, 64));
+  float s_new = s_old;
+  bool requant = false;
+  if (t0 == 0) {
+    s_new = amax / 448.0f;
+  } else if (!(amax <= 448.0f * s_old)) {
+    s_new = amax / 448.0f;
+    requant = true;
+  }
+  uint32_t* rw = reinterpret_cast<uint32_t*>(reg);
+  const bool fast = __builtin_amdgcn_readfirstlane(div_fast(s_new));
+  const float y = 1.0f / s_new;
+  auto code4 = [&](const uint2& x) {
+    const float f[4] = {__uint_as_float(x.x << 16), __uint_as_float(x.x & 0xFFFF0000u), __uint_as_float(x.y << 16),
+                        __uint_as_float(x.y & 0xFFFF0000u)};
+    if (fast)
+      return pack_e4m3(div_by(f[0], s_new, y), div_by(f[1], s_new, y), div_by(f[2], s_new, y), div_by(f[3], s_new, y));
+    if (!(s_new > 0.0f)) return 0u;
+    return f32_to_e4m3(f[0] / s_new) | f32_to_e4m3(f[1] / s_new) << 8 | f32_to_e4m3(f[2] / s_new) << 16 |
+           f32_to_e4m3(f[3] / s_new) << 24;
+  };
+#pragma unroll
+  for (int i = 0; i < NP; ++i) {
+    const int t = TP * i + tl;
+    uint32_t* da = rw + t * D4 + ca / 4;
+    uint32_t* db = rw + t * D4 + cb / 4;
+    if (t >= t0 && t < t1) {
+      *da = code4(xa[i]);
+      *db = code4(xb[i]);
+    } else if (t0 == 0) {
+      *da = *db = 0u;
+    } else if (requant && t < t0) {
+      auto again = [&](uint32_t w) {
+        uint32_t o = 0;
+#pragma unroll
+        for (int b = 0; b < 4; ++b) o |= f32_to_e4m3((e4m3_to_f32((w >> (8 * b)) & 0xFFu) * s_old) / s_new) << (8 * b);
+        return o;
+      };
+      *da = again(*da);
+      *db = again(*db);
+    }
+  }
+  if (lane == 0) sc[0] = s_new;
+}
+
+// append_quant_kernel with the keys rotated.  A workgroup takes a listed page and up to hb
+// of the call's (layer, head) pairs: the cosines and sines of the page's 16 tokens are
+// computed once into LDS, then each wave quantizes K and V of one pair after the other.
+template <int D, bool VEC>
+__global__ __launch_bounds__(256) void append_rope_quant_kernel(PoolView P, int layer_sel, int n_lcall, int hb,
+                                                                const int32_t* sb, const int32_t* cu,
+                                                                int n_new_total, const uint16_t* k,
+                                                                const uint16_t* v, int64_t kts, int64_t vts,
+                                                                RopeView R, const int32_t* pos) {
+  extern __shared__ __align__(16) double2 s_tab[];  // [16][rot / 2]
+  if (P.ctrl[CTRL_ABORT]) return;
+  const int H = P.n_kv_heads, LH = n_lcall * H, nb = (LH + hb - 1) / hb, m = R.rot / 2;
+  const int64_t n_units = (int64_t)P.ctrl[CTRL_NLIST] * nb;
+  const int tid = threadIdx.x, lane = tid & 63, wid = __builtin_amdgcn_readfirstlane(tid >> 6);
+  for (int64_t u = blockIdx.x; u < n_units; u += gridDim.x) {
+    const int e = (int)(u / nb), lh0 = (int)(u % nb) * hb, lh1 = min(lh0 + hb, LH);
+    const int r = P.list[4 * e], p = P.list[4 * e + 1], id = P.list[4 * e + 2];
+    const int s0 = sb[r], n = cu[r + 1] - cu[r];
+    const int t0 = max(0, s0 - p * PAGE), t1 = min(PAGE, s0 + n - p * PAGE);
+    const int64_t row0 = (int64_t)cu[r] + (int64_t)p * PAGE - s0;  // input row of slot t is row0 + t
+    __syncthreads();  // the last unit's table has been read
+    for (int it = t0 * m + tid; it < t1 * m; it += 256) {
+      const int t = it / m, i = it - t * m;
+      const RopeEntry en = R.tab[i];
+      double c, s;
+      rope_cos_sin(rope_pos(pos, n_new_total, row0 + t, en.axis, p * PAGE + t) * en.freq, R.scale, c, s);
+      s_tab[t * m + (VEC ? (i & 3) * (m / 4) + (i >> 2) : i)] = make_double2(c, s);
+    }
+    __syncthreads();
+    for (int lh = lh0 + wid; lh < lh1; lh += 4) {
+      const int li = lh / H, h = lh - li * H, layer = layer_sel < 0 ? li : layer_sel;
+      const int64_t ph = ((int64_t)layer * P.n_fp8 + id) * H + h;
+      uint8_t* reg = P.fp8 + ph * fp8_region_bytes(D);
+      float* sc = P.fp8_scales + ph * 2;
+      rope_quant_keys<D, VEC>(reg, sc, k + (int64_t)li * n_new_total * kts + (int64_t)h * D, row0, t0, t1, kts, R,
+                              s_tab, lane);
+      quant_task<D, true>(reg, sc, v + (int64_t)li * n_new_total * vts + (int64_t)h * D, row0, t0, t1, vts, lane);
+    }
+  }
 }
 
 // Small appends (decode steps: a few tokens per request): one wave per task
@@ -403,17 +568,21 @@ constexpr int STEP_APPEND_MAX_REQ = 256;
 constexpr int STEP_APPEND_MAX_WAVES = 4096;
 
 
-template <int D>
+// ROPE: the key tasks rotate their rows by the rows' positions before anything else reads
+// them (rows of k and v are kts and vts elements apart).
+template <int D, bool ROPE>
 __global__ __launch_bounds__(64) void append_step_kernel(PoolView P, int layer_sel, int n_lcall,
                                                          int n_req, int32_t* bt, uint8_t* tags,
                                                          int max_pages, const int32_t* sb,
                                                          const int32_t* cu, int n_new_total,
-                                                         const uint16_t* k, const uint16_t* v) {
+                                                         const uint16_t* k, const uint16_t* v, int64_t kts,
+                                                         int64_t vts, RopeView R, const int32_t* pos) {
   constexpr int RQ = STEP_APPEND_MAX_REQ / 64, EQ = STEP_APPEND_MAX_TOKENS / 64;
   __shared__ int s_base[STEP_APPEND_MAX_REQ + 1];  // first list entry of request r
   __shared__ int s_cu[STEP_APPEND_MAX_REQ], s_n[STEP_APPEND_MAX_REQ], s_s0[STEP_APPEND_MAX_REQ];
   __shared__ __align__(16) uint32_t s_img[PAGE * D / 4];
   __shared__ uint8_t s_lut[256];
+  __shared__ __align__(16) uint16_t s_rows[ROPE ? PAGE * D : 8];
   const int lane = threadIdx.x;
   const int H = P.n_kv_heads;
   // ---- round trip 1: rows, starts, free-list top
@@ -497,7 +666,9 @@ __global__ __launch_bounds__(64) void append_step_kernel(PoolView P, int layer_s
     T.t0 = max(0, s0 - T.p * PAGE);
     T.t1 = min(PAGE, s0 + n - T.p * PAGE);
     // a listed page belongs to a request whose rows passed the range checks
-    small_task_load_x<D>(T, H, n_new_total, k, v, lane);
+    small_task_load_x<D>(T, kts, vts, n_new_total, k, v, lane);
+    if constexpr (ROPE)
+      if (!T.kv) small_task_rotate<D>(T, R, pos, n_new_total, s_rows, lane);
   }
   // ---- validation and fresh-page ranks (identical in every wave)
   int fresh[EQ], rank[EQ], n_fresh = 0;
@@ -1865,12 +2036,13 @@ hipError_t launch_append(const PoolView& P, int layer, int n_req, int32_t* bt, u
   if (n_new_total <= STEP_APPEND_MAX_TOKENS && n_req <= STEP_APPEND_MAX_REQ &&
       step_waves <= STEP_APPEND_MAX_WAVES) {
     const int grid = step_waves < 1 ? 1 : (int)step_waves;
+    const int64_t ts = (int64_t)P.n_kv_heads * P.d;
     if (P.d == 256)
-      hipLaunchKernelGGL(append_step_kernel<256>, dim3(grid), dim3(64), 0, s, P, layer, n_lcall,
-                         n_req, bt, tags, max_pages, sb, cu, n_new_total, k, v);
+      hipLaunchKernelGGL((append_step_kernel<256, false>), dim3(grid), dim3(64), 0, s, P, layer, n_lcall,
+                         n_req, bt, tags, max_pages, sb, cu, n_new_total, k, v, ts, ts, RopeView{}, nullptr);
     else
-      hipLaunchKernelGGL(append_step_kernel<128>, dim3(grid), dim3(64), 0, s, P, layer, n_lcall,
-                         n_req, bt, tags, max_pages, sb, cu, n_new_total, k, v);
+      hipLaunchKernelGGL((append_step_kernel<128, false>), dim3(grid), dim3(64), 0, s, P, layer, n_lcall,
+                         n_req, bt, tags, max_pages, sb, cu, n_new_total, k, v, ts, ts, RopeView{}, nullptr);
     return hipGetLastError();
   }
   hipLaunchKernelGGL(append_plan_kernel, dim3(1), dim3(1024), 0, s, n_req, bt, tags, max_pages, sb,
@@ -1884,6 +2056,45 @@ hipError_t launch_append(const PoolView& P, int layer, int n_req, int32_t* bt, u
   else
     hipLaunchKernelGGL(append_quant_kernel<128>, dim3(grid), dim3(256), 0, s, P, layer, n_lcall, sb,
                        cu, n_new_total, k, v);
+  return hipGetLastError();
+}
+
+hipError_t launch_append_rope(const PoolView& P, const RopeView& R, int layer, int n_req, int32_t* bt,
+                              uint8_t* tags, int max_pages, const int32_t* sb, const int32_t* cu,
+                              int n_new_total, const int32_t* pos, const uint16_t* k, int64_t kts,
+                              const uint16_t* v, int64_t vts, hipStream_t s) {
+  const int n_lcall = layer < 0 ? P.n_layers : 1;
+  const int64_t step_waves = (int64_t)n_new_total * n_lcall * P.n_kv_heads * 2;
+  if (n_new_total <= STEP_APPEND_MAX_TOKENS && n_req <= STEP_APPEND_MAX_REQ &&
+      step_waves <= STEP_APPEND_MAX_WAVES) {
+    const int grid = step_waves < 1 ? 1 : (int)step_waves;
+    if (P.d == 256)
+      hipLaunchKernelGGL((append_step_kernel<256, true>), dim3(grid), dim3(64), 0, s, P, layer, n_lcall,
+                         n_req, bt, tags, max_pages, sb, cu, n_new_total, k, v, kts, vts, R, pos);
+    else
+      hipLaunchKernelGGL((append_step_kernel<128, true>), dim3(grid), dim3(64), 0, s, P, layer, n_lcall,
+                         n_req, bt, tags, max_pages, sb, cu, n_new_total, k, v, kts, vts, R, pos);
+    return hipGetLastError();
+  }
+  hipLaunchKernelGGL(append_plan_kernel, dim3(1), dim3(1024), 0, s, n_req, bt, tags, max_pages, sb,
+                     cu, P.ctrl, P.fp8_stack, P.list, P.n_fp8, n_new_total, P.rc8);
+  // (layer, head) pairs per workgroup: enough to spread the page's angles over, as long as
+  // that leaves about four workgroups per CU
+  const int64_t pages_bound = (int64_t)n_new_total / PAGE + n_req + 1, lh = (int64_t)n_lcall * P.n_kv_heads;
+  int64_t hb = pages_bound * lh / 1024 / 4 * 4;
+  hb = hb < 4 ? 4 : hb > 32 ? 32 : hb;
+  const int grid = grid_for(pages_bound * ((lh + hb - 1) / hb), 4096);
+  const size_t lds = (size_t)PAGE * (R.rot / 2) * sizeof(double2);
+  const int hbi = (int)hb;
+  auto go = [&](auto kern) {
+    hipLaunchKernelGGL(kern, dim3(grid), dim3(256), lds, s, P, layer, n_lcall, hbi, sb, cu, n_new_total, k, v, kts,
+                       vts, R, pos);
+  };
+  const bool vec = R.rot % 8 == 0;
+  if (P.d == 256)
+    vec ? go(append_rope_quant_kernel<256, true>) : go(append_rope_quant_kernel<256, false>);
+  else
+    vec ? go(append_rope_quant_kernel<128, true>) : go(append_rope_quant_kernel<128, false>);
   return hipGetLastError();
 }
 

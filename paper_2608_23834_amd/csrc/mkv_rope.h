@@ -1,0 +1,109 @@
+// Rotary positions: the angle of a (position, frequency), its cosine and sine, and the
+// rotation of channel pairs, shared by the query rotation, the appends that rotate their
+// keys and the decode step that rotates both.
+//
+// Pair i of a head turns by th = fl64(pos[axis_i] * f_i): (x0, x1) -> m (x0 cos th - x1
+// sin th, x1 cos th + x0 sin th).  Everything is fp64 and the result is rounded to bf16
+// once, so that the same inputs give the same bits in every kernel here and in any other
+// fp64 evaluation (an error of 2^-50 of a value crosses a bf16 rounding boundary once in
+// 2^41), and the FP8 pages of a rotated append equal those of a rotation followed by a
+// plain append.  In fp32 the angle of position 10^6 would be off by 2^-5.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace mkv {
+
+constexpr int ROPE_MAX_AXES = 4;
+
+// One entry per frequency: what a lane needs of it in one 16-byte load.
+struct RopeEntry {
+  double freq;
+  int32_t axis, pad;
+};
+struct RopeView {
+  const RopeEntry* tab;  // device [rot / 2]
+  double scale;          // m
+  int rot, n_axes, interleaved;
+};
+
+// cos and sin of th in (-2^34, 2^34), times m.  k = the nearest multiple of pi/2; th - k
+// P1 is exact (a multiple of 2^-52 below 1), k P2 corrects P1's rounding; then the Taylor
+// series of both on |r| <= pi/4 to below 2^-58.
+__device__ __forceinline__ void rope_cos_sin(double th, double m, double& c, double& s) {
+#pragma clang fp contract(off)
+  const double k = rint(th * 0x1.45f306dc9c883p-1);  // 2 / pi
+  double r = __builtin_fma(-k, 0x1.921fb54442d18p+0, th);  // pi / 2 in two parts
+  r = __builtin_fma(-k, 0x1.1a62633145c07p-54, r);
+  const double z = r * r;
+  double a = 1.0 / 355687428096000.0;  // 1 / 17!, 1 / 15!, ...
+  a = __builtin_fma(a, z, -1.0 / 1307674368000.0);
+  a = __builtin_fma(a, z, 1.0 / 6227020800.0);
+  a = __builtin_fma(a, z, -1.0 / 39916800.0);
+  a = __builtin_fma(a, z, 1.0 / 362880.0);
+  a = __builtin_fma(a, z, -1.0 / 5040.0);
+  a = __builtin_fma(a, z, 1.0 / 120.0);
+  a = __builtin_fma(a, z, -1.0 / 6.0);
+  const double sn = __builtin_fma(a * z, r, r);
+  double b = 1.0 / 20922789888000.0;  // 1 / 16!, 1 / 14!, ...
+  b = __builtin_fma(b, z, -1.0 / 87178291200.0);
+  b = __builtin_fma(b, z, 1.0 / 479001600.0);
+  b = __builtin_fma(b, z, -1.0 / 3628800.0);
+  b = __builtin_fma(b, z, 1.0 / 40320.0);
+  b = __builtin_fma(b, z, -1.0 / 720.0);
+  b = __builtin_fma(b, z, 1.0 / 24.0);
+  b = __builtin_fma(b, z, -0.5);
+  const double cn = __builtin_fma(b, z, 1.0);
+  // quadrant k mod 4 (|k| < 2^34): swap, then the signs
+  const int q = (int)(int64_t)k & 3;
+  const double cu = q & 1 ? sn : cn, su = q & 1 ? cn : sn;
+  c = ((q + 1) & 2 ? -cu : cu) * m;
+  s = (q & 2 ? -su : su) * m;
+}
+
+__device__ __forceinline__ void rope_rotate(double x0, double x1, double c, double s, double& y0, double& y1) {
+#pragma clang fp contract(off)
+  y0 = __builtin_fma(x0, c, -(x1 * s));
+  y1 = __builtin_fma(x1, c, x0 * s);
+}
+
+// fp64 -> fp32 rounded to odd: truncated, the last bit set when anything was cut off.
+// fp32 keeps 16 bits more than bf16, so rounding the result to bf16, nearest even, is
+// one rounding of x.  (NaN stays NaN: its payload's top bit is set.)
+__device__ __forceinline__ uint32_t f64_to_f32_odd(double x) {
+  const float f = (float)x;
+  const double d = (double)f;
+  uint32_t u = __float_as_uint(f);
+  u -= fabs(d) > fabs(x) ? 1u : 0u;
+  u |= d != x ? 1u : 0u;
+  return u;
+}
+__device__ __forceinline__ uint32_t f32_bits_to_bf16(uint32_t u) {
+  return (u & 0x7FFFFFFFu) > 0x7F800000u ? (u >> 16) | 0x40u : (u + 0x7FFFu + ((u >> 16) & 1u)) >> 16;
+}
+__device__ __forceinline__ uint32_t f64_to_bf16(double x) { return f32_bits_to_bf16(f64_to_f32_odd(x)); }
+
+// position of a token on an axis: entry `row` of [n_axes][n], or its place in the cache
+__device__ __forceinline__ double rope_pos(const int32_t* pos, int64_t n, int64_t row, int axis, int at) {
+  return (double)(pos ? pos[(int64_t)axis * n + row] : at);
+}
+
+// where the pair of frequency i sits, and the pair of channel c
+__device__ __forceinline__ int2 rope_pair(const RopeView& R, int i) {
+  return R.interleaved ? make_int2(2 * i, 2 * i + 1) : make_int2(i, i + R.rot / 2);
+}
+__device__ __forceinline__ void rope_of_channel(const RopeView& R, int c, int& freq, int& partner, bool& upper) {
+  const int m = R.rot / 2;
+  if (R.interleaved) {
+    freq = c >> 1;
+    partner = c ^ 1;
+    upper = c & 1;
+  } else {
+    upper = c >= m;
+    freq = upper ? c - m : c;
+    partner = upper ? c - m : c + m;
+  }
+}
+
+}  // namespace mkv
