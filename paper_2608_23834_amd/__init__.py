@@ -146,15 +146,24 @@ def _check(fn, code):
 
 
 def _ptr(t):
-    if t is None:
-        return None
-    return ctypes.c_void_p(t.data_ptr())
+    return None if t is None else t.data_ptr()
 
 
 def _stream(stream=None):
+    if stream is not None:
+        return stream.cuda_stream
     import torch
-    s = torch.cuda.current_stream() if stream is None else stream
-    return ctypes.c_void_p(s.cuda_stream)
+    # the current stream's handle without the Stream object around it: 0.2 us of a call, 3 with it
+    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+
+
+def _here(*tensors):
+    """Every tensor (None aside) lies on the current device, without gaps."""
+    import torch
+    dev = torch._C._cuda_getDevice()
+    for t in tensors:
+        if t is not None and (t.get_device() != dev or not t.is_contiguous()):
+            raise ValueError("tensors are contiguous and on the current device")
 
 
 def pool_bytes(n_layers, n_q_heads, n_kv_heads, head_dim, n_fp8_pages, n_tq3_pages, recent_tokens):
@@ -373,27 +382,31 @@ class Rope:
 
 def _rows(t):
     """Elements from one row [heads][d] of t to the next; the heads lie together."""
-    d = t.shape[-1]
-    if t.stride(-1) != 1 or (t.shape[-2] > 1 and t.stride(-2) != d):
-        raise ValueError("rows are [heads][head_dim] without gaps")
-    n = t.shape[-3]
-    stride = t.stride(-3) if n > 1 else max(t.shape[-2] * d, t.stride(-3))
-    if t.dim() == 4 and t.shape[0] > 1 and t.stride(0) != n * stride:
+    import torch
+    *_, n, heads, d = shape = t.shape
+    st = t.stride()
+    if st[-1] != 1 or (heads > 1 and st[-2] != d) or t.get_device() != torch._C._cuda_getDevice():
+        raise ValueError("rows are [heads][head_dim] without gaps, on the current device")
+    stride = st[-3] if n > 1 else max(heads * d, st[-3])
+    if len(shape) == 4 and shape[0] > 1 and st[0] != n * stride:
         raise ValueError("one layer's rows follow the other's")
     return stride
 
 
 def _positions(rope, positions, n):
-    if positions is not None and (tuple(positions.shape) != (rope.n_axes, n) or not positions.is_contiguous()):
-        raise ValueError(f"positions are contiguous int32 [{rope.n_axes}][{n}]")
-    return _ptr(positions)
+    if positions is None:
+        return None
+    if positions.shape != (rope.n_axes, n):
+        raise ValueError(f"positions are int32 [{rope.n_axes}][{n}]")
+    _here(positions)
+    return positions.data_ptr()
 
 
 def kv_rope_apply(rope: Rope, x, positions, out, stream=None):
     """Rotate bf16 rows x [n][heads][head_dim] (int16 bits, tokens may be strided) into out;
     positions: int32 [n_axes][n]."""
     n, heads, d = x.shape
-    if tuple(out.shape) != tuple(x.shape) or d != rope.head_dim:
+    if out.shape != x.shape or d != rope.head_dim:
         raise ValueError("x and out are [n][heads][head_dim]")
     _check("kv_rope_apply", lib().kv_rope_apply(
         rope.handle, n, heads, _ptr(x), _rows(x), _positions(rope, positions, n), _ptr(out), _rows(out),
@@ -405,7 +418,8 @@ def kv_append_fp8_rope(pool: Pool, rope: Rope, layer, block_table, tags, seq_len
     """kv_append_fp8 with the keys rotated on the way; k, v: [n][H][d] of one layer or
     [n_layers][n][H][d], tokens may be strided; positions: int32 [n_axes][n] or None."""
     n_req, max_pages = block_table.shape
-    n = int(k.shape[-3])
+    n = k.shape[-3]
+    _here(block_table, tags, seq_lens_before, cu_new_tokens)
     _check("kv_append_fp8_rope", lib().kv_append_fp8_rope(
         pool.handle, rope.handle, layer, n_req, _ptr(block_table), _ptr(tags), max_pages, _ptr(seq_lens_before),
         _ptr(cu_new_tokens), n, _positions(rope, positions, n), _ptr(k), _rows(k), _ptr(v), _rows(v),
@@ -417,6 +431,7 @@ def paged_attn_decode_append_rope(pool: Pool, rope: Rope, layer, q, k_new, v_new
     """paged_attn_decode_append with q and k_new rotated in the launch; positions: int32
     [n_axes][n_req] or None (the token's place in the cache)."""
     n_req, max_pages = block_table.shape
+    _here(q, k_new, v_new, block_table, tags, seq_lens_before, out, lse, ws)
     _check("paged_attn_decode_append_rope", lib().paged_attn_decode_append_rope(
         pool.handle, rope.handle, layer, n_req, _ptr(q), _ptr(k_new), _ptr(v_new),
         _positions(rope, positions, n_req), _ptr(block_table), _ptr(tags), max_pages, _ptr(seq_lens_before),
@@ -449,6 +464,7 @@ def kv_page_bounds_update(pool: Pool, layer, block_table, tags, seq_lens_from, s
     n_req, max_pages = block_table.shape
     if (n_req, max_pages) != (bounds.n_req, bounds.max_pages):
         raise ValueError("the bounds are those of another table shape")
+    _here(block_table, tags, seq_lens_from, seq_lens, bounds.codes)
     _check("kv_page_bounds_update", lib().kv_page_bounds_update(
         pool.handle, layer, n_req, _ptr(block_table), _ptr(tags), max_pages, _ptr(seq_lens_from), _ptr(seq_lens),
         *bounds._args(), _stream(stream)))
@@ -467,8 +483,9 @@ def paged_attn_select_pages(pool: Pool, layer, q, seq_lens, bounds: PageBounds, 
     """Per request and KV head the pages to attend to: pages int32 [n_req][H][n_select]
     (ascending, -1 behind), counts int32 [n_req][H]; q is the rotated query."""
     n_req, H, n_select = pages.shape
-    if n_req != bounds.n_req or H != pool.n_kv_heads or tuple(counts.shape) != (n_req, H):
+    if n_req != bounds.n_req or H != pool.n_kv_heads or counts.shape != (n_req, H):
         raise ValueError("pages are [n_req][H][n_select], counts [n_req][H]")
+    _here(q, seq_lens, bounds.codes, pages, counts, ws)
     _check("paged_attn_select_pages", lib().paged_attn_select_pages(
         pool.handle, layer, n_req, _ptr(q), _ptr(seq_lens), bounds.max_pages, *bounds._args(), n_select, n_first,
         n_last, _ptr(pages), _ptr(counts), _ptr(ws), ws.numel() * ws.element_size(), _stream(stream)))
@@ -478,8 +495,9 @@ def paged_attn_decode_sparse(pool: Pool, layer, q, block_table, tags, seq_lens, 
                              stream=None):
     """paged_attn_decode over the listed logical pages of each request and KV head."""
     n_req, max_pages = block_table.shape
-    if pages.dim() != 3 or tuple(pages.shape[:2]) != (n_req, pool.n_kv_heads) or tuple(counts.shape) != tuple(pages.shape[:2]):
+    if pages.dim() != 3 or counts.shape != (n_req, pool.n_kv_heads) or pages.shape[:2] != counts.shape:
         raise ValueError("pages are [n_req][H][n_select], counts [n_req][H]")
+    _here(q, block_table, tags, seq_lens, pages, counts, out, lse, ws)
     _check("paged_attn_decode_sparse", lib().paged_attn_decode_sparse(
         pool.handle, layer, n_req, _ptr(q), _ptr(block_table), _ptr(tags), max_pages, _ptr(seq_lens),
         int(pages.shape[2]), _ptr(pages), _ptr(counts), _ptr(out), _ptr(lse), _ptr(ws),

@@ -476,7 +476,7 @@ mkv_status kv_append_fp8_rope(mkv_pool* pool, const kv_rope* rope, int32_t layer
   if (n_new_total > 0) {
     if (!k || !v) return MKV_EINVAL;
     const int64_t width = (int64_t)pool->n_kv_heads * pool->d;
-    if (k_stride > ((int64_t)1 << 31) || v_stride > ((int64_t)1 << 31)) return MKV_ERANGE;
+    if (k_stride > ((int64_t)1 << 26) || v_stride > ((int64_t)1 << 26)) return MKV_ERANGE;  // a page's rows: 32-bit offsets
     if (!good_rows(k, k_stride, width) || !good_rows(v, v_stride, width)) return MKV_EINVAL;
   }
   if (layer != MKV_ALL_LAYERS && (layer < 0 || layer >= pool->n_layers)) return MKV_ERANGE;

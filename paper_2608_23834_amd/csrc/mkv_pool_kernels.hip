@@ -203,7 +203,8 @@ __device__ __forceinline__ float div_by(float x, float s, float y) {
 __device__ __forceinline__ bool div_fast(float s) { return s >= 0x1p-60f && s <= 0x1p60f; }
 // four fp32 values -> four E4M3 bytes, as f32_to_e4m3
 __device__ __forceinline__ uint32_t pack_e4m3(float a, float b, float c, float d) {
-  auto sat = [](float x) { return fminf(fmaxf(x, -448.0f), 448.0f); };
+  // (the median of a NaN is the smaller bound, as the clamp's result is)
+  auto sat = [](float x) { return __builtin_amdgcn_fmed3f(x, -448.0f, 448.0f); };
   const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(sat(a), sat(b), 0, false);
   return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(sat(c), sat(d), lo, true);
 }
@@ -224,7 +225,9 @@ __device__ __forceinline__ void quant_task(uint8_t* reg, float* sc, const uint16
                                            int t0, int t1, int64_t tstride, int lane) {
   constexpr int CL = D / 16, D4 = D / 4, NT = PAGE * D4 / 64, NG = NT / 4;
   const int cg = lane % D4, tb = (lane / D4) * NT;  // channel group, first token
-  const uint16_t* srow = src + row0 * tstride + 4 * cg;  // token t at srow[t * tstride]
+  // token tb + k of this lane's channels: a wave-uniform address and a 32-bit offset
+  const uint8_t* srow = reinterpret_cast<const uint8_t*>(src + row0 * tstride);
+  const uint32_t so = (uint32_t)tb * (uint32_t)(2 * tstride) + 8 * cg;
   uint32_t* rw = reinterpret_cast<uint32_t*>(reg + (kv ? PAGE * D : 0));
   // K: dword of token t at t D4 + cg; V: the dwords of token group g at
   // ((r 4 + g) CL + m), r = 4 cg / CL, m = 4 cg % CL .. + 3
@@ -235,7 +238,7 @@ __device__ __forceinline__ void quant_task(uint8_t* reg, float* sc, const uint16
   for (int k = 0; k < NT; ++k) {
     const int t = tb + k;
     x[k] = make_uint2(0u, 0u);
-    if (t >= t0 && t < t1) x[k] = *reinterpret_cast<const uint2*>(srow + t * tstride);
+    if (t >= t0 && t < t1) x[k] = *reinterpret_cast<const uint2*>(srow + k * (2 * tstride) + so);
   }
   float amax = 0.0f;
 #pragma unroll
@@ -255,6 +258,9 @@ __device__ __forceinline__ void quant_task(uint8_t* reg, float* sc, const uint16
     s_new = amax / 448.0f;
     requant = true;
   }
+  // (the rows stay packed: kept unpacked from here to the codes they would take twice the registers)
+#pragma unroll
+  for (int k = 0; k < NT; ++k) asm volatile("" : "+v"(x[k].x), "+v"(x[k].y));
   // four channels of token tb + k
   auto f4 = [&](int k, int b) {
     const uint32_t w = b < 2 ? x[k].x : x[k].y;
@@ -297,6 +303,7 @@ __device__ __forceinline__ void quant_task(uint8_t* reg, float* sc, const uint16
           if (nw || t0 == 0) rw[t * D4 + cg] = nw ? w[u] : 0u;
         }
       }
+      __builtin_amdgcn_sched_barrier(0);  // one group at a time: bounded register use
     }
   } else {
     // old codes to re-round, or a scale without a fast division: rare, so one
@@ -387,139 +394,217 @@ __global__ __launch_bounds__(256) void append_quant_kernel(PoolView P, int layer
 // ones.  D / 8 lanes share a token, each with the two groups of four channels a and b whose
 // pairs it can turn by itself: 4 j .. and rot / 2 + 4 j .. (halves), 8 j .. and 8 j + 4 ..
 // (neighbours), so cosines and sines are four 16-byte LDS reads a token ([t][i % 4][i / 4]:
-// the lanes of a read are neighbours) and the rows are loaded once, into registers.  VEC
-// needs rot / 2 in fours; otherwise (!VEC) a lane holds channels 8 j .. and loads the other
-// half of each pair again.
+// the lanes of a read are neighbours).  VEC needs rot / 2 in fours; otherwise (!VEC) a lane
+// holds channels 8 j .. and loads the other half of each pair again.
+// A whole page (VEC) has its rows loaded once, all in flight together, and kept as bf16 in
+// registers.  A partly filled one, which may hold old codes to re-round, goes token by token
+// twice, for the largest value and for the codes, and loads and turns its rows both times:
+// at most two pages of a request, in a function of its own and few registers.
+// 33 K tokens x 4 heads x 4 layers at d = 256 (0.8 GB, 158 us of a copy's bandwidth): the
+// call takes 206 us with 118 registers and four waves a SIMD, 249 with 233 and two (rows kept
+// unpacked, both kinds of page in one body); the plain append of them takes 172.
 template <int D, bool VEC>
-__device__ __forceinline__ void rope_quant_keys(uint8_t* reg, float* sc, const uint16_t* src, int64_t row0,
-                                                int t0, int t1, int64_t tstride, const RopeView& R,
-                                                const double2* tab, int lane) {
-  constexpr int LT = D / 8, TP = 64 / LT, NP = PAGE / TP, D4 = D / 4;
-  const int j = lane % LT, tl = lane / LT, m = R.rot / 2;
-  const bool turn = VEC ? j < m / 4 : 8 * j < R.rot;
-  int ca = 8 * j, cb = 8 * j + 4;
-  if (VEC && !R.interleaved) {
-    ca = turn ? 4 * j : R.rot + 8 * (j - m / 4);
-    cb = turn ? m + 4 * j : ca + 4;
+struct RopeLane {
+  static constexpr int LT = D / 8, TP = 64 / LT, NP = PAGE / TP;  // lanes a token, tokens a pass, passes
+  int j, tl, m, ca, cb;
+  bool turn, inter;
+  uint32_t to, oa, ob;  // byte offsets into the rows: token tl, and its two groups
+  __device__ RopeLane(const RopeView& R, int64_t tstride, int lane) {
+    j = lane % LT;
+    tl = lane / LT;
+    m = R.rot / 2;
+    inter = R.interleaved;
+    turn = VEC ? j < m / 4 : 8 * j < R.rot;
+    ca = 8 * j;
+    cb = 8 * j + 4;
+    if (VEC && !inter) {
+      ca = turn ? 4 * j : R.rot + 8 * (j - m / 4);
+      cb = turn ? m + 4 * j : ca + 4;
+    }
+    to = (uint32_t)tl * (uint32_t)(2 * tstride);
+    oa = to + 2 * ca;
+    ob = to + 2 * cb;
   }
-  const uint16_t* srow = src + row0 * tstride;
-  const float s_old = t0 > 0 ? sc[0] : 0.0f;
+};
+// the eight channels (a, b: as loaded) of token t turned, as fp32 values
+template <int D, bool VEC>
+__device__ __forceinline__ void rope_turn8(const RopeLane<D, VEC>& L, const RopeView& R, const double2* tab, int t,
+                                           const uint8_t* row, const uint2& a, const uint2& b, float* x) {
+  const uint32_t w[4] = {a.x, a.y, b.x, b.y};
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    x[2 * q] = __uint_as_float(w[q] << 16);
+    x[2 * q + 1] = __uint_as_float(w[q] & 0xFFFF0000u);
+  }
+  if (!L.turn) return;
+  if constexpr (VEC) {
+    const double2* tt = tab + t * L.m + L.j;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const double2 cs = tt[q * (L.m / 4)];
+      double y0, y1;
+      if (L.inter) {
+        rope_rotate((double)x[2 * q], (double)x[2 * q + 1], cs.x, cs.y, y0, y1);
+        x[2 * q] = f64_round_bf16(y0);
+        x[2 * q + 1] = f64_round_bf16(y1);
+      } else {
+        rope_rotate((double)x[q], (double)x[q + 4], cs.x, cs.y, y0, y1);
+        x[q] = f64_round_bf16(y0);
+        x[q + 4] = f64_round_bf16(y1);
+      }
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int c = 8 * L.j + i;
+      if (c < R.rot) {
+        int f, pc;
+        bool up;
+        rope_of_channel(R, c, f, pc, up);
+        const double2 cs = tab[t * L.m + f];
+        const double xo = (double)x[i];
+        const double xp = (double)bf16_to_f32(*reinterpret_cast<const uint16_t*>(row + (L.to + 2 * pc)));
+        double y0, y1;
+        rope_rotate(up ? xp : xo, up ? xo : xp, cs.x, cs.y, y0, y1);
+        x[i] = f64_round_bf16(up ? y1 : y0);
+      }
+    }
+  }
+}
+// four values over s -> four codes; fast: div_fast(s) and y = 1 / s
+__device__ __forceinline__ uint32_t codes_over(const float* f, float s, float y, bool fast) {
+  if (fast) return pack_e4m3(div_by(f[0], s, y), div_by(f[1], s, y), div_by(f[2], s, y), div_by(f[3], s, y));
+  if (!(s > 0.0f)) return 0u;
+  return f32_to_e4m3(f[0] / s) | f32_to_e4m3(f[1] / s) << 8 | f32_to_e4m3(f[2] / s) << 16 | f32_to_e4m3(f[3] / s) << 24;
+}
+__device__ __forceinline__ float wave_max(float x) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) x = fmaxf(x, __shfl_xor(x, o, 64));
+  return x;
+}
+
+template <int D>
+__device__ __forceinline__ void rope_quant_whole(uint8_t* reg, float* sc, const uint8_t* rows, int64_t tstride,
+                                                 const RopeView& R, const double2* tab, int lane) {
+  const RopeLane<D, true> L(R, tstride, lane);
+  constexpr int TP = L.TP, NP = L.NP;
   uint2 xa[NP], xb[NP];
 #pragma unroll
   for (int i = 0; i < NP; ++i) {
-    const int t = TP * i + tl;
-    xa[i] = xb[i] = make_uint2(0u, 0u);
-    if (t >= t0 && t < t1) {
-      xa[i] = *reinterpret_cast<const uint2*>(srow + t * tstride + ca);
-      xb[i] = *reinterpret_cast<const uint2*>(srow + t * tstride + cb);
-    }
+    xa[i] = *reinterpret_cast<const uint2*>(rows + TP * i * (2 * tstride) + L.oa);
+    xb[i] = *reinterpret_cast<const uint2*>(rows + TP * i * (2 * tstride) + L.ob);
   }
   float amax = 0.0f;
 #pragma unroll
   for (int i = 0; i < NP; ++i) {
-    const int t = TP * i + tl;
-    if (turn && t >= t0 && t < t1) {
-      uint32_t h[8] = {xa[i].x & 0xFFFFu, xa[i].x >> 16, xa[i].y & 0xFFFFu, xa[i].y >> 16,
-                       xb[i].x & 0xFFFFu, xb[i].x >> 16, xb[i].y & 0xFFFFu, xb[i].y >> 16};
-      if constexpr (VEC) {
-        const double2* tt = tab + t * m + j;
+    float x[8];
+    rope_turn8<D, true>(L, R, tab, TP * i + L.tl, rows, xa[i], xb[i], x);
+    xa[i] = make_uint2(bf16_pair(x[0], x[1]), bf16_pair(x[2], x[3]));
+    xb[i] = make_uint2(bf16_pair(x[4], x[5]), bf16_pair(x[6], x[7]));
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const double2 cs = tt[q * (m / 4)];
-          double y0, y1;
-          const double x0 = (double)bf16_to_f32((uint16_t)(R.interleaved ? h[2 * q] : h[q]));
-          const double x1 = (double)bf16_to_f32((uint16_t)(R.interleaved ? h[2 * q + 1] : h[q + 4]));
-          rope_rotate(x0, x1, cs.x, cs.y, y0, y1);
-          if (R.interleaved) {
-            h[2 * q] = f64_to_bf16(y0);
-            h[2 * q + 1] = f64_to_bf16(y1);
-          } else {
-            h[q] = f64_to_bf16(y0);
-            h[q + 4] = f64_to_bf16(y1);
-          }
-        }
-      } else {
-#pragma unroll
-        for (int b = 0; b < 8; ++b) {
-          const int c = 8 * j + b;
-          if (c < R.rot) {
-            int f, pc;
-            bool up;
-            rope_of_channel(R, c, f, pc, up);
-            const double2 cs = tab[t * m + f];
-            const double x = (double)bf16_to_f32((uint16_t)h[b]), xp = (double)bf16_to_f32(srow[t * tstride + pc]);
-            double y0, y1;
-            rope_rotate(up ? xp : x, up ? x : xp, cs.x, cs.y, y0, y1);
-            h[b] = f64_to_bf16(up ? y1 : y0);
-          }
-        }
-      }
-      xa[i] = make_uint2(h[0] | h[1] << 16, h[2] | h[3] << 16);
-      xb[i] = make_uint2(h[4] | h[5] << 16, h[6] | h[7] << 16);
-    }
-    amax = fmaxf(amax, fmaxf(fmaxf(fmaxf(fabsf(__uint_as_float(xa[i].x << 16)), fabsf(__uint_as_float(xa[i].x & 0xFFFF0000u))),
-                                   fmaxf(fabsf(__uint_as_float(xa[i].y << 16)), fabsf(__uint_as_float(xa[i].y & 0xFFFF0000u)))),
-                             fmaxf(fmaxf(fabsf(__uint_as_float(xb[i].x << 16)), fabsf(__uint_as_float(xb[i].x & 0xFFFF0000u))),
-                                   fmaxf(fabsf(__uint_as_float(xb[i].y << 16)), fabsf(__uint_as_float(xb[i].y & 0xFFFF0000u))))));
+    for (int b = 0; b < 8; ++b) amax = fmaxf(amax, fabsf(x[b]));
+    __builtin_amdgcn_sched_barrier(0);  // one token at a time: bounded register use
   }
+  amax = wave_max(amax);
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor(amax, o, 64));
-  float s_new = s_old;
-  bool requant = false;
-  if (t0 == 0) {
-    s_new = amax / 448.0f;
-  } else if (!(amax <= 448.0f * s_old)) {
-    s_new = amax / 448.0f;
-    requant = true;
-  }
-  uint32_t* rw = reinterpret_cast<uint32_t*>(reg);
-  const bool fast = __builtin_amdgcn_readfirstlane(div_fast(s_new));
-  const float y = 1.0f / s_new;
-  auto code4 = [&](const uint2& x) {
-    const float f[4] = {__uint_as_float(x.x << 16), __uint_as_float(x.x & 0xFFFF0000u), __uint_as_float(x.y << 16),
-                        __uint_as_float(x.y & 0xFFFF0000u)};
-    if (fast)
-      return pack_e4m3(div_by(f[0], s_new, y), div_by(f[1], s_new, y), div_by(f[2], s_new, y), div_by(f[3], s_new, y));
-    if (!(s_new > 0.0f)) return 0u;
-    return f32_to_e4m3(f[0] / s_new) | f32_to_e4m3(f[1] / s_new) << 8 | f32_to_e4m3(f[2] / s_new) << 16 |
-           f32_to_e4m3(f[3] / s_new) << 24;
-  };
+  for (int i = 0; i < NP; ++i) asm volatile("" : "+v"(xa[i].x), "+v"(xa[i].y), "+v"(xb[i].x), "+v"(xb[i].y));
+  const float s = amax / 448.0f, y = 1.0f / s;
+  const bool fast = __builtin_amdgcn_readfirstlane(div_fast(s));
+  const uint32_t da = (uint32_t)(L.tl * D + L.ca), db = (uint32_t)(L.tl * D + L.cb);
 #pragma unroll
   for (int i = 0; i < NP; ++i) {
-    const int t = TP * i + tl;
-    uint32_t* da = rw + t * D4 + ca / 4;
-    uint32_t* db = rw + t * D4 + cb / 4;
+    const uint32_t w[4] = {xa[i].x, xa[i].y, xb[i].x, xb[i].y};
+    float x[8];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      x[2 * q] = __uint_as_float(w[q] << 16);
+      x[2 * q + 1] = __uint_as_float(w[q] & 0xFFFF0000u);
+    }
+    *reinterpret_cast<uint32_t*>(reg + TP * D * i + da) = codes_over(x, s, y, fast);
+    *reinterpret_cast<uint32_t*>(reg + TP * D * i + db) = codes_over(x + 4, s, y, fast);
+  }
+  if (lane == 0) sc[0] = s;
+}
+
+template <int D, bool VEC>
+__device__ __attribute__((noinline)) void rope_quant_part(uint8_t* reg, float* sc, const uint8_t* rows, int64_t tstride,
+                                                const RopeView& R, const double2* tab, int t0, int t1, int lane) {
+  const RopeLane<D, VEC> L(R, tstride, lane);
+  constexpr int TP = L.TP, NP = L.NP;
+  auto turned = [&](int i, float* x) {
+    const uint8_t* row = rows + TP * i * (2 * tstride);
+    const uint2 a = *reinterpret_cast<const uint2*>(row + L.oa), b = *reinterpret_cast<const uint2*>(row + L.ob);
+    rope_turn8<D, VEC>(L, R, tab, TP * i + L.tl, row, a, b, x);
+  };
+  float amax = 0.0f;
+#pragma unroll 1
+  for (int i = 0; i < NP; ++i) {
+    const int t = TP * i + L.tl;
     if (t >= t0 && t < t1) {
-      *da = code4(xa[i]);
-      *db = code4(xb[i]);
+      float x[8];
+      turned(i, x);
+#pragma unroll
+      for (int b = 0; b < 8; ++b) amax = fmaxf(amax, fabsf(x[b]));
+    }
+  }
+  amax = wave_max(amax);
+  const float s_old = t0 > 0 ? sc[0] : 0.0f;
+  const bool grown = t0 == 0 || !(amax <= 448.0f * s_old);
+  const float s = grown ? amax / 448.0f : s_old, y = 1.0f / s;
+  const bool fast = __builtin_amdgcn_readfirstlane(div_fast(s));
+#pragma unroll 1
+  for (int i = 0; i < NP; ++i) {
+    const int t = TP * i + L.tl;
+    uint32_t* da = reinterpret_cast<uint32_t*>(reg + t * D + L.ca);
+    uint32_t* db = reinterpret_cast<uint32_t*>(reg + t * D + L.cb);
+    if (t >= t0 && t < t1) {
+      float x[8];
+      turned(i, x);
+      *da = codes_over(x, s, y, fast);
+      *db = codes_over(x + 4, s, y, fast);
     } else if (t0 == 0) {
       *da = *db = 0u;
-    } else if (requant && t < t0) {
+    } else if (grown && t < t0) {  // old codes, re-rounded to the new scale
       auto again = [&](uint32_t w) {
         uint32_t o = 0;
 #pragma unroll
-        for (int b = 0; b < 4; ++b) o |= f32_to_e4m3((e4m3_to_f32((w >> (8 * b)) & 0xFFu) * s_old) / s_new) << (8 * b);
+        for (int b = 0; b < 4; ++b) o |= f32_to_e4m3((e4m3_to_f32((w >> (8 * b)) & 0xFFu) * s_old) / s) << (8 * b);
         return o;
       };
       *da = again(*da);
       *db = again(*db);
     }
   }
-  if (lane == 0) sc[0] = s_new;
+  if (lane == 0) sc[0] = s;
+}
+
+// Cosines and sines of slots [t0, t1) of a page, by the whole workgroup; a function of its own:
+// inlined, the series' constants stay in registers over the rest of the kernel.
+template <bool VEC>
+__device__ __attribute__((noinline)) void rope_fill_table(RopeView R, const int32_t* pos, int n_new_total, int64_t row0,
+                                                          int at0, int t0, int t1, double2* tab) {
+  const int m = R.rot / 2;
+  for (int it = t0 * m + threadIdx.x; it < t1 * m; it += 256) {
+    const int t = it / m, i = it - t * m;
+    const RopeEntry en = R.tab[i];
+    double c, s;
+    rope_cos_sin(rope_pos(pos, n_new_total, row0 + t, en.axis, at0 + t) * en.freq, R.scale, c, s);
+    tab[t * m + (VEC ? (i & 3) * (m / 4) + (i >> 2) : i)] = make_double2(c, s);
+  }
 }
 
 // append_quant_kernel with the keys rotated.  A workgroup takes a listed page and up to hb
 // of the call's (layer, head) pairs: the cosines and sines of the page's 16 tokens are
 // computed once into LDS, then each wave quantizes K and V of one pair after the other.
 template <int D, bool VEC>
-__global__ __launch_bounds__(256) void append_rope_quant_kernel(PoolView P, int layer_sel, int n_lcall, int hb,
+__global__ __launch_bounds__(256, VEC ? 4 : 3) void append_rope_quant_kernel(PoolView P, int layer_sel, int n_lcall, int hb,
                                                                 const int32_t* sb, const int32_t* cu,
                                                                 int n_new_total, const uint16_t* k,
                                                                 const uint16_t* v, int64_t kts, int64_t vts,
                                                                 RopeView R, const int32_t* pos) {
   extern __shared__ __align__(16) double2 s_tab[];  // [16][rot / 2]
   if (P.ctrl[CTRL_ABORT]) return;
-  const int H = P.n_kv_heads, LH = n_lcall * H, nb = (LH + hb - 1) / hb, m = R.rot / 2;
+  const int H = P.n_kv_heads, LH = n_lcall * H, nb = (LH + hb - 1) / hb;
   const int64_t n_units = (int64_t)P.ctrl[CTRL_NLIST] * nb;
   const int tid = threadIdx.x, lane = tid & 63, wid = __builtin_amdgcn_readfirstlane(tid >> 6);
   for (int64_t u = blockIdx.x; u < n_units; u += gridDim.x) {
@@ -529,21 +614,18 @@ __global__ __launch_bounds__(256) void append_rope_quant_kernel(PoolView P, int 
     const int t0 = max(0, s0 - p * PAGE), t1 = min(PAGE, s0 + n - p * PAGE);
     const int64_t row0 = (int64_t)cu[r] + (int64_t)p * PAGE - s0;  // input row of slot t is row0 + t
     __syncthreads();  // the last unit's table has been read
-    for (int it = t0 * m + tid; it < t1 * m; it += 256) {
-      const int t = it / m, i = it - t * m;
-      const RopeEntry en = R.tab[i];
-      double c, s;
-      rope_cos_sin(rope_pos(pos, n_new_total, row0 + t, en.axis, p * PAGE + t) * en.freq, R.scale, c, s);
-      s_tab[t * m + (VEC ? (i & 3) * (m / 4) + (i >> 2) : i)] = make_double2(c, s);
-    }
+    rope_fill_table<VEC>(R, pos, n_new_total, row0, p * PAGE, t0, t1, s_tab);
     __syncthreads();
     for (int lh = lh0 + wid; lh < lh1; lh += 4) {
       const int li = lh / H, h = lh - li * H, layer = layer_sel < 0 ? li : layer_sel;
       const int64_t ph = ((int64_t)layer * P.n_fp8 + id) * H + h;
       uint8_t* reg = P.fp8 + ph * fp8_region_bytes(D);
       float* sc = P.fp8_scales + ph * 2;
-      rope_quant_keys<D, VEC>(reg, sc, k + (int64_t)li * n_new_total * kts + (int64_t)h * D, row0, t0, t1, kts, R,
-                              s_tab, lane);
+      const uint8_t* rows = reinterpret_cast<const uint8_t*>(k + ((int64_t)li * n_new_total + row0) * kts + (int64_t)h * D);
+      if (VEC && t0 == 0 && t1 == PAGE)
+        rope_quant_whole<D>(reg, sc, rows, kts, R, s_tab, lane);
+      else
+        rope_quant_part<D, VEC>(reg, sc, rows, kts, R, s_tab, t0, t1, lane);
       quant_task<D, true>(reg, sc, v + (int64_t)li * n_new_total * vts + (int64_t)h * D, row0, t0, t1, vts, lane);
     }
   }

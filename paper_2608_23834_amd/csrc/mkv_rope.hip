@@ -46,44 +46,65 @@ __global__ __launch_bounds__(256) void rope_apply_kernel(RopeView R, int n_token
       rope_cos_sin((double)pos[(int64_t)e.axis * n_tokens + t] * e.freq, R.scale, c[i], s[i]);
     }
   }
+  // the rows of HU heads are in flight together
+  constexpr int HU = 4;
   const uint16_t* xr = x + t * xs;
   uint16_t* orow = out + t * os;
-  for (int h = h0; h < h1; ++h) {
-    const uint16_t* xh = xr + (int64_t)h * D;
-    const uint2 a = *reinterpret_cast<const uint2*>(xh + ca), b = *reinterpret_cast<const uint2*>(xh + cb);
-    uint32_t w[8] = {a.x & 0xFFFFu, a.x >> 16, a.y & 0xFFFFu, a.y >> 16, b.x & 0xFFFFu, b.x >> 16, b.y & 0xFFFFu, b.y >> 16};
-    if (turn) {
-      if constexpr (VEC) {
+  for (int hu = h0; hu < h1; hu += HU) {
+    uint2 a[HU], b[HU];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          double y0, y1;
-          if (R.interleaved) {
-            rope_rotate((double)bf16_to_f32((uint16_t)w[2 * i]), (double)bf16_to_f32((uint16_t)w[2 * i + 1]), c[i], s[i], y0, y1);
-            w[2 * i] = f64_to_bf16(y0);
-            w[2 * i + 1] = f64_to_bf16(y1);
-          } else {
-            rope_rotate((double)bf16_to_f32((uint16_t)w[i]), (double)bf16_to_f32((uint16_t)w[i + 4]), c[i], s[i], y0, y1);
-            w[i] = f64_to_bf16(y0);
-            w[i + 4] = f64_to_bf16(y1);
+    for (int k = 0; k < HU; ++k) {
+      const uint16_t* xh = xr + (int64_t)min(hu + k, h1 - 1) * D;
+      a[k] = *reinterpret_cast<const uint2*>(xh + ca);
+      b[k] = *reinterpret_cast<const uint2*>(xh + cb);
+    }
+#pragma unroll
+    for (int k = 0; k < HU; ++k) {
+      if (hu + k >= h1) break;
+      const uint32_t w[4] = {a[k].x, a[k].y, b[k].x, b[k].y};
+      uint32_t o[8];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        o[2 * i] = w[i] << 16;
+        o[2 * i + 1] = w[i] & 0xFFFF0000u;
+      }
+      if (turn) {
+        auto val = [&](int i) { return (double)__uint_as_float(o[i]); };
+        auto put = [&](int i, double y) { o[i] = __float_as_uint(f64_round_bf16(y)); };
+        if constexpr (VEC) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int u = 2 * i, v = 2 * i + 1;
+            double y0, y1;
+            if (R.interleaved) {
+              rope_rotate(val(u), val(v), c[i], s[i], y0, y1);
+              put(u, y0);
+              put(v, y1);
+            } else {
+              rope_rotate(val(i), val(i + 4), c[i], s[i], y0, y1);
+              put(i, y0);
+              put(i + 4, y1);
+            }
+          }
+        } else {
+          const uint16_t* xh = xr + (int64_t)(hu + k) * D;
+          uint16_t other[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) other[i] = xh[pc[i]];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            if (8 * j + i >= R.rot) continue;
+            const double xo = val(i), xp = (double)bf16_to_f32(other[i]);
+            double y0, y1;
+            rope_rotate(up[i] ? xp : xo, up[i] ? xo : xp, c[i], s[i], y0, y1);
+            put(i, up[i] ? y1 : y0);
           }
         }
-      } else {
-        uint16_t other[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) other[i] = xh[pc[i]];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          if (8 * j + i >= R.rot) continue;
-          const double xo = (double)bf16_to_f32((uint16_t)w[i]), xp = (double)bf16_to_f32(other[i]);
-          double y0, y1;
-          rope_rotate(up[i] ? xp : xo, up[i] ? xo : xp, c[i], s[i], y0, y1);
-          w[i] = f64_to_bf16(up[i] ? y1 : y0);
-        }
       }
+      uint16_t* oh = orow + (int64_t)(hu + k) * D;
+      *reinterpret_cast<uint2*>(oh + ca) = make_uint2(o[0] >> 16 | o[1], o[2] >> 16 | o[3]);
+      *reinterpret_cast<uint2*>(oh + cb) = make_uint2(o[4] >> 16 | o[5], o[6] >> 16 | o[7]);
     }
-    uint16_t* oh = orow + (int64_t)h * D;
-    *reinterpret_cast<uint2*>(oh + ca) = make_uint2(w[0] | w[1] << 16, w[2] | w[3] << 16);
-    *reinterpret_cast<uint2*>(oh + cb) = make_uint2(w[4] | w[5] << 16, w[6] | w[7] << 16);
   }
 }
 

@@ -194,6 +194,41 @@ def test_append_single_layers():
             _append(t, (rope, freq, axis, False), counts, rng, layer=layer, positions=layer != 0, pad=layer)
 
 
+@pytest.mark.parametrize("turned", [False, True])
+def test_append_special_values(turned):
+    """NaN, infinities, zeros and the smallest and largest values: one large call and calls of single
+    pages leave the same pages (different kernels)."""
+    import paper_2608_23834_amd as mk
+    torch = _torch()
+    rng = np.random.default_rng(21)
+    vals = np.array([0x0000, 0x8000, 0x0001, 0x8001, 0x0080, 0x7F7F, 0xFF7F, 0x7F80, 0xFF80, 0x7FC0, 0x3F80, 0xBF81], np.uint16)
+    n, w = 640, _w(256, 8, 2, 1)
+    K, V = _bits(rng, n, 2, 256), _bits(rng, n, 2, 256)
+    for x in (K, V):  # page by page: a few special values, whole rows of them, tiny scales
+        for p in range(0, 20):
+            sel = rng.random((16, 2, 256)) < (0.001, 0.02, 1.0)[p % 3]
+            x[16 * p: 16 * p + 16] = np.where(sel, rng.choice(vals[: 7 + p % 6], (16, 2, 256)), x[16 * p: 16 * p + 16])
+        x[16 * 20: 16 * 21] = rng.choice(np.array([0x0001, 0x8001, 0x0003, 0], np.uint16), (16, 2, 256))
+        x[16 * 21: 16 * 22] = 0
+    rope, _, _ = _rope(256, 64, 1)
+    pos = _gpu(np.arange(n, dtype=np.int32)[None])
+
+    def put(t, a, b):
+        sb, cu = _gpu(np.array([a], np.int32)), _gpu(np.array([0, b - a], np.int32))
+        if turned:
+            mk.kv_append_fp8_rope(t.gpu, rope, 0, t.bt, t.tags, sb, cu, pos[:, a:b].contiguous(), _i16(K[a:b]), _i16(V[a:b]))
+        else:
+            mk.kv_append_fp8(t.gpu, 0, t.bt, t.tags, sb, cu, _i16(K[a:b]), _i16(V[a:b]))
+    ta, tb = _twin(w, [n], 1), _twin(w, [n], 1)
+    put(ta, 0, n)
+    for a in range(0, n, 16):
+        put(tb, a, a + 16)
+    torch.cuda.synchronize()
+    assert torch.equal(ta.bt, tb.bt)
+    assert torch.equal(ta.gpu.fp8, tb.gpu.fp8)
+    assert np.array_equal(ta.gpu.fp8_scales.cpu().numpy().view(np.uint32), tb.gpu.fp8_scales.cpu().numpy().view(np.uint32))
+
+
 def test_append_nothing_and_refusals():
     import paper_2608_23834_amd as mk
     torch = _torch()
