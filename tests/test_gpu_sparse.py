@@ -71,6 +71,22 @@ def test_bounds_match(d, hq, hkv):
     assert mk.kv_pool_check_errors(t.gpu) == 0
 
 
+def test_bounds_of_many_requests():
+    """More requests than one launch takes, most of them a page or none."""
+    import paper_2608_23834_amd as mk
+    rng = np.random.default_rng(3)
+    lens = [int(x) for x in rng.integers(0, 40, 2100)]
+    lens[1023], lens[1024], lens[2099] = 300, 0, 129
+    t = _twin(_w(128, 8, 1, len(lens)), lens)
+    t.fill()
+    b = mk.PageBounds(t.gpu, t.n_req, t.max_pages)
+    mk.kv_page_bounds_update(t.gpu, 0, t.bt, t.tags, _gpu(np.zeros(t.n_req, np.int32)), _gpu(np.array(t.cur, np.int32)), b)
+    want, sc = ref.bounds(t.orc.fp8, t.orc.fp8_scale, t.obt, t.cur, 128)
+    got, gs = _values(b)
+    assert np.array_equal(got, want) and np.array_equal(gs, sc)
+    assert mk.kv_pool_check_errors(t.gpu) == 0
+
+
 def test_bounds_of_wrong_pages():
     import paper_2608_23834_amd as mk
     t = _twin(_w(128, 8, 2, 4), [400, 400, 400, 400], recent=64)
