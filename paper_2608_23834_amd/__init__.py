@@ -149,18 +149,25 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
+def _current():
+    """(current device, its current stream's handle): without the Stream object around it 0.2 us
+    of a call instead of 3."""
+    global _current
+    import torch
+    device, raw = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
+
+    def _current():
+        d = device()
+        return d, raw(d)
+    return _current()
+
+
 def _stream(stream=None):
-    if stream is not None:
-        return stream.cuda_stream
-    import torch
-    # the current stream's handle without the Stream object around it: 0.2 us of a call, 3 with it
-    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+    return _current()[1] if stream is None else stream.cuda_stream
 
 
-def _here(*tensors):
-    """Every tensor (None aside) lies on the current device, without gaps."""
-    import torch
-    dev = torch._C._cuda_getDevice()
+def _here(dev, *tensors):
+    """Every tensor (None aside) lies on device dev, without gaps."""
     for t in tensors:
         if t is not None and (t.get_device() != dev or not t.is_contiguous()):
             raise ValueError("tensors are contiguous and on the current device")
@@ -380,62 +387,69 @@ class Rope:
             pass
 
 
-def _rows(t):
+def _rows(dev, t):
     """Elements from one row [heads][d] of t to the next; the heads lie together."""
-    import torch
-    *_, n, heads, d = shape = t.shape
+    shape = t.shape
+    if t.get_device() != dev:
+        raise ValueError("tensors are on the current device")
+    if t.is_contiguous():
+        return shape[-2] * shape[-1]
+    n, heads, d = shape[-3:]
     st = t.stride()
-    if st[-1] != 1 or (heads > 1 and st[-2] != d) or t.get_device() != torch._C._cuda_getDevice():
-        raise ValueError("rows are [heads][head_dim] without gaps, on the current device")
-    stride = st[-3] if n > 1 else max(heads * d, st[-3])
+    if st[-1] != 1 or (heads > 1 and st[-2] != d):
+        raise ValueError("rows are [heads][head_dim] without gaps")
+    stride = st[-3] if n > 1 else heads * d
     if len(shape) == 4 and shape[0] > 1 and st[0] != n * stride:
         raise ValueError("one layer's rows follow the other's")
     return stride
 
 
-def _positions(rope, positions, n):
+def _positions(dev, rope, positions, n):
     if positions is None:
         return None
-    if positions.shape != (rope.n_axes, n):
-        raise ValueError(f"positions are int32 [{rope.n_axes}][{n}]")
-    _here(positions)
+    if positions.shape != (rope.n_axes, n) or positions.get_device() != dev or not positions.is_contiguous():
+        raise ValueError(f"positions are contiguous int32 [{rope.n_axes}][{n}] on the current device")
     return positions.data_ptr()
 
 
 def kv_rope_apply(rope: Rope, x, positions, out, stream=None):
     """Rotate bf16 rows x [n][heads][head_dim] (int16 bits, tokens may be strided) into out;
     positions: int32 [n_axes][n]."""
+    dev, cur = _current()
     n, heads, d = x.shape
     if out.shape != x.shape or d != rope.head_dim:
         raise ValueError("x and out are [n][heads][head_dim]")
     _check("kv_rope_apply", lib().kv_rope_apply(
-        rope.handle, n, heads, _ptr(x), _rows(x), _positions(rope, positions, n), _ptr(out), _rows(out),
-        _stream(stream)))
+        rope.handle, n, heads, x.data_ptr(), _rows(dev, x), _positions(dev, rope, positions, n), out.data_ptr(),
+        _rows(dev, out), cur if stream is None else stream.cuda_stream))
 
 
 def kv_append_fp8_rope(pool: Pool, rope: Rope, layer, block_table, tags, seq_lens_before, cu_new_tokens,
                        positions, k, v, stream=None):
     """kv_append_fp8 with the keys rotated on the way; k, v: [n][H][d] of one layer or
     [n_layers][n][H][d], tokens may be strided; positions: int32 [n_axes][n] or None."""
+    dev, cur = _current()
     n_req, max_pages = block_table.shape
     n = k.shape[-3]
-    _here(block_table, tags, seq_lens_before, cu_new_tokens)
+    _here(dev, block_table, tags, seq_lens_before, cu_new_tokens)
     _check("kv_append_fp8_rope", lib().kv_append_fp8_rope(
-        pool.handle, rope.handle, layer, n_req, _ptr(block_table), _ptr(tags), max_pages, _ptr(seq_lens_before),
-        _ptr(cu_new_tokens), n, _positions(rope, positions, n), _ptr(k), _rows(k), _ptr(v), _rows(v),
-        _stream(stream)))
+        pool.handle, rope.handle, layer, n_req, block_table.data_ptr(), tags.data_ptr(), max_pages,
+        seq_lens_before.data_ptr(), cu_new_tokens.data_ptr(), n, _positions(dev, rope, positions, n), k.data_ptr(),
+        _rows(dev, k), v.data_ptr(), _rows(dev, v), cur if stream is None else stream.cuda_stream))
 
 
 def paged_attn_decode_append_rope(pool: Pool, rope: Rope, layer, q, k_new, v_new, positions, block_table, tags,
                                   seq_lens_before, out, lse, ws, stream=None):
     """paged_attn_decode_append with q and k_new rotated in the launch; positions: int32
     [n_axes][n_req] or None (the token's place in the cache)."""
+    dev, cur = _current()
     n_req, max_pages = block_table.shape
-    _here(q, k_new, v_new, block_table, tags, seq_lens_before, out, lse, ws)
+    _here(dev, q, k_new, v_new, block_table, tags, seq_lens_before, out, lse, ws)
     _check("paged_attn_decode_append_rope", lib().paged_attn_decode_append_rope(
-        pool.handle, rope.handle, layer, n_req, _ptr(q), _ptr(k_new), _ptr(v_new),
-        _positions(rope, positions, n_req), _ptr(block_table), _ptr(tags), max_pages, _ptr(seq_lens_before),
-        _ptr(out), _ptr(lse), _ptr(ws), ws.numel() * ws.element_size(), _stream(stream)))
+        pool.handle, rope.handle, layer, n_req, q.data_ptr(), k_new.data_ptr(), v_new.data_ptr(),
+        _positions(dev, rope, positions, n_req), block_table.data_ptr(), tags.data_ptr(), max_pages,
+        seq_lens_before.data_ptr(), out.data_ptr(), _ptr(lse), ws.data_ptr(), ws.nbytes,
+        cur if stream is None else stream.cuda_stream))
 
 
 class PageBounds:
@@ -454,20 +468,20 @@ class PageBounds:
         self.scales = torch.zeros(shape, dtype=torch.float32, device=device)
         assert self.codes.numel() == c.value and self.scales.numel() * 4 == s.value
 
-    def _args(self):
-        return _ptr(self.codes), self.codes.numel(), _ptr(self.scales), 4 * self.scales.numel()
+        self._args = (self.codes.data_ptr(), c.value, self.scales.data_ptr(), s.value)
 
 
 def kv_page_bounds_update(pool: Pool, layer, block_table, tags, seq_lens_from, seq_lens, bounds: PageBounds,
                           stream=None):
     """Recompute the bounds of the pages that hold tokens [seq_lens_from, seq_lens)."""
+    dev, cur = _current()
     n_req, max_pages = block_table.shape
-    if (n_req, max_pages) != (bounds.n_req, bounds.max_pages):
+    if n_req != bounds.n_req or max_pages != bounds.max_pages:
         raise ValueError("the bounds are those of another table shape")
-    _here(block_table, tags, seq_lens_from, seq_lens, bounds.codes)
+    _here(dev, block_table, tags, seq_lens_from, seq_lens, bounds.codes)
     _check("kv_page_bounds_update", lib().kv_page_bounds_update(
-        pool.handle, layer, n_req, _ptr(block_table), _ptr(tags), max_pages, _ptr(seq_lens_from), _ptr(seq_lens),
-        *bounds._args(), _stream(stream)))
+        pool.handle, layer, n_req, block_table.data_ptr(), tags.data_ptr(), max_pages, seq_lens_from.data_ptr(),
+        seq_lens.data_ptr(), *bounds._args, cur if stream is None else stream.cuda_stream))
 
 
 def select_workspace(pool: Pool, n_req, max_pages, device="cuda"):
@@ -482,26 +496,29 @@ def paged_attn_select_pages(pool: Pool, layer, q, seq_lens, bounds: PageBounds, 
                             stream=None):
     """Per request and KV head the pages to attend to: pages int32 [n_req][H][n_select]
     (ascending, -1 behind), counts int32 [n_req][H]; q is the rotated query."""
+    dev, cur = _current()
     n_req, H, n_select = pages.shape
     if n_req != bounds.n_req or H != pool.n_kv_heads or counts.shape != (n_req, H):
         raise ValueError("pages are [n_req][H][n_select], counts [n_req][H]")
-    _here(q, seq_lens, bounds.codes, pages, counts, ws)
+    _here(dev, q, seq_lens, bounds.codes, pages, counts, ws)
     _check("paged_attn_select_pages", lib().paged_attn_select_pages(
-        pool.handle, layer, n_req, _ptr(q), _ptr(seq_lens), bounds.max_pages, *bounds._args(), n_select, n_first,
-        n_last, _ptr(pages), _ptr(counts), _ptr(ws), ws.numel() * ws.element_size(), _stream(stream)))
+        pool.handle, layer, n_req, q.data_ptr(), seq_lens.data_ptr(), bounds.max_pages, *bounds._args, n_select,
+        n_first, n_last, pages.data_ptr(), counts.data_ptr(), ws.data_ptr(), ws.nbytes,
+        cur if stream is None else stream.cuda_stream))
 
 
 def paged_attn_decode_sparse(pool: Pool, layer, q, block_table, tags, seq_lens, pages, counts, out, lse, ws,
                              stream=None):
     """paged_attn_decode over the listed logical pages of each request and KV head."""
+    dev, cur = _current()
     n_req, max_pages = block_table.shape
     if pages.dim() != 3 or counts.shape != (n_req, pool.n_kv_heads) or pages.shape[:2] != counts.shape:
         raise ValueError("pages are [n_req][H][n_select], counts [n_req][H]")
-    _here(q, block_table, tags, seq_lens, pages, counts, out, lse, ws)
+    _here(dev, q, block_table, tags, seq_lens, pages, counts, out, lse, ws)
     _check("paged_attn_decode_sparse", lib().paged_attn_decode_sparse(
-        pool.handle, layer, n_req, _ptr(q), _ptr(block_table), _ptr(tags), max_pages, _ptr(seq_lens),
-        int(pages.shape[2]), _ptr(pages), _ptr(counts), _ptr(out), _ptr(lse), _ptr(ws),
-        ws.numel() * ws.element_size(), _stream(stream)))
+        pool.handle, layer, n_req, q.data_ptr(), block_table.data_ptr(), tags.data_ptr(), max_pages,
+        seq_lens.data_ptr(), pages.shape[2], pages.data_ptr(), counts.data_ptr(), out.data_ptr(), _ptr(lse),
+        ws.data_ptr(), ws.nbytes, cur if stream is None else stream.cuda_stream))
 
 
 def paged_attn_chunk(pool: Pool, layer, q, cu_q, block_table, tags, seq_lens, out, ws,

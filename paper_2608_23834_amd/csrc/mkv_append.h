@@ -55,12 +55,11 @@ __device__ __forceinline__ void small_task_load_x(SmallTask<D>& T, int64_t kts, 
   (void)lane;
 }
 
-// Rotate a key task's rows (x as loaded) by their positions, through an LDS block of the
-// rows [token][channel] (xs, at least (t1 - t0) D bf16): one lane per (token, pair), so an
-// angle is evaluated once and any pairing is the same code.
-template <int D>
-__device__ __forceinline__ void small_task_rotate(SmallTask<D>& T, const RopeView& R, const int32_t* pos,
-                                                  int n_pos, uint16_t* xs, int lane) {
+// Rotate a key task's rows (x as loaded), through an LDS block of them [token][channel]
+// (xs, at least (t1 - t0) D bf16): one lane per (token, pair), so an angle is evaluated once
+// and any pairing is the same code.  cos_sin(t, i, c, s): those of token t0 + t, pair i.
+template <int D, class F>
+__device__ __forceinline__ void small_task_rotate(SmallTask<D>& T, const RopeView& R, uint16_t* xs, int lane, F cos_sin) {
   constexpr int D4 = SmallTask<D>::D4;
   const int nt = T.t1 - T.t0, n4 = nt * D4, m = R.rot / 2;
 #pragma unroll
@@ -69,17 +68,24 @@ __device__ __forceinline__ void small_task_rotate(SmallTask<D>& T, const RopeVie
     if (idx < n4) reinterpret_cast<uint2*>(xs)[idx] = T.x[j];
   }
   __builtin_amdgcn_wave_barrier();
-  for (int it = lane; it < nt * m; it += 64) {
-    const int t = it / m, i = it - t * m;
-    const RopeEntry e = R.tab[i];
-    const double th = rope_pos(pos, n_pos, (int64_t)T.row0 + T.t0 + t, e.axis, T.p * PAGE + T.t0 + t) * e.freq;
+  int t = 0, i = lane;  // pair lane, lane + 64, .. of the run of tokens
+  while (i >= m) {
+    i -= m;
+    ++t;
+  }
+  while (t < nt) {
     double c, s, y0, y1;
-    rope_cos_sin(th, R.scale, c, s);
+    cos_sin(t, i, c, s);
     const int2 pr = rope_pair(R, i);
     uint16_t* x = xs + t * D;
     rope_rotate((double)bf16_to_f32(x[pr.x]), (double)bf16_to_f32(x[pr.y]), c, s, y0, y1);
     x[pr.x] = (uint16_t)f64_to_bf16(y0);
     x[pr.y] = (uint16_t)f64_to_bf16(y1);
+    i += 64;
+    while (i >= m) {
+      i -= m;
+      ++t;
+    }
   }
   __builtin_amdgcn_wave_barrier();
 #pragma unroll

@@ -372,9 +372,23 @@ __global__ __launch_bounds__(DecodeCfg<PAIR>::NT, PAIR && D == 128 ? 4 : 2) void
 #pragma unroll
   for (int i = 0; i < QV; ++i) sg[i] = P.sigma[QV * lane + i];
   // ROPE: the angles of the request's token, one lane each (rot / 2 <= 128 of the 512 lanes)
+  // and the other half of each of the wave's pairs
   [[maybe_unused]] double turn_f = 0.0;
   [[maybe_unused]] int turn_axis = 0, turn_pos[ROPE_MAX_AXES] = {0, 0, 0, 0};
+  [[maybe_unused]] uint16_t turn_x[2][QV];
   if constexpr (ROPE) {
+#pragma unroll
+    for (int ps = 0; ps < 2; ++ps) {
+      const int hd = head_of_col<G6>(wid + NW * ps);
+      const uint16_t* qh = a.q + ((int64_t)r * Hq + h * G + (hd >= 0 && hd < G ? hd : 0)) * D;
+#pragma unroll
+      for (int i = 0; i < QV; ++i) {
+        int f, pc = QV * lane + i;
+        bool up;
+        if (pc < a.rope.rot) rope_of_channel(a.rope, QV * lane + i, f, pc, up);
+        turn_x[ps][i] = qh[pc];
+      }
+    }
     if (tid < a.rope.rot / 2) {
       const RopeEntry e = a.rope.tab[tid];
       turn_f = e.freq;
@@ -387,6 +401,9 @@ __global__ __launch_bounds__(DecodeCfg<PAIR>::NT, PAIR && D == 128 ? 4 : 2) void
     }
   }
 
+  // (where the table of the token's cosines and sines lies in the ring)
+  constexpr int TURN_AT = ((NW - 2) * SLOTS + (SLOTS - 1)) * STAGE + PAGE * D + 256;
+  static_assert(NW - 2 >= 4 && PAGE * D + 256 + D / 2 * 16 <= STAGE && STAGE % 16 == 0, "the table fits");
   float* part = a.partials + (((int64_t)r * H + h) * a.max_chunks + chunk) * part_stride(G, D);
   // ---- chunk -> logical page range: equal-cost ranges over the table width,
   // known before any load, so the sequence length and the chunk's tags and
@@ -454,10 +471,10 @@ __global__ __launch_bounds__(DecodeCfg<PAIR>::NT, PAIR && D == 128 ? 4 : 2) void
     return;
   }
   if constexpr (ROPE) {
-    // cosine and sine per frequency, in the last wave's ring slot: its first copy is issued
-    // behind the barrier that follows the query build
-    double2* s_turn = reinterpret_cast<double2*>(ring + (NW - 1) * SLOTS * STAGE);
-    static_assert(NW - 1 >= 4 && D / 2 * (int)sizeof(double2) <= SLOTS * STAGE, "the table fits a slot not yet in use");
+    // cosine and sine per frequency, in the slot in which the append's K wave will assemble
+    // its page, behind that page's codes and table: that wave copies nothing into it before
+    // it has turned the new key
+    double2* s_turn = reinterpret_cast<double2*>(ring + TURN_AT);
     if (tid < a.rope.rot / 2) {
       int at = turn_pos[0];
 #pragma unroll
@@ -467,12 +484,10 @@ __global__ __launch_bounds__(DecodeCfg<PAIR>::NT, PAIR && D == 128 ? 4 : 2) void
       s_turn[tid] = make_double2(c, s);
     }
     __syncthreads();
-    // (the other half of each pair is loaded here: the first load has brought its line)
 #pragma unroll
     for (int ps = 0; ps < 2; ++ps) {
       const int hd = head_of_col<G6>(wid + NW * ps);
       if (hd < 0 || hd >= G) continue;  // wave-uniform
-      const uint16_t* qh = a.q + ((int64_t)r * Hq + h * G + hd) * D;
 #pragma unroll
       for (int i = 0; i < QV; ++i) {
         const int ch = QV * lane + i;
@@ -480,11 +495,11 @@ __global__ __launch_bounds__(DecodeCfg<PAIR>::NT, PAIR && D == 128 ? 4 : 2) void
           int f, pc;
           bool up;
           rope_of_channel(a.rope, ch, f, pc, up);
-          const double x = (double)qx[ps][i], xp = (double)bf16_to_f32(qh[pc]);
+          const double x = (double)qx[ps][i], xp = (double)bf16_to_f32(turn_x[ps][i]);
           const double2 cs = s_turn[f];
           double y0, y1;
           rope_rotate(up ? xp : x, up ? x : xp, cs.x, cs.y, y0, y1);
-          qx[ps][i] = bf16_to_f32((uint16_t)f64_to_bf16(up ? y1 : y0));
+          qx[ps][i] = f64_round_bf16(up ? y1 : y0);
         }
       }
     }
@@ -854,9 +869,16 @@ __global__ __launch_bounds__(DecodeCfg<PAIR>::NT, PAIR && D == 128 ? 4 : 2) void
       T.li = 0;
       T.h = h;
       small_task_load_x<D>(T, (int64_t)H * D, (int64_t)H * D, a.n_req, a.k_new, a.v_new, lane);
-      if constexpr (ROPE)
-        if (!kv) small_task_rotate<D>(T, a.rope, a.pos, a.n_req, reinterpret_cast<uint16_t*>(own), lane);
       small_task_load_old<D>(T, P, id, lane);
+      if constexpr (ROPE)
+        if (!kv) {  // while the old codes are on their way
+          const double2* s_turn = reinterpret_cast<const double2*>(ring + TURN_AT);
+          small_task_rotate<D>(T, a.rope, reinterpret_cast<uint16_t*>(own), lane, [&](int, int i, double& c, double& s) {
+            const double2 cs = s_turn[i];
+            c = cs.x;
+            s = cs.y;
+          });
+        }
       small_task_run<D>(T, P, id, reinterpret_cast<uint32_t*>(own), own + PAGE * D, lane);
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the token's codes and scale are stored
       if (lane == 0 && kv == 0) s_stage[n_st - 1].y = id;
@@ -959,11 +981,11 @@ __global__ __launch_bounds__(DecodeCfg<PAIR>::NT, PAIR && D == 128 ? 4 : 2) void
     // v_perm per 4 codes) and meet the query's E4M3 terms directly
     float4v sa = zero4, sb = zero4;
     if constexpr (FINE) {
-      // on the f16 MFMA: codebook values by the same v_perm and a conversion, hi and lo
-      // products in sums of their own, two each
-      float4v pa[4], pb[4];
+      // on the f16 MFMA: codebook values by the same v_perm and a conversion; the products
+      // with the query's high halves in two sums, those with its low halves in a third
+      float4v pa[3], pb[3];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) pa[i] = pb[i] = zero4;
+      for (int i = 0; i < 3; ++i) pa[i] = pb[i] = zero4;
       auto keys = [&](const uint32_t* k, int s) {
         const uint32_t u = __builtin_amdgcn_perm(KLUT_HI, KLUT_LO, quad_sel<NDW>(k, 2 * s));
         const uint32_t w = __builtin_amdgcn_perm(KLUT_HI, KLUT_LO, quad_sel<NDW>(k, 2 * s + 1));
@@ -974,15 +996,15 @@ __global__ __launch_bounds__(DecodeCfg<PAIR>::NT, PAIR && D == 128 ? 4 : 2) void
         const half8 qh = qrh[s * 64 + qlane], ql = qrl[s * 64 + qlane];
         const half8 ka = keys(kA, s);
         pa[s & 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ka, qh, pa[s & 1], 0, 0, 0);
-        pa[2 + (s & 1)] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ka, ql, pa[2 + (s & 1)], 0, 0, 0);
+        pa[2] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ka, ql, pa[2], 0, 0, 0);
         if (pair) {
           const half8 kb = keys(kB, s);
           pb[s & 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kb, qh, pb[s & 1], 0, 0, 0);
-          pb[2 + (s & 1)] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kb, ql, pb[2 + (s & 1)], 0, 0, 0);
+          pb[2] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kb, ql, pb[2], 0, 0, 0);
         }
       }
-      sa = (pa[0] + pa[1]) + (pa[2] + pa[3]);
-      if (pair) sb = (pb[0] + pb[1]) + (pb[2] + pb[3]);
+      sa = (pa[0] + pa[1]) + pa[2];
+      if (pair) sb = (pb[0] + pb[1]) + pb[2];
     } else {
 #pragma unroll
     for (int S = 0; S < NK8; ++S) {
@@ -1024,41 +1046,17 @@ __global__ __launch_bounds__(DecodeCfg<PAIR>::NT, PAIR && D == 128 ? 4 : 2) void
     // subnormal is c * 2^-9; the converter's power-of-two scale 2^9 makes it
     // c); v = zero + scale * code is applied in fp32 to the MFMA output,
     // the zero term through the rows' weight sums PS (MFMAs against ones)
-    if constexpr (FINE) {
-      // the products with the weights' low parts apart: added to the high parts' sum inside
-      // the matrix unit they lose their last bits, always downwards, and zero + scale *
-      // code, two sums of one sign each that nearly cancel, would not forgive it
-      const float4v PS = __builtin_amdgcn_mfma_f32_16x16x32_f16(pT, ones8, zero4, 0, 0, 0) +
-                         __builtin_amdgcn_mfma_f32_16x16x32_f16(pTl, ones8, zero4, 0, 0, 0);
-      auto codes_of = [&](int m) {
-        const uint32_t ua = quad_sel<NDW>(vA, m), ub = quad_sel<NDW>(vB, m);
-        return h8(cvt_code<false>(ua), cvt_code<true>(ua), cvt_code<false>(ub), cvt_code<true>(ub));
-      };
-      auto pv2 = [&](int m, float4v& hi, float4v& lo) {
-        const half8 c = codes_of(m);
-        hi = __builtin_amdgcn_mfma_f32_16x16x32_f16(pT, c, zero4, 0, 0, 0);
-        lo = __builtin_amdgcn_mfma_f32_16x16x32_f16(pTl, c, zero4, 0, 0, 0);
-      };
-      float4v X, Xl;
-      pv2(0, X, Xl);
-#pragma unroll
-      for (int m = 0; m < CL; ++m) {
-        float4v Xn = X, Xln = Xl;
-        if (m + 1 < CL) pv2(m + 1, Xn, Xln);
-        const float sm = (float)sO[m >> 1][m & 1], zm = (float)zO[m >> 1][m & 1];
-#pragma unroll
-        for (int i = 0; i < NI; ++i) st.acc[m][i] += fmaf(sm, Xl[i], fmaf(sm, X[i], zm * PS[i]));
-        X = Xn;
-        Xl = Xln;
-      }
-    } else {
+    // (FINE: the low parts' products first.  Added to the sum of the high parts' they would
+    // lose their last bits inside the matrix unit, always downwards, and zero + scale * code,
+    // two sums of one sign each that nearly cancel, would not forgive it)
+    const half8 p1 = FINE ? pTl : pT, p2 = FINE ? pT : pTl;
     const float4v PS = __builtin_amdgcn_mfma_f32_16x16x32_f16(
-        pTl, ones8, __builtin_amdgcn_mfma_f32_16x16x32_f16(pT, ones8, zero4, 0, 0, 0), 0, 0, 0);
+        p2, ones8, __builtin_amdgcn_mfma_f32_16x16x32_f16(p1, ones8, zero4, 0, 0, 0), 0, 0, 0);
     auto pv = [&](int m) {
       const uint32_t ua = quad_sel<NDW>(vA, m), ub = quad_sel<NDW>(vB, m);
       const half8 c = h8(cvt_code<false>(ua), cvt_code<true>(ua), cvt_code<false>(ub), cvt_code<true>(ub));
       return __builtin_amdgcn_mfma_f32_16x16x32_f16(
-          pTl, c, __builtin_amdgcn_mfma_f32_16x16x32_f16(pT, c, zero4, 0, 0, 0), 0, 0, 0);
+          p2, c, __builtin_amdgcn_mfma_f32_16x16x32_f16(p1, c, zero4, 0, 0, 0), 0, 0, 0);
     };
     // one tile ahead, so the MFMA of tile m + 1 runs while tile m is scaled
     float4v X = pv(0);
@@ -1071,7 +1069,6 @@ __global__ __launch_bounds__(DecodeCfg<PAIR>::NT, PAIR && D == 128 ? 4 : 2) void
       for (int i = 0; i < NI; ++i)
         st.acc[m][i] = fmaf((float)zm, PS[i], fmaf((float)sm, X[i], st.acc[m][i]));
       X = Xn;
-    }
     }
     if (SLOTS == 1) {
       jc = jr;
@@ -1111,18 +1108,18 @@ __global__ __launch_bounds__(DecodeCfg<PAIR>::NT, PAIR && D == 128 ? 4 : 2) void
     const float2 ksv = *reinterpret_cast<const float2*>(ra + R8);
     wait_lgkm0();  // the stage is in registers: refill its slot
     if (refill) issue(e2, slot);
-    // (FINE: four sums instead of one: the matrix unit rounds every eight products to the sum)
-    constexpr int NSUM = FINE ? 4 : 1;
-    float4v part4[NSUM];
+    // (FINE: two sums instead of one: the matrix unit rounds every eight products to the sum)
+    constexpr int NSUM = FINE ? 2 : 1;
+    float4v part2[NSUM];
 #pragma unroll
-    for (int s = 0; s < NSUM; ++s) part4[s] = zero4;
+    for (int s = 0; s < NSUM; ++s) part2[s] = zero4;
 #pragma unroll
     for (int s = 0; s < NS; ++s)
-      part4[s % NSUM] = __builtin_amdgcn_mfma_f32_16x16x32_f16(
+      part2[s % NSUM] = __builtin_amdgcn_mfma_f32_16x16x32_f16(
           h8(cvt_lo(kA[2 * s]), cvt_hi(kA[2 * s]), cvt_lo(kA[2 * s + 1]), cvt_hi(kA[2 * s + 1])),
-          qpl[s * 64 + qlane], part4[s % NSUM], 0, 0, 0);
-    float4v sa = part4[0];
-    if constexpr (FINE) sa = (sa + part4[1]) + (part4[2] + part4[3]);
+          qpl[s * 64 + qlane], part2[s % NSUM], 0, 0, 0);
+    float4v sa = part2[0];
+    if constexpr (FINE) sa = sa + part2[NSUM - 1];
     float sc[4];
     {
       const float kk = FINE ? ksv.x * smk * pinv : ksv.x * smk;
@@ -1145,11 +1142,8 @@ __global__ __launch_bounds__(DecodeCfg<PAIR>::NT, PAIR && D == 128 ? 4 : 2) void
 #pragma unroll
     for (int m = 0; m < CL; ++m) {
       const half8 v = h8(cvt_lo(vA[m]), cvt_hi(vA[m]), z2, z2);
-      const float4v X =
-          FINE ? __builtin_amdgcn_mfma_f32_16x16x32_f16(pT, v, zero4, 0, 0, 0) +
-                     __builtin_amdgcn_mfma_f32_16x16x32_f16(pTl, v, zero4, 0, 0, 0)
-               : __builtin_amdgcn_mfma_f32_16x16x32_f16(
-                     pTl, v, __builtin_amdgcn_mfma_f32_16x16x32_f16(pT, v, zero4, 0, 0, 0), 0, 0, 0);
+      const float4v X = __builtin_amdgcn_mfma_f32_16x16x32_f16(
+          FINE ? pT : pTl, v, __builtin_amdgcn_mfma_f32_16x16x32_f16(FINE ? pTl : pT, v, zero4, 0, 0, 0), 0, 0, 0);
 #pragma unroll
       for (int i = 0; i < NI; ++i) st.acc[m][i] = fmaf(ksv.y, X[i], st.acc[m][i]);
     }

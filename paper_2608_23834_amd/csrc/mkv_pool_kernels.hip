@@ -651,7 +651,8 @@ constexpr int STEP_APPEND_MAX_WAVES = 4096;
 
 
 // ROPE: the key tasks rotate their rows by the rows' positions before anything else reads
-// them (rows of k and v are kts and vts elements apart).
+// them (rows of k and v are kts and vts elements apart); the frequencies come in with round
+// trip 1, the positions with the rows.
 template <int D, bool ROPE>
 __global__ __launch_bounds__(64) void append_step_kernel(PoolView P, int layer_sel, int n_lcall,
                                                          int n_req, int32_t* bt, uint8_t* tags,
@@ -665,9 +666,15 @@ __global__ __launch_bounds__(64) void append_step_kernel(PoolView P, int layer_s
   __shared__ __align__(16) uint32_t s_img[PAGE * D / 4];
   __shared__ uint8_t s_lut[256];
   __shared__ __align__(16) uint16_t s_rows[ROPE ? PAGE * D : 8];
+  __shared__ RopeEntry s_freq[ROPE ? D / 2 : 1];
+  __shared__ int s_pos[ROPE ? ROPE_MAX_AXES * PAGE : 1];  // [axis][slot of the page]
   const int lane = threadIdx.x;
   const int H = P.n_kv_heads;
   // ---- round trip 1: rows, starts, free-list top
+  if constexpr (ROPE) {
+    if (!(blockIdx.x & 1))  // a key task
+      for (int i = lane; i < R.rot / 2; i += 64) s_freq[i] = R.tab[i];
+  }
   const int top = P.ctrl[CTRL_FP8_TOP];
   int bad = (cu[0] != 0 || cu[n_req] != n_new_total) ? (int)MKV_DEVERR_RANGE : 0;
   int run = 0;  // list entries of the requests before this group of 64
@@ -729,6 +736,7 @@ __global__ __launch_bounds__(64) void append_step_kernel(PoolView P, int layer_s
   const int64_t task = blockIdx.x;
   SmallTask<D> T;
   int e_t = 0;
+  [[maybe_unused]] int at = 0;  // ROPE: position of (axis lane / 16, slot lane % 16)
   if (task < n_tasks) {
     T.kv = (int)(task & 1);
     const int64_t item = task >> 1;
@@ -749,8 +757,12 @@ __global__ __launch_bounds__(64) void append_step_kernel(PoolView P, int layer_s
     T.t1 = min(PAGE, s0 + n - T.p * PAGE);
     // a listed page belongs to a request whose rows passed the range checks
     small_task_load_x<D>(T, kts, vts, n_new_total, k, v, lane);
-    if constexpr (ROPE)
-      if (!T.kv) small_task_rotate<D>(T, R, pos, n_new_total, s_rows, lane);
+    if constexpr (ROPE) {
+      const int t = lane & 15, ax = lane >> 4;  // a lane per (axis, slot)
+      static_assert(ROPE_MAX_AXES * PAGE == 64, "ROPE_MAX_AXES * PAGE lanes");
+      if (!T.kv && t >= T.t0 && t < T.t1 && ax < R.n_axes)
+        at = pos ? pos[(int64_t)ax * n_new_total + T.row0 + t] : T.p * PAGE + t;
+    }
   }
   // ---- validation and fresh-page ranks (identical in every wave)
   int fresh[EQ], rank[EQ], n_fresh = 0;
@@ -783,6 +795,14 @@ __global__ __launch_bounds__(64) void append_step_kernel(PoolView P, int layer_s
     for (int j = 0; j < EQ; ++j) idv = (e_t >> 6) == j ? ent_id[j] : idv;
     const int id = __builtin_amdgcn_readfirstlane(__shfl(idv, e_t & 63, 64));
     small_task_load_old<D>(T, P, id, lane);
+    if constexpr (ROPE)
+      if (!T.kv) {  // while the old codes are on their way
+        s_pos[lane] = at;
+        small_task_rotate<D>(T, R, s_rows, lane, [&](int tt, int i, double& c, double& s) {
+          const RopeEntry e = s_freq[i];
+          rope_cos_sin((double)s_pos[e.axis * PAGE + T.t0 + tt] * e.freq, R.scale, c, s);
+        });
+      }
     small_task_run<D>(T, P, id, s_img, s_lut, lane);
   }
   // ---- nothing to publish (no fresh page; every wave reached the same
