@@ -201,6 +201,16 @@ __device__ __forceinline__ float div_by(float x, float s, float y) {
   return __builtin_copysignf(q, x);
 }
 __device__ __forceinline__ bool div_fast(float s) { return s >= 0x1p-60f && s <= 0x1p60f; }
+// The same for a bf16 x whose quotient becomes an E4M3 code: one Newton step.  Its result
+// is x / s rounded, but for quotients within 2^-46 of the middle of two floats; a float that
+// an E4M3 boundary (five significant bits) parts from its neighbour there would need s of
+// mantissa all ones and the boundary 2^-10, and that one comes out right.  (Every mantissa of
+// s with every mantissa and sign of x and every exponent between: 5 10^10 equal codes.)
+__device__ __forceinline__ float div_by_for_code(float x, float s, float y) {
+  float q = x * y;
+  q = __builtin_fmaf(__builtin_fmaf(-q, s, x), y, q);
+  return __builtin_copysignf(q, x);
+}
 // four fp32 values -> four E4M3 bytes, as f32_to_e4m3
 __device__ __forceinline__ uint32_t pack_e4m3(float a, float b, float c, float d) {
   // (the median of a NaN is the smaller bound, as the clamp's result is)
@@ -276,7 +286,7 @@ __device__ __forceinline__ void quant_task(uint8_t* reg, float* sc, const uint16
 #pragma unroll
       for (int u = 0; u < 4; ++u)
 #pragma unroll
-        for (int b = 0; b < 4; ++b) q[u][b] = div_by(f4(4 * j + u, b), s_new, y);
+        for (int b = 0; b < 4; ++b) q[u][b] = div_by_for_code(f4(4 * j + u, b), s_new, y);
       // the group's dwords: K dword u = token ta + u, V dword b = channel 4 cg + b
       uint32_t w[4];
 #pragma unroll
@@ -473,7 +483,9 @@ __device__ __forceinline__ void rope_turn8(const RopeLane<D, VEC>& L, const Rope
 }
 // four values over s -> four codes; fast: div_fast(s) and y = 1 / s
 __device__ __forceinline__ uint32_t codes_over(const float* f, float s, float y, bool fast) {
-  if (fast) return pack_e4m3(div_by(f[0], s, y), div_by(f[1], s, y), div_by(f[2], s, y), div_by(f[3], s, y));
+  if (fast)
+    return pack_e4m3(div_by_for_code(f[0], s, y), div_by_for_code(f[1], s, y), div_by_for_code(f[2], s, y),
+                     div_by_for_code(f[3], s, y));
   if (!(s > 0.0f)) return 0u;
   return f32_to_e4m3(f[0] / s) | f32_to_e4m3(f[1] / s) << 8 | f32_to_e4m3(f[2] / s) << 16 | f32_to_e4m3(f[3] / s) << 24;
 }
