@@ -401,198 +401,122 @@ __global__ __launch_bounds__(256) void append_quant_kernel(PoolView P, int layer
 }
 
 // Keys of one page-head rotated and quantized by one wave, as quant_task does the plain
-// ones.  D / 8 lanes share a token, each with the two groups of four channels a and b whose
-// pairs it can turn by itself: 4 j .. and rot / 2 + 4 j .. (halves), 8 j .. and 8 j + 4 ..
-// (neighbours), so cosines and sines are four 16-byte LDS reads a token ([t][i % 4][i / 4]:
-// the lanes of a read are neighbours).  VEC needs rot / 2 in fours; otherwise (!VEC) a lane
-// holds channels 8 j .. and loads the other half of each pair again.
-// A whole page (VEC) has its rows loaded once, all in flight together, and kept as bf16 in
-// registers.  A partly filled one, which may hold old codes to re-round, goes token by token
-// twice, for the largest value and for the codes, and loads and turns its rows both times:
-// at most two pages of a request, in a function of its own and few registers.
+// ones: D / (2 V) lanes a token (rope_lane), the page's cosines and sines in LDS, [t][i % V]
+// [i / V], so that the lanes of a read are neighbours.  All rows are loaded at once and kept
+// as bf16 in registers between the largest value and the codes; where a page is partly
+// filled, the lanes of its other slots take the nearest row, which changes no maximum, and
+// hold their stores.
 // 33 K tokens x 4 heads x 4 layers at d = 256 (0.8 GB, 158 us of a copy's bandwidth): the
-// call takes 206 us with 118 registers and four waves a SIMD, 249 with 233 and two (rows kept
-// unpacked, both kinds of page in one body); the plain append of them takes 172.
-template <int D, bool VEC>
-struct RopeLane {
-  static constexpr int LT = D / 8, TP = 64 / LT, NP = PAGE / TP;  // lanes a token, tokens a pass, passes
-  int j, tl, m, ca, cb;
-  bool turn, inter;
-  uint32_t to, oa, ob;  // byte offsets into the rows: token tl, and its two groups
-  __device__ RopeLane(const RopeView& R, int64_t tstride, int lane) {
-    j = lane % LT;
-    tl = lane / LT;
-    m = R.rot / 2;
-    inter = R.interleaved;
-    turn = VEC ? j < m / 4 : 8 * j < R.rot;
-    ca = 8 * j;
-    cb = 8 * j + 4;
-    if (VEC && !inter) {
-      ca = turn ? 4 * j : R.rot + 8 * (j - m / 4);
-      cb = turn ? m + 4 * j : ca + 4;
-    }
-    to = (uint32_t)tl * (uint32_t)(2 * tstride);
-    oa = to + 2 * ca;
-    ob = to + 2 * cb;
-  }
-};
-// the eight channels (a, b: as loaded) of token t turned, as fp32 values
-template <int D, bool VEC>
-__device__ __forceinline__ void rope_turn8(const RopeLane<D, VEC>& L, const RopeView& R, const double2* tab, int t,
-                                           const uint8_t* row, const uint2& a, const uint2& b, float* x) {
-  const uint32_t w[4] = {a.x, a.y, b.x, b.y};
-#pragma unroll
-  for (int q = 0; q < 4; ++q) {
-    x[2 * q] = __uint_as_float(w[q] << 16);
-    x[2 * q + 1] = __uint_as_float(w[q] & 0xFFFF0000u);
-  }
-  if (!L.turn) return;
-  if constexpr (VEC) {
-    const double2* tt = tab + t * L.m + L.j;
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const double2 cs = tt[q * (L.m / 4)];
-      double y0, y1;
-      if (L.inter) {
-        rope_rotate((double)x[2 * q], (double)x[2 * q + 1], cs.x, cs.y, y0, y1);
-        x[2 * q] = f64_round_bf16(y0);
-        x[2 * q + 1] = f64_round_bf16(y1);
-      } else {
-        rope_rotate((double)x[q], (double)x[q + 4], cs.x, cs.y, y0, y1);
-        x[q] = f64_round_bf16(y0);
-        x[q + 4] = f64_round_bf16(y1);
-      }
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int c = 8 * L.j + i;
-      if (c < R.rot) {
-        int f, pc;
-        bool up;
-        rope_of_channel(R, c, f, pc, up);
-        const double2 cs = tab[t * L.m + f];
-        const double xo = (double)x[i];
-        const double xp = (double)bf16_to_f32(*reinterpret_cast<const uint16_t*>(row + (L.to + 2 * pc)));
-        double y0, y1;
-        rope_rotate(up ? xp : xo, up ? xo : xp, cs.x, cs.y, y0, y1);
-        x[i] = f64_round_bf16(up ? y1 : y0);
-      }
-    }
-  }
-}
-// four values over s -> four codes; fast: div_fast(s) and y = 1 / s
-__device__ __forceinline__ uint32_t codes_over(const float* f, float s, float y, bool fast) {
-  if (fast)
-    return pack_e4m3(div_by_for_code(f[0], s, y), div_by_for_code(f[1], s, y), div_by_for_code(f[2], s, y),
-                     div_by_for_code(f[3], s, y));
-  if (!(s > 0.0f)) return 0u;
-  return f32_to_e4m3(f[0] / s) | f32_to_e4m3(f[1] / s) << 8 | f32_to_e4m3(f[2] / s) << 16 | f32_to_e4m3(f[3] / s) << 24;
-}
+// call takes 197 us with 128 registers and four waves a SIMD, 249 with 233 and two (rows kept
+// unpacked); 214 with the partly filled pages in a loop over the tokens, which the launch
+// then waits for; the plain append of them takes 170.
 __device__ __forceinline__ float wave_max(float x) {
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) x = fmaxf(x, __shfl_xor(x, o, 64));
   return x;
 }
-
-template <int D>
-__device__ __forceinline__ void rope_quant_whole(uint8_t* reg, float* sc, const uint8_t* rows, int64_t tstride,
-                                                 const RopeView& R, const double2* tab, int lane) {
-  const RopeLane<D, true> L(R, tstride, lane);
-  constexpr int TP = L.TP, NP = L.NP;
-  uint2 xa[NP], xb[NP];
+template <int V>
+__device__ __forceinline__ void rope_codes(uint8_t* p, const float* x, float s, float y, bool fast, bool zero) {
+  uint32_t c = 0;
+  if (fast) {
+    if constexpr (V == 4) {
+      c = pack_e4m3(div_by_for_code(x[0], s, y), div_by_for_code(x[1], s, y), div_by_for_code(x[2], s, y),
+                    div_by_for_code(x[3], s, y));
+    } else {
 #pragma unroll
-  for (int i = 0; i < NP; ++i) {
-    xa[i] = *reinterpret_cast<const uint2*>(rows + TP * i * (2 * tstride) + L.oa);
-    xb[i] = *reinterpret_cast<const uint2*>(rows + TP * i * (2 * tstride) + L.ob);
-  }
-  float amax = 0.0f;
-#pragma unroll
-  for (int i = 0; i < NP; ++i) {
-    float x[8];
-    rope_turn8<D, true>(L, R, tab, TP * i + L.tl, rows, xa[i], xb[i], x);
-    xa[i] = make_uint2(bf16_pair(x[0], x[1]), bf16_pair(x[2], x[3]));
-    xb[i] = make_uint2(bf16_pair(x[4], x[5]), bf16_pair(x[6], x[7]));
-#pragma unroll
-    for (int b = 0; b < 8; ++b) amax = fmaxf(amax, fabsf(x[b]));
-    __builtin_amdgcn_sched_barrier(0);  // one token at a time: bounded register use
-  }
-  amax = wave_max(amax);
-#pragma unroll
-  for (int i = 0; i < NP; ++i) asm volatile("" : "+v"(xa[i].x), "+v"(xa[i].y), "+v"(xb[i].x), "+v"(xb[i].y));
-  const float s = amax / 448.0f, y = 1.0f / s;
-  const bool fast = __builtin_amdgcn_readfirstlane(div_fast(s));
-  const uint32_t da = (uint32_t)(L.tl * D + L.ca), db = (uint32_t)(L.tl * D + L.cb);
-#pragma unroll
-  for (int i = 0; i < NP; ++i) {
-    const uint32_t w[4] = {xa[i].x, xa[i].y, xb[i].x, xb[i].y};
-    float x[8];
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      x[2 * q] = __uint_as_float(w[q] << 16);
-      x[2 * q + 1] = __uint_as_float(w[q] & 0xFFFF0000u);
+      for (int k = 0; k < V; ++k) c |= f32_to_e4m3(div_by_for_code(x[k], s, y)) << (8 * k);
     }
-    *reinterpret_cast<uint32_t*>(reg + TP * D * i + da) = codes_over(x, s, y, fast);
-    *reinterpret_cast<uint32_t*>(reg + TP * D * i + db) = codes_over(x + 4, s, y, fast);
+  } else if (s > 0.0f) {
+#pragma unroll
+    for (int k = 0; k < V; ++k) c |= f32_to_e4m3(x[k] / s) << (8 * k);
   }
-  if (lane == 0) sc[0] = s;
+  if (zero) c = 0;
+  if constexpr (V == 4) *reinterpret_cast<uint32_t*>(p) = c;
+  else if constexpr (V == 2) *reinterpret_cast<uint16_t*>(p) = (uint16_t)c;
+  else *p = (uint8_t)c;
 }
 
-template <int D, bool VEC>
-__device__ __attribute__((noinline)) void rope_quant_part(uint8_t* reg, float* sc, const uint8_t* rows, int64_t tstride,
-                                                const RopeView& R, const double2* tab, int t0, int t1, int lane) {
-  const RopeLane<D, VEC> L(R, tstride, lane);
-  constexpr int TP = L.TP, NP = L.NP;
-  auto turned = [&](int i, float* x) {
-    const uint8_t* row = rows + TP * i * (2 * tstride);
-    const uint2 a = *reinterpret_cast<const uint2*>(row + L.oa), b = *reinterpret_cast<const uint2*>(row + L.ob);
-    rope_turn8<D, VEC>(L, R, tab, TP * i + L.tl, row, a, b, x);
-  };
-  float amax = 0.0f;
-#pragma unroll 1
-  for (int i = 0; i < NP; ++i) {
-    const int t = TP * i + L.tl;
-    if (t >= t0 && t < t1) {
-      float x[8];
-      turned(i, x);
+// codes of a page's first n bytes re-rounded from scale s_old to s: a page that was appended
+// to before and whose largest value has grown
+__device__ __attribute__((noinline)) void rope_requant(uint8_t* reg, int n, float s_old, float s, int lane) {
+  for (int i = 4 * lane; i < n; i += 256) {
+    uint32_t* p = reinterpret_cast<uint32_t*>(reg + i);
+    const uint32_t w = *p;
+    uint32_t o = 0;
 #pragma unroll
-      for (int b = 0; b < 8; ++b) amax = fmaxf(amax, fabsf(x[b]));
-    }
+    for (int b = 0; b < 4; ++b) o |= f32_to_e4m3((e4m3_to_f32((w >> (8 * b)) & 0xFFu) * s_old) / s) << (8 * b);
+    *p = o;
+  }
+}
+
+template <int D, int V, bool NEAR>
+__device__ __forceinline__ void rope_quant_task(uint8_t* reg, float* sc, const uint8_t* rows, int64_t tstride,
+                                                const RopeView& R, const double2* tab, int t0, int t1, int lane) {
+  typedef typename RopeGroup<V>::type group;
+  // LT lanes a token; a pass holds TP tokens or (D = 256, V = 1) half of one
+  constexpr int LT = D / (2 * V), NP = PAGE * LT / 64;
+  const int m = R.rot / 2;
+  const uint32_t ts = (uint32_t)(2 * tstride);
+  uint32_t w[NP][V];
+  auto slot = [&](int i, int& t, int& j) {
+    t = (64 * i) / LT + (LT < 64 ? lane / LT : 0);
+    j = (64 * i) % LT + (LT < 64 ? lane % LT : lane);
+  };
+#pragma unroll
+  for (int i = 0; i < NP; ++i) {
+    int t, j, ca, cb;
+    slot(i, t, j);
+    rope_lane<V>(R, j, ca, cb);
+    t = min(max(t, t0), t1 - 1);
+    const uint8_t* row = rows + (int64_t)t * ts;
+    const group a = *reinterpret_cast<const group*>(row + 2 * ca), b = *reinterpret_cast<const group*>(row + 2 * cb);
+    rope_words(a, b, w[i]);
+  }
+  float amax = 0.0f;
+  asm volatile("" : "+v"(lane));  // each walk over the passes works its slots out again
+#pragma unroll
+  for (int i = 0; i < NP; ++i) {
+    int t, j;
+    slot(i, t, j);
+    t = min(max(t, t0), t1 - 1);
+    float x[2 * V];
+    rope_unpack<V>(w[i], x);
+    const double2* tt = tab + t * m + j;
+    if (j < m / V) rope_turn<V, NEAR>(x, [&](int q) { return tt[q * (m / V)]; });
+    rope_pack<V>(x, w[i]);
+#pragma unroll
+    for (int b = 0; b < 2 * V; ++b) amax = fmaxf(amax, fabsf(x[b]));
+    __builtin_amdgcn_sched_barrier(0);  // one pass at a time: bounded register use
   }
   amax = wave_max(amax);
-  const float s_old = t0 > 0 ? sc[0] : 0.0f;
-  const bool grown = t0 == 0 || !(amax <= 448.0f * s_old);
-  const float s = grown ? amax / 448.0f : s_old, y = 1.0f / s;
-  const bool fast = __builtin_amdgcn_readfirstlane(div_fast(s));
-#pragma unroll 1
-  for (int i = 0; i < NP; ++i) {
-    const int t = TP * i + L.tl;
-    uint32_t* da = reinterpret_cast<uint32_t*>(reg + t * D + L.ca);
-    uint32_t* db = reinterpret_cast<uint32_t*>(reg + t * D + L.cb);
-    if (t >= t0 && t < t1) {
-      float x[8];
-      turned(i, x);
-      *da = codes_over(x, s, y, fast);
-      *db = codes_over(x + 4, s, y, fast);
-    } else if (t0 == 0) {
-      *da = *db = 0u;
-    } else if (grown && t < t0) {  // old codes, re-rounded to the new scale
-      auto again = [&](uint32_t w) {
-        uint32_t o = 0;
+#pragma unroll  // read the words again: kept unpacked, the values would fill the register file
+  for (int i = 0; i < NP; ++i)
 #pragma unroll
-        for (int b = 0; b < 4; ++b) o |= f32_to_e4m3((e4m3_to_f32((w >> (8 * b)) & 0xFFu) * s_old) / s) << (8 * b);
-        return o;
-      };
-      *da = again(*da);
-      *db = again(*db);
+    for (int q = 0; q < V; ++q) asm volatile("" : "+v"(w[i][q]));
+  asm volatile("" : "+v"(lane));
+  const float s_old = t0 > 0 ? sc[0] : 0.0f;
+  const float s = fmaxf(s_old, amax / 448.0f), y = 1.0f / s;
+  const bool fast = __builtin_amdgcn_readfirstlane(div_fast(s));
+#pragma unroll
+  for (int i = 0; i < NP; ++i) {
+    int t, j, ca, cb;
+    slot(i, t, j);
+    rope_lane<V>(R, j, ca, cb);
+    float x[2 * V];
+    rope_unpack<V>(w[i], x);
+    // slots behind the last token become zeros in a new page and stay in one that holds tokens
+    if (t >= t0 && (t < t1 || t0 == 0)) {
+      rope_codes<V>(reg + t * D + ca, x, s, y, fast, t >= t1);
+      rope_codes<V>(reg + t * D + cb, x + V, s, y, fast, t >= t1);
     }
   }
+  if (__builtin_amdgcn_readfirstlane(t0 > 0 && s > s_old)) rope_requant(reg, t0 * D, s_old, s, lane);
   if (lane == 0) sc[0] = s;
 }
 
 // Cosines and sines of slots [t0, t1) of a page, by the whole workgroup; a function of its own:
 // inlined, the series' constants stay in registers over the rest of the kernel.
-template <bool VEC>
+template <int V>
 __device__ __attribute__((noinline)) void rope_fill_table(RopeView R, const int32_t* pos, int n_new_total, int64_t row0,
                                                           int at0, int t0, int t1, double2* tab) {
   const int m = R.rot / 2;
@@ -601,15 +525,15 @@ __device__ __attribute__((noinline)) void rope_fill_table(RopeView R, const int3
     const RopeEntry en = R.tab[i];
     double c, s;
     rope_cos_sin(rope_pos(pos, n_new_total, row0 + t, en.axis, at0 + t) * en.freq, R.scale, c, s);
-    tab[t * m + (VEC ? (i & 3) * (m / 4) + (i >> 2) : i)] = make_double2(c, s);
+    tab[t * m + (i % V) * (m / V) + i / V] = make_double2(c, s);
   }
 }
 
 // append_quant_kernel with the keys rotated.  A workgroup takes a listed page and up to hb
 // of the call's (layer, head) pairs: the cosines and sines of the page's 16 tokens are
 // computed once into LDS, then each wave quantizes K and V of one pair after the other.
-template <int D, bool VEC>
-__global__ __launch_bounds__(256, VEC ? 4 : 3) void append_rope_quant_kernel(PoolView P, int layer_sel, int n_lcall, int hb,
+template <int D, int V, bool NEAR>
+__global__ __launch_bounds__(256, 4) void append_rope_quant_kernel(PoolView P, int layer_sel, int n_lcall, int hb,
                                                                 const int32_t* sb, const int32_t* cu,
                                                                 int n_new_total, const uint16_t* k,
                                                                 const uint16_t* v, int64_t kts, int64_t vts,
@@ -626,7 +550,7 @@ __global__ __launch_bounds__(256, VEC ? 4 : 3) void append_rope_quant_kernel(Poo
     const int t0 = max(0, s0 - p * PAGE), t1 = min(PAGE, s0 + n - p * PAGE);
     const int64_t row0 = (int64_t)cu[r] + (int64_t)p * PAGE - s0;  // input row of slot t is row0 + t
     __syncthreads();  // the last unit's table has been read
-    rope_fill_table<VEC>(R, pos, n_new_total, row0, p * PAGE, t0, t1, s_tab);
+    rope_fill_table<V>(R, pos, n_new_total, row0, p * PAGE, t0, t1, s_tab);
     __syncthreads();
     for (int lh = lh0 + wid; lh < lh1; lh += 4) {
       const int li = lh / H, h = lh - li * H, layer = layer_sel < 0 ? li : layer_sel;
@@ -634,10 +558,7 @@ __global__ __launch_bounds__(256, VEC ? 4 : 3) void append_rope_quant_kernel(Poo
       uint8_t* reg = P.fp8 + ph * fp8_region_bytes(D);
       float* sc = P.fp8_scales + ph * 2;
       const uint8_t* rows = reinterpret_cast<const uint8_t*>(k + ((int64_t)li * n_new_total + row0) * kts + (int64_t)h * D);
-      if (VEC && t0 == 0 && t1 == PAGE)
-        rope_quant_whole<D>(reg, sc, rows, kts, R, s_tab, lane);
-      else
-        rope_quant_part<D, VEC>(reg, sc, rows, kts, R, s_tab, t0, t1, lane);
+      rope_quant_task<D, V, NEAR>(reg, sc, rows, kts, R, s_tab, t0, t1, lane);
       quant_task<D, true>(reg, sc, v + (int64_t)li * n_new_total * vts + (int64_t)h * D, row0, t0, t1, vts, lane);
     }
   }
@@ -2204,11 +2125,15 @@ hipError_t launch_append_rope(const PoolView& P, const RopeView& R, int layer, i
     hipLaunchKernelGGL(kern, dim3(grid), dim3(256), lds, s, P, layer, n_lcall, hbi, sb, cu, n_new_total, k, v, kts,
                        vts, R, pos);
   };
-  const bool vec = R.rot % 8 == 0;
+  const int V = rope_width(R.rot);
   if (P.d == 256)
-    vec ? go(append_rope_quant_kernel<256, true>) : go(append_rope_quant_kernel<256, false>);
+    V == 4   ? R.interleaved ? go(append_rope_quant_kernel<256, 4, true>) : go(append_rope_quant_kernel<256, 4, false>)
+    : V == 2 ? R.interleaved ? go(append_rope_quant_kernel<256, 2, true>) : go(append_rope_quant_kernel<256, 2, false>)
+    : R.interleaved ? go(append_rope_quant_kernel<256, 1, true>) : go(append_rope_quant_kernel<256, 1, false>);
   else
-    vec ? go(append_rope_quant_kernel<128, true>) : go(append_rope_quant_kernel<128, false>);
+    V == 4   ? R.interleaved ? go(append_rope_quant_kernel<128, 4, true>) : go(append_rope_quant_kernel<128, 4, false>)
+    : V == 2 ? R.interleaved ? go(append_rope_quant_kernel<128, 2, true>) : go(append_rope_quant_kernel<128, 2, false>)
+    : R.interleaved ? go(append_rope_quant_kernel<128, 1, true>) : go(append_rope_quant_kernel<128, 1, false>);
   return hipGetLastError();
 }
 

@@ -93,10 +93,11 @@ __device__ __forceinline__ double rope_pos(const int32_t* pos, int64_t n, int64_
   return (double)(pos ? pos[(int64_t)axis * n + row] : at);
 }
 
-// where the pair of frequency i sits, and the pair of channel c
+// where the pair of frequency i sits
 __device__ __forceinline__ int2 rope_pair(const RopeView& R, int i) {
   return R.interleaved ? make_int2(2 * i, 2 * i + 1) : make_int2(i, i + R.rot / 2);
 }
+// and the pair of channel c: its frequency, the other channel, whether c is the upper one
 __device__ __forceinline__ void rope_of_channel(const RopeView& R, int c, int& freq, int& partner, bool& upper) {
   const int m = R.rot / 2;
   if (R.interleaved) {
@@ -108,6 +109,72 @@ __device__ __forceinline__ void rope_of_channel(const RopeView& R, int c, int& f
     freq = upper ? c - m : c;
     partner = upper ? c - m : c + m;
   }
+}
+
+// Rows by D / (2 V) lanes, V = 4, 2 or 1 (rot / 2 a multiple of V): lane j holds V whole
+// pairs, in two groups of V neighbouring channels, so it turns them by itself: V j .. and
+// rot / 2 + V j .. (halves), 2 V j .. and 2 V j + V .. (neighbours); lanes past the rotated
+// channels hold the others, two groups each.
+template <int V>
+struct RopeGroup;
+template <> struct RopeGroup<4> { typedef uint2 type; };
+template <> struct RopeGroup<2> { typedef uint32_t type; };
+template <> struct RopeGroup<1> { typedef uint16_t type; };
+
+inline int rope_width(int rot) { return rot % 8 == 0 ? 4 : rot % 4 == 0 ? 2 : 1; }
+
+template <int V>
+__device__ __forceinline__ bool rope_lane(const RopeView& R, int j, int& ca, int& cb) {
+  const int m = R.rot / 2;
+  const bool turn = j < m / V;
+  ca = 2 * V * j;
+  cb = ca + V;
+  if (!R.interleaved) {
+    ca = turn ? V * j : R.rot + 2 * V * (j - m / V);
+    cb = turn ? m + V * j : ca + V;
+  }
+  return turn;
+}
+// the two groups as V words of two values; these as 2 V fp32 values, and back
+__device__ __forceinline__ void rope_words(uint2 a, uint2 b, uint32_t (&w)[4]) { w[0] = a.x, w[1] = a.y, w[2] = b.x, w[3] = b.y; }
+__device__ __forceinline__ void rope_words(uint32_t a, uint32_t b, uint32_t (&w)[2]) { w[0] = a, w[1] = b; }
+__device__ __forceinline__ void rope_words(uint16_t a, uint16_t b, uint32_t (&w)[1]) { w[0] = a | (uint32_t)b << 16; }
+template <int V>
+__device__ __forceinline__ void rope_groups(const uint32_t (&w)[V], typename RopeGroup<V>::type& a, typename RopeGroup<V>::type& b) {
+  if constexpr (V == 4) a = make_uint2(w[0], w[1]), b = make_uint2(w[2], w[3]);
+  else if constexpr (V == 2) a = w[0], b = w[1];
+  else a = (uint16_t)w[0], b = (uint16_t)(w[0] >> 16);
+}
+template <int V>
+__device__ __forceinline__ void rope_unpack(const uint32_t (&w)[V], float* x) {
+#pragma unroll
+  for (int q = 0; q < V; ++q) {
+    x[2 * q] = __uint_as_float(w[q] << 16);
+    x[2 * q + 1] = __uint_as_float(w[q] & 0xFFFF0000u);
+  }
+}
+template <int V>
+__device__ __forceinline__ void rope_pack(const float* x, uint32_t (&w)[V]) {
+#pragma unroll
+  for (int q = 0; q < V; ++q) w[q] = bf16_pair(x[2 * q], x[2 * q + 1]);
+}
+// the lane's pairs turned, cos_sin(q) those of pair q; the values are bf16 again
+template <int V, bool NEAR, class F>
+__device__ __forceinline__ void rope_turn(float* x, F cos_sin) {
+#pragma unroll
+  for (int q = 0; q < V; ++q) {
+    constexpr int step = NEAR ? 2 : 1, other = NEAR ? 1 : V;
+    const double2 cs = cos_sin(q);
+    double y0, y1;
+    rope_rotate((double)x[step * q], (double)x[step * q + other], cs.x, cs.y, y0, y1);
+    x[step * q] = f64_round_bf16(y0);
+    x[step * q + other] = f64_round_bf16(y1);
+  }
+}
+template <int V, class F>
+__device__ __forceinline__ void rope_turn(float* x, bool interleaved, F cos_sin) {
+  if (interleaved) rope_turn<V, true>(x, cos_sin);
+  else rope_turn<V, false>(x, cos_sin);
 }
 
 }  // namespace mkv
