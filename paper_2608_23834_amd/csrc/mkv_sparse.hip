@@ -189,6 +189,9 @@ typedef __bf16 bf2 __attribute__((ext_vector_type(2)));
 // of the sum so far, which grows to sum |q b| <= 448 sum |q| over two sums of d / 8 such
 // steps (d = 256: 32): 32 * 8.5 / 2 * 2^-24 = 2^-16.9 of it; 2^-16 here.  (Measured: 2^-25.)
 constexpr float SCORE_ERR = 448.0f * 0x1p-16f;
+// Where products are subnormal or a subnormal query entry counts as 0: at most 448 * 2^-126
+// of each of 256 channels, 2^-109, over s_p; and 2^-126 for the product with s_p itself.
+constexpr float SCORE_SUB = 0x1p-109f;
 
 // Step 1: one wave per 16 pages and step of the grid.  A: lane (page l % 16, group l / 16)
 // loads 16 bytes of every 64 of its page's row; B: the same channels of head l % 16, in
@@ -300,7 +303,10 @@ __device__ __forceinline__ uint64_t exact_key(const uint16_t* qs, int G, const u
     lo[i] = (double)e4m3_to_f32(cl >> (8 * i) & 0xFFu);
   }
   double best = -INFINITY;
-  bool nan = false;
+  bool nan = false;  // a NaN among the extremes is one whatever the query's signs
+#pragma unroll
+  for (int i = 0; i < NC; ++i) nan |= hi[i] != hi[i] || lo[i] != lo[i];
+  nan = __any(nan);
 #pragma unroll 2
   for (int g = 0; g < G; ++g) {
     double a = 0.0;
@@ -375,6 +381,7 @@ __global__ __launch_bounds__(SEL_NT) void select_pick_kernel(int H, int G, const
   static_assert(SEL_LDS <= SEL_MAX_PAGES / 32, "the scores fit");
   __shared__ int s_idx[SEL_NB], s_scan[SEL_NW + 1], s_sum[2][SEL_NW], s_digit, s_above, s_here, s_nb, s_in;
   __shared__ float s_min[SEL_NW], s_max[SEL_NW], s_smax[SEL_NW], s_l1[16];
+  __shared__ int s_nan[SEL_NW];
   const int h = blockIdx.x, r = blockIdx.y, tid = threadIdx.x, lane = tid & 63;
   const int wid = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int64_t row = (int64_t)r * H + h;
@@ -407,11 +414,13 @@ __global__ __launch_bounds__(SEL_NT) void select_pick_kernel(int H, int G, const
     // ---- 1. range and error
     for (int i = tid; i < SEL_BINS; i += SEL_NT) s_cnt[i] = 0;
     float mn = INFINITY, mx = -INFINITY, sm = 0.0f, l1 = 0.0f;
+    bool nan = false;
     for (int p = m0 + tid; p < m1; p += SEL_NT) {
       const float a = sg[p];
       if (few) s_sc[p] = a;
       mn = fminf(mn, a);
       mx = fmaxf(mx, a);
+      nan |= a != a;
       sm = larger(sm, fabsf(bs[p]));
     }
     if (wid < G) {
@@ -435,7 +444,9 @@ __global__ __launch_bounds__(SEL_NT) void select_pick_kernel(int H, int G, const
     fold(std::integral_constant<int, 8>{});
     fold(std::integral_constant<int, 16>{});
     fold(std::integral_constant<int, 32>{});
+    const int any_nan = __any(nan);
     if (lane == 0) {
+      s_nan[wid] = any_nan;
       s_min[wid] = mn;
       s_max[wid] = mx;
       s_smax[wid] = sm;
@@ -450,16 +461,18 @@ __global__ __launch_bounds__(SEL_NT) void select_pick_kernel(int H, int G, const
       mx = fmaxf(mx, s_max[w]);
       sm = larger(sm, s_smax[w]);
       l1 = larger(l1, s_l1[w]);
+      nan |= s_nan[w];
     }
-    const float E2 = 2.0f * SCORE_ERR * l1 * sm;
-    // ---- 2. the bin of the need-th largest.  A range without a finite width, or an error
-    // without one, leaves every page open
+    const float E2 = 2.0f * (SCORE_ERR * l1 + SCORE_SUB) * sm + 0x1p-125f;
+    // ---- 2. the bin of the need-th largest.  A range without a finite width, or of one at
+    // which bin() would lose its bits to the subnormals, or an error without one, leaves
+    // every page open
     const float width = mx - mn;
-    const bool bins = width > 0.0f && width < INFINITY && E2 < INFINITY;
+    const bool bins = width > 0x1p-100f && width < INFINITY && E2 < INFINITY;
     const float inv = bins ? (float)(SEL_BINS - 1) / width : 0.0f;
     auto bin = [&](float a) { return bins ? min(max((int)((a - mn) * inv), 0), SEL_BINS - 1) : 0; };
     float lo = -INFINITY;
-    if (E2 == 0.0f) {  // a query or scales of zeros: every score is 0
+    if ((l1 == 0.0f || sm == 0.0f) && mn == mx && !nan) {  // a query or scales of zeros: every score is 0
       lowest = need;
       lo = INFINITY;
     }
@@ -625,7 +638,7 @@ hipError_t launch_select(const PoolView& P, int layer, int n_req, const uint16_t
   if (max_pages > n_select) {
     // waves: three a SIMD, not more than there are tiles
     const int64_t pairs = (int64_t)n_req * H, tiles = (max_pages + 15) / 16;
-    int64_t nb = (3072 + pairs - 1) / pairs;
+    int64_t nb = (3 * 1024 + pairs - 1) / pairs;
     if (nb > tiles) nb = tiles;
     const dim3 grid((unsigned)nb, (unsigned)H, (unsigned)n_req);
     auto go = [&](auto kern) {

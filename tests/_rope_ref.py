@@ -49,6 +49,7 @@ def e4m3(codes):
     c = np.asarray(codes, np.uint8).astype(np.int64)
     e, m = (c >> 3) & 15, c & 7
     v = np.where(e == 0, m * 2.0 ** -9, (8 + m) * 2.0 ** (e.astype(np.float64) - 10))
+    v = np.where(c & 127 == 127, np.nan, v)
     return np.where(c & 128, -v, v)
 
 

@@ -197,6 +197,38 @@ def test_selection_scales_that_overflow():
     assert np.array_equal(got, want) and 5 in got[0, 0] and 30 in got[0, 0]
 
 
+@pytest.mark.parametrize("qe,se", [(-60, -75), (-126, -3), (-133, -10), (-20, -126), (-140, -126), (-100, 20)])
+def test_selection_of_tiny_scores(qe, se):
+    """Queries and scales whose products fall below fp32's numbers: the choice is fp64's."""
+    import paper_2608_23834_amd as mk
+    rng = np.random.default_rng(8)
+    pool = mk.Pool(1, 16, 2, 256, 1, 1, 64, np.ones(256, np.int8))
+    b = _random_bounds(rng, pool, 2, 500)
+    b.scales.copy_(_gpu((2.0 ** se * rng.uniform(1, 2, b.scales.shape)).astype(np.float32)))
+    q = wl.bf16_round((2.0 ** qe * rng.standard_normal((2, 16, 256))).astype(np.float32))
+    vals, sc = _values(b)
+    want, cnt = ref.select(ref.scores(q, vals[0], sc[0]), [8000, 7991], 40, 2, 3)
+    got, gc = _select(pool, b, q, [8000, 7991], 40, 2, 3)
+    assert np.array_equal(gc, cnt) and np.array_equal(got, want)
+
+
+def test_selection_zero_query_and_nan_keys():
+    """0 * NaN is NaN: pages whose extremes hold one come last even where all other scores are 0."""
+    import paper_2608_23834_amd as mk
+    rng = np.random.default_rng(9)
+    pool = mk.Pool(1, 8, 2, 128, 1, 1, 64, np.ones(128, np.int8))
+    b = _random_bounds(rng, pool, 2, 300)
+    codes = b.codes.cpu().numpy()
+    codes[0, :, :, [3, 17, 40], 0, 5] = 0x7F
+    b.codes.copy_(_gpu(codes))
+    vals, sc = _values(b)
+    q = wl.bf16_round(rng.standard_normal((2, 8, 128)).astype(np.float32))
+    q[0] = 0
+    want, _ = ref.select(ref.scores(q, vals[0], sc[0]), [4800, 4800], 30, 0, 1)
+    got, _ = _select(pool, b, q, [4800, 4800], 30, 0, 1)
+    assert np.array_equal(got, want) and not np.isin(got[0], [3, 17]).any()
+
+
 def test_selection_bad_lengths_and_refusals():
     import paper_2608_23834_amd as mk
     torch = _torch()
