@@ -368,6 +368,7 @@ class Rope:
         b = ctypes.c_size_t()
         _check("kv_rope_bytes", lib().kv_rope_bytes(self.rot_dim, ctypes.byref(b)))
         self.table = torch.zeros(b.value, dtype=torch.uint8, device=device)
+        self.device = self.table.get_device()
         desc = RopeDesc(head_dim, self.rot_dim, n_axes, int(bool(interleaved)), float(scale), f.ctypes.data,
                         None if ax is None else ax.ctypes.data, self.table.data_ptr(), b.value)
         h = ctypes.c_void_p()
@@ -405,9 +406,12 @@ def _rows(dev, t):
 
 
 def _positions(dev, rope, positions, n):
+    if rope.device != dev:
+        raise ValueError("the rope's table is on another device")
     if positions is None:
         return None
-    if positions.shape != (rope.n_axes, n) or positions.get_device() != dev or not positions.is_contiguous():
+    if (positions.shape != (rope.n_axes, n) or positions.get_device() != dev or positions.element_size() != 4
+            or not positions.is_contiguous()):
         raise ValueError(f"positions are contiguous int32 [{rope.n_axes}][{n}] on the current device")
     return positions.data_ptr()
 
@@ -431,6 +435,9 @@ def kv_append_fp8_rope(pool: Pool, rope: Rope, layer, block_table, tags, seq_len
     dev, cur = _current()
     n_req, max_pages = block_table.shape
     n = k.shape[-3]
+    want = (n, pool.n_kv_heads, pool.d)
+    if k.shape != v.shape or k.shape != (want if layer >= 0 else (pool.n_layers, *want)):
+        raise ValueError("k and v are [n][H][head_dim], with all layers [n_layers][n][H][head_dim]")
     _here(dev, block_table, tags, seq_lens_before, cu_new_tokens)
     _check("kv_append_fp8_rope", lib().kv_append_fp8_rope(
         pool.handle, rope.handle, layer, n_req, block_table.data_ptr(), tags.data_ptr(), max_pages,

@@ -453,7 +453,7 @@ template <int D, int V, bool NEAR>
 __device__ __forceinline__ void rope_quant_task(uint8_t* reg, float* sc, const uint8_t* rows, int64_t tstride,
                                                 const RopeView& R, const double2* tab, int t0, int t1, int lane) {
   typedef typename RopeGroup<V>::type group;
-  // LT lanes a token; a pass holds TP tokens or (D = 256, V = 1) half of one
+  // LT lanes a token; a pass of the wave holds 64 / LT tokens, or (D = 256, V = 1) half of one
   constexpr int LT = D / (2 * V), NP = PAGE * LT / 64;
   const int m = R.rot / 2;
   const uint32_t ts = (uint32_t)(2 * tstride);
@@ -495,7 +495,8 @@ __device__ __forceinline__ void rope_quant_task(uint8_t* reg, float* sc, const u
     for (int q = 0; q < V; ++q) asm volatile("" : "+v"(w[i][q]));
   asm volatile("" : "+v"(lane));
   const float s_old = t0 > 0 ? sc[0] : 0.0f;
-  const float s = fmaxf(s_old, amax / 448.0f), y = 1.0f / s;
+  const bool grown = t0 == 0 || !(amax <= 448.0f * s_old);
+  const float s = grown ? amax / 448.0f : s_old, y = 1.0f / s;
   const bool fast = __builtin_amdgcn_readfirstlane(div_fast(s));
 #pragma unroll
   for (int i = 0; i < NP; ++i) {
@@ -510,7 +511,7 @@ __device__ __forceinline__ void rope_quant_task(uint8_t* reg, float* sc, const u
       rope_codes<V>(reg + t * D + cb, x + V, s, y, fast, t >= t1);
     }
   }
-  if (__builtin_amdgcn_readfirstlane(t0 > 0 && s > s_old)) rope_requant(reg, t0 * D, s_old, s, lane);
+  if (__builtin_amdgcn_readfirstlane(t0 > 0 && grown)) rope_requant(reg, t0 * D, s_old, s, lane);
   if (lane == 0) sc[0] = s;
 }
 

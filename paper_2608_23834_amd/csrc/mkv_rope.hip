@@ -13,17 +13,17 @@ namespace mkv {
 // works.  Memory bound from some thousand rows on (16,384 tokens of 24 heads at d = 256: 403 MB
 // in 86 us, a copy of them takes 74); with one head in flight instead of four it took 100.
 template <int D, int V>
-__global__ __launch_bounds__(256) void rope_apply_kernel(RopeView R, int n_tokens, int n_heads, int hb,
+__global__ __launch_bounds__(256) void rope_apply_kernel(RopeView R, int64_t t0, int n_here, int n_tokens, int n_heads, int hb,
                                                          const uint16_t* x, int64_t xs, const int32_t* pos,
                                                          uint16_t* out, int64_t os) {
   typedef typename RopeGroup<V>::type group;
   constexpr int LT = D / (2 * V), HU = 4;  // lanes of a token; heads in flight
   const int nb = (n_heads + hb - 1) / hb;
   const int64_t unit = (int64_t)blockIdx.x * (256 / LT) + threadIdx.x / LT;
-  if (unit >= (int64_t)n_tokens * nb) return;
+  if (unit >= (int64_t)n_here * nb) return;
   const int j = threadIdx.x % LT;
-  const int64_t t = unit / nb;
-  const int h0 = (int)(unit - t * nb) * hb, h1 = min(h0 + hb, n_heads);
+  const int64_t tu = unit / nb, t = t0 + tu;
+  const int h0 = (int)(unit - tu * nb) * hb, h1 = min(h0 + hb, n_heads);
   int ca, cb;
   const bool turn = rope_lane<V>(R, j, ca, cb);
   double c[V], s[V];
@@ -67,17 +67,21 @@ __global__ __launch_bounds__(256) void rope_apply_kernel(RopeView R, int n_token
 
 hipError_t launch_rope_apply(const RopeView& R, int d, int n_tokens, int n_heads, const uint16_t* x, int64_t xs,
                              const int32_t* pos, uint16_t* out, int64_t os, hipStream_t s) {
-  if (n_tokens == 0) return hipSuccess;
   // heads per lane group: all of them once that fills the chip (eight waves per SIMD), so
   // that an angle serves every head
   const int V = rope_width(R.rot), lt = d / (2 * V), per = 256 / lt;
   int64_t nb = ((int64_t)8192 * 64 / lt + n_tokens - 1) / n_tokens;
   if (nb > n_heads) nb = n_heads;
   const int hb = (int)((n_heads + nb - 1) / nb);
-  const int64_t units = (int64_t)n_tokens * ((n_heads + hb - 1) / hb);
-  const dim3 grid((unsigned)((units + per - 1) / per));
   auto go = [&](auto kern) {
-    hipLaunchKernelGGL(kern, grid, dim3(256), 0, s, R, n_tokens, n_heads, hb, x, xs, pos, out, os);
+    // (a launch holds 2^32 threads at most: 2^22 tokens and up to 8192 * 64 lanes' worth of
+    // head blocks stay below 2^30)
+    for (int64_t t0 = 0; t0 < n_tokens; t0 += 1 << 22) {
+      const int n_here = (int)(n_tokens - t0 < 1 << 22 ? n_tokens - t0 : 1 << 22);
+      const int64_t units = (int64_t)n_here * ((n_heads + hb - 1) / hb);
+      hipLaunchKernelGGL(kern, dim3((unsigned)((units + per - 1) / per)), dim3(256), 0, s, R, t0, n_here, n_tokens,
+                         n_heads, hb, x, xs, pos, out, os);
+    }
   };
   if (d == 256)
     V == 4 ? go(rope_apply_kernel<256, 4>) : V == 2 ? go(rope_apply_kernel<256, 2>) : go(rope_apply_kernel<256, 1>);

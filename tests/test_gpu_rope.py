@@ -123,6 +123,46 @@ def test_apply_other_stream():
     assert ref.same_bits(out.cpu().numpy(), ref.rotate(x, pos, freq, axis, False))
 
 
+@pytest.mark.parametrize("rot", [128, 6])
+def test_apply_of_many_tokens(rot):
+    """More tokens than one launch takes, byte offsets past 2^31 between input and positions."""
+    import paper_2608_23834_amd as mk
+    torch = _torch()
+    n = (1 << 23) + 77
+    rope, freq, axis = _rope(128, rot, 2)
+    rng = np.random.default_rng(rot)
+    some = _bits(rng, 4096, 1, 128)
+    x = _i16(some).repeat((n + 4095) // 4096, 1, 1)[:n].contiguous()
+    pos = torch.arange(2 * n, dtype=torch.int32, device="cuda").view(2, n)
+    mk.kv_rope_apply(rope, x, pos, x)
+    for a in (0, (1 << 22) - 40, (1 << 23) - 40, n - 50):
+        i = np.arange(a, a + 50)
+        want = ref.rotate(some[i % 4096], np.stack([i, n + i]).astype(np.int32), freq, axis, False)
+        assert ref.same_bits(x[a:a + 50].cpu().numpy(), want), a
+
+
+def test_wrapper_refusals():
+    import paper_2608_23834_amd as mk
+    torch = _torch()
+    rope, _, _ = _rope(128, 64, 2)
+    x = torch.zeros((4, 2, 128), dtype=torch.int16, device="cuda")
+    pos = torch.zeros((2, 4), dtype=torch.int32, device="cuda")
+    for bad in (pos.long(), pos[:1], pos.cpu(), pos.t().contiguous().t()):
+        with pytest.raises(ValueError):
+            mk.kv_rope_apply(rope, x, bad, x)
+    rope.device += 1  # as if its table lay on another card
+    with pytest.raises(ValueError):
+        mk.kv_rope_apply(rope, x, pos, x)
+    rope.device -= 1
+    t = _twin(_w(128, 8, 2, 1), [64], 2)
+    z, cu = torch.zeros(1, dtype=torch.int32, device="cuda"), _gpu(np.array([0, 4], np.int32))
+    two = torch.zeros((2, 4, 2, 128), dtype=torch.int16, device="cuda")
+    for layer, k, v in ((0, x, x[:3]), (-1, x, x), (0, two, two), (-1, two[:1], two[:1]), (0, x[:, :1], x[:, :1])):
+        with pytest.raises(ValueError):
+            mk.kv_append_fp8_rope(t.gpu, rope, layer, t.bt, t.tags, z, cu, pos, k, v)
+    t.check_tables()
+
+
 # ---------------------------------------------------------------- appends
 
 def _w(d, hq, hkv, n_req, layers=1):
@@ -227,6 +267,39 @@ def test_append_special_values(turned):
     assert torch.equal(ta.bt, tb.bt)
     assert torch.equal(ta.gpu.fp8, tb.gpu.fp8)
     assert np.array_equal(ta.gpu.fp8_scales.cpu().numpy().view(np.uint32), tb.gpu.fp8_scales.cpu().numpy().view(np.uint32))
+
+
+@pytest.mark.parametrize("d,rot,inter", [(256, 64, False), (256, 20, True), (256, 22, False), (128, 128, True),
+                                         (128, 36, False), (128, 126, True)])
+def test_append_grown_pages_of_any_magnitude(d, rot, inter):
+    """Pages that three large calls fill in turn, with values from bf16's subnormals up, equal, a
+    little larger or much larger from call to call: the pages of a rotation and a plain append."""
+    import paper_2608_23834_amd as mk
+    torch = _torch()
+    rng = np.random.default_rng(d + rot)
+    n_req, w = 96, _w(d, 4, 2, 96)
+    ta, tb = _twin(w, [64] * n_req, 1), _twin(w, [64] * n_req, 1)
+    rope, _, _ = _rope(d, rot, 1, inter)
+    mag = 2.0 ** rng.integers(-134, 4, (n_req, 1, 2, 1))
+    at = np.zeros(n_req, np.int32)
+    for call in range(3):
+        c = rng.integers(1, 21, n_req)
+        cu = np.r_[0, np.cumsum(c)].astype(np.int32)
+        n, r = int(cu[-1]), np.repeat(np.arange(n_req), c)
+        assert n > 512
+        f = rng.choice([0.25, 1.0, 1.0, 1.01, 8.0], (n_req, 1, 2, 1))
+        mag = mag * f
+        base = np.sign(rng.standard_normal((n, 2, d))) * rng.choice([0.5, 1.0, 0.01], (n, 2, d))
+        K, V = (wl.bf16_round((base * mag[r][:, 0]).astype(np.float32)) for _ in range(2))
+        pos = np.where(rng.random((1, n)) < 0.5, 0, rng.integers(0, 5000, (1, n))).astype(np.int32)
+        kg, vg, pg, sb, cug = _i16(K), _i16(V), _gpu(pos), _gpu(at), _gpu(cu)
+        mk.kv_append_fp8_rope(ta.gpu, rope, 0, ta.bt, ta.tags, sb, cug, pg, kg, vg)
+        mk.kv_rope_apply(rope, kg, pg, kg)
+        mk.kv_append_fp8(tb.gpu, 0, tb.bt, tb.tags, sb, cug, kg, vg)
+        torch.cuda.synchronize()
+        assert torch.equal(ta.bt, tb.bt) and torch.equal(ta.gpu.fp8, tb.gpu.fp8), call
+        assert torch.equal(ta.gpu.fp8_scales.view(torch.int32), tb.gpu.fp8_scales.view(torch.int32)), call
+        at = at + c.astype(np.int32)
 
 
 def test_append_nothing_and_refusals():
