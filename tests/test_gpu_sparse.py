@@ -515,3 +515,143 @@ def test_serving_run(d, hq, hkv, captured):
             t.migrate()
             t.check_tables()
     assert mk.kv_pool_check_errors(t.gpu) == 0
+
+
+def test_far_pages():
+    """Page ids whose bytes lie past 2^32: the same answers, bit for bit, as from a small pool."""
+    import paper_2608_23834_amd as mk
+    torch = _torch()
+    d, hq, hkv, lens = 256, 24, 4, [900, 33, 17]
+    rng = np.random.default_rng(12)
+    n = sum(lens)
+    rows, new = (_i16(wl.bf16_round(rng.standard_normal((c, hq + 2 * hkv, d)).astype(np.float32))) for c in (n, 3))
+    q = _i16(wl.bf16_round(rng.standard_normal((3, hq, d)).astype(np.float32)))
+    rope = mk.Rope(d, 1e6 ** (-np.arange(32) / 32))
+    cu, zero, one = _gpu(np.r_[0, np.cumsum(lens)].astype(np.int32)), _gpu(np.zeros(3, np.int32)), _gpu(np.arange(4, dtype=np.int32))
+    held, after = _gpu(np.array(lens, np.int32)), _gpu(np.array(lens, np.int32) + 1)
+
+    def answers(n8, order):
+        pool = mk.Pool(1, hq, hkv, d, n8, 1, 4096, np.ones(d, np.int8), order)
+        mk.paged_attn_set_deterministic(pool, True)
+        bt = torch.full((3, 60), -1, dtype=torch.int32, device="cuda")
+        tags = torch.full((3, 60), 0xFF, dtype=torch.uint8, device="cuda")
+        mk.kv_append_fp8_rope(pool, rope, 0, bt, tags, zero, cu, None, rows[:, hq:hq + hkv], rows[:, hq + hkv:])
+        mk.kv_append_fp8_rope(pool, rope, 0, bt, tags, held, one, None, new[:, hq:hq + hkv], new[:, hq + hkv:])
+        b = mk.PageBounds(pool, 3, 60)
+        mk.kv_page_bounds_update(pool, 0, bt, tags, zero, after, b)
+        pages, counts = torch.zeros((3, hkv, 20), dtype=torch.int32, device="cuda"), torch.zeros((3, hkv), dtype=torch.int32, device="cuda")
+        mk.paged_attn_select_pages(pool, 0, q, after, b, 1, 2, pages, counts, mk.select_workspace(pool, 3, 60))
+        out, lse = torch.zeros((3, hq, d), device="cuda"), torch.zeros((3, hq), device="cuda")
+        mk.paged_attn_decode_sparse(pool, 0, q, bt, tags, after, pages, counts, out, lse, mk.workspace(pool, 3, 20))
+        step, slse = torch.zeros((3, hq, d), device="cuda"), torch.zeros((3, hq), device="cuda")
+        mk.paged_attn_decode_append_rope(pool, rope, 0, q, new[:, hq:hq + hkv].contiguous(), new[:, hq + hkv:].contiguous(),
+                                         None, bt, tags, after, step, slse, mk.workspace(pool, 3, 60))
+        torch.cuda.synchronize()
+        assert mk.kv_pool_check_errors(pool) == 0
+        return bt.max().item(), [x.clone() for x in (b.codes, b.scales, pages, counts, out, lse, step, slse)]
+    n8 = 140000  # 32 KB a page
+    small = answers(80, None)[1]
+    tops = []
+    for order in (np.arange(n8, dtype=np.int32), np.arange(n8, dtype=np.int32)[::-1]):
+        top, far = answers(n8, order)
+        tops.append(top)
+        for k, (x, y) in enumerate(zip(small, far)):
+            assert torch.equal(x, y), k
+    assert max(tops) * 32768 > 2 ** 32
+
+
+def test_far_bounds():
+    """Bounds of more than 2^32 bytes, the request in question at their end and its sequence the
+    table's whole width."""
+    import paper_2608_23834_amd as mk
+    torch = _torch()
+    n_req, mp, k = 130, 65536, 100
+    rng = np.random.default_rng(14)
+    pool = mk.Pool(1, 4, 2, 128, 64, 1, 64, np.ones(128, np.int8))
+    b = mk.PageBounds(pool, n_req, mp)
+    assert b.codes.numel() > 2 ** 32
+    some = _random_bounds(rng, pool, 1, 400)
+    at = np.sort(rng.choice(mp, 400, replace=False))
+    for h in range(2):
+        b.codes[0, -1, h, torch.from_numpy(at).cuda()] = some.codes[0, 0, h]
+        b.scales[0, -1, h, torch.from_numpy(at).cuda()] = some.scales[0, 0, h]
+    q = wl.bf16_round(rng.standard_normal((n_req, 4, 128)).astype(np.float32))
+    lens = np.full(n_req, 16, np.int32)
+    lens[-1] = mp * PAGE
+    got, cnt = _select(pool, b, q, lens, k, 3, 5)
+    vals, sc = _values(some)
+    score = np.zeros((1, 2, mp))
+    score[:, :, at] = ref.scores(q[-1:], vals[0], sc[0])
+    want, _ = ref.select(score, [mp * PAGE], k, 3, 5)
+    assert np.array_equal(got[-1], want[0]) and np.all(cnt[-1] == k)
+    assert np.all(cnt[:-1] == 1) and np.all(got[:-1, :, 0] == 0) and np.all(got[:-1, :, 1:] == -1)
+    # its last page, updated from a pool
+    bt = torch.full((n_req, mp), -1, dtype=torch.int32, device="cuda")
+    tags = torch.full((n_req, mp), 0xFF, dtype=torch.uint8, device="cuda")
+    bt[-1, -1], tags[-1, -1] = 63, 0
+    pool.fp8_view()[0, 63] = 0x22
+    pool.fp8_scales_view()[0, 63] = 0.5
+    frm, seq = np.zeros(n_req, np.int32), np.zeros(n_req, np.int32)
+    frm[-1], seq[-1] = mp * PAGE - 1, mp * PAGE
+    mk.kv_page_bounds_update(pool, 0, bt, tags, _gpu(frm), _gpu(seq), b)
+    torch.cuda.synchronize()
+    assert mk.kv_pool_check_errors(pool) == 0
+    assert torch.all(b.codes[0, -1, :, -1] == 0x22) and torch.all(b.scales[0, -1, :, -1] == 0.5)
+    assert not b.codes[0, :-1].any()
+
+
+def test_two_streams_and_two_graphs():
+    """Calls on two streams at once, each with its buffers, and two graphs over one workspace replayed
+    in turn: the answers of separate calls."""
+    import paper_2608_23834_amd as mk
+    torch = _torch()
+    w = _w(256, 24, 4, 2)
+    lens = [1900, 700]
+    t = _twin(w, lens)
+    rng = np.random.default_rng(31)
+    K, V = (wl.bf16_round(rng.standard_normal((sum(lens), 4, 256)).astype(np.float32)) for _ in range(2))
+    cu, zero, seq = (_gpu(np.array(x, np.int32)) for x in ([0, 1900, 2600], [0, 0], lens))
+    mk.kv_append_fp8(t.gpu, 0, t.bt, t.tags, zero, cu, _i16(K), _i16(V))
+    b = mk.PageBounds(t.gpu, 2, t.max_pages)
+    mk.kv_page_bounds_update(t.gpu, 0, t.bt, t.tags, zero, seq, b)
+    mk.paged_attn_set_deterministic(t.gpu, True)
+    q = [_i16(wl.bf16_round(rng.standard_normal((2, 24, 256)).astype(np.float32))) for _ in range(2)]
+
+    def buffers():
+        return (torch.zeros((2, 4, 16), dtype=torch.int32, device="cuda"), torch.zeros((2, 4), dtype=torch.int32, device="cuda"),
+                torch.zeros((2, 24, 256), device="cuda"), torch.zeros((2, 24), device="cuda"))
+
+    def spaces():
+        return mk.select_workspace(t.gpu, 2, t.max_pages), mk.workspace(t.gpu, 2, 16)
+
+    def call(x, to, ws, stream=None):
+        mk.paged_attn_select_pages(t.gpu, 0, x, seq, b, 1, 3, to[0], to[1], ws[0], stream=stream)
+        mk.paged_attn_decode_sparse(t.gpu, 0, x, t.bt, t.tags, seq, to[0], to[1], to[2], to[3], ws[1], stream=stream)
+    want, got = [buffers() for _ in q], [buffers() for _ in q]
+    for x, to in zip(q, want):
+        call(x, to, spaces())
+    assert not torch.equal(want[0][2], want[1][2])
+    own, side = [spaces() for _ in q], [torch.cuda.Stream() for _ in q]
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for i in range(2):
+            call(q[i], got[i], own[i], stream=side[i])
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert all(torch.equal(x, y) for x, y in zip(want[i], got[i])), i
+    graphs = []
+    for i in range(2):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=side[0]):
+            call(q[i], got[i], own[0])
+        graphs.append(g)
+    for _ in range(3):
+        for to in got:
+            for x in to:
+                x.zero_()
+        for g in graphs:
+            g.replay()
+        torch.cuda.synchronize()
+        for i in range(2):
+            assert all(torch.equal(x, y) for x, y in zip(want[i], got[i])), i
+    assert mk.kv_pool_check_errors(t.gpu) == 0
