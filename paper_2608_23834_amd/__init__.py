@@ -388,9 +388,8 @@ class Rope:
             pass
 
 
-def _rows(dev, t):
-    """Elements from one row [heads][d] of t to the next; the heads lie together."""
-    shape = t.shape
+def _rows(dev, t, shape):
+    """Elements from one row [heads][d] of t, of this shape, to the next; the heads lie together."""
     if t.get_device() != dev:
         raise ValueError("tensors are on the current device")
     if t.is_contiguous():
@@ -420,12 +419,13 @@ def kv_rope_apply(rope: Rope, x, positions, out, stream=None):
     """Rotate bf16 rows x [n][heads][head_dim] (int16 bits, tokens may be strided) into out;
     positions: int32 [n_axes][n]."""
     dev, cur = _current()
-    n, heads, d = x.shape
-    if out.shape != x.shape or d != rope.head_dim:
+    shape = x.shape
+    n, heads, d = shape
+    if out.shape != shape or d != rope.head_dim:
         raise ValueError("x and out are [n][heads][head_dim]")
     _check("kv_rope_apply", lib().kv_rope_apply(
-        rope.handle, n, heads, x.data_ptr(), _rows(dev, x), _positions(dev, rope, positions, n), out.data_ptr(),
-        _rows(dev, out), cur if stream is None else stream.cuda_stream))
+        rope.handle, n, heads, x.data_ptr(), _rows(dev, x, shape), _positions(dev, rope, positions, n), out.data_ptr(),
+        _rows(dev, out, shape), cur if stream is None else stream.cuda_stream))
 
 
 def kv_append_fp8_rope(pool: Pool, rope: Rope, layer, block_table, tags, seq_lens_before, cu_new_tokens,
@@ -434,15 +434,20 @@ def kv_append_fp8_rope(pool: Pool, rope: Rope, layer, block_table, tags, seq_len
     [n_layers][n][H][d], tokens may be strided; positions: int32 [n_axes][n] or None."""
     dev, cur = _current()
     n_req, max_pages = block_table.shape
-    n = k.shape[-3]
-    want = (n, pool.n_kv_heads, pool.d)
-    if k.shape != v.shape or k.shape != (want if layer >= 0 else (pool.n_layers, *want)):
+    shape = k.shape
+    ok = v.shape == shape
+    if layer >= 0:
+        ok = ok and len(shape) == 3
+    else:
+        ok = ok and len(shape) == 4 and shape[0] == pool.n_layers
+    if not ok or shape[-2] != pool.n_kv_heads or shape[-1] != pool.d:
         raise ValueError("k and v are [n][H][head_dim], with all layers [n_layers][n][H][head_dim]")
+    n = shape[-3]
     _here(dev, block_table, tags, seq_lens_before, cu_new_tokens)
     _check("kv_append_fp8_rope", lib().kv_append_fp8_rope(
         pool.handle, rope.handle, layer, n_req, block_table.data_ptr(), tags.data_ptr(), max_pages,
         seq_lens_before.data_ptr(), cu_new_tokens.data_ptr(), n, _positions(dev, rope, positions, n), k.data_ptr(),
-        _rows(dev, k), v.data_ptr(), _rows(dev, v), cur if stream is None else stream.cuda_stream))
+        _rows(dev, k, shape), v.data_ptr(), _rows(dev, v, shape), cur if stream is None else stream.cuda_stream))
 
 
 def paged_attn_decode_append_rope(pool: Pool, rope: Rope, layer, q, k_new, v_new, positions, block_table, tags,
