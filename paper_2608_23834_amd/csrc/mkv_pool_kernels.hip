@@ -449,9 +449,10 @@ __device__ __attribute__((noinline)) void rope_requant(uint8_t* reg, int n, floa
   }
 }
 
-template <int D, int V, bool NEAR>
+// cos_sin(t, j, q): cosine and sine of slot t, pair V j + q
+template <int D, int V, bool NEAR, class F>
 __device__ __forceinline__ void rope_quant_task(uint8_t* reg, float* sc, const uint8_t* rows, int64_t tstride,
-                                                const RopeView& R, const double2* tab, int t0, int t1, int lane) {
+                                                const RopeView& R, F cos_sin, int t0, int t1, int lane) {
   typedef typename RopeGroup<V>::type group;
   // LT lanes a token; a pass of the wave holds 64 / LT tokens, or (D = 256, V = 1) half of one
   constexpr int LT = D / (2 * V), NP = PAGE * LT / 64;
@@ -481,8 +482,7 @@ __device__ __forceinline__ void rope_quant_task(uint8_t* reg, float* sc, const u
     t = min(max(t, t0), t1 - 1);
     float x[2 * V];
     rope_unpack<V>(w[i], x);
-    const double2* tt = tab + t * m + j;
-    if (j < m / V) rope_turn<V, NEAR>(x, [&](int q) { return tt[q * (m / V)]; });
+    if (j < m / V) rope_turn<V, NEAR>(x, [&](int q) { return cos_sin(t, j, q); });
     rope_pack<V>(x, w[i]);
 #pragma unroll
     for (int b = 0; b < 2 * V; ++b) amax = fmaxf(amax, fabsf(x[b]));
@@ -541,7 +541,7 @@ __global__ __launch_bounds__(256, 4) void append_rope_quant_kernel(PoolView P, i
                                                                 RopeView R, const int32_t* pos) {
   extern __shared__ __align__(16) double2 s_tab[];  // [16][rot / 2]
   if (P.ctrl[CTRL_ABORT]) return;
-  const int H = P.n_kv_heads, LH = n_lcall * H, nb = (LH + hb - 1) / hb;
+  const int H = P.n_kv_heads, LH = n_lcall * H, nb = (LH + hb - 1) / hb, m = R.rot / 2;
   const int64_t n_units = (int64_t)P.ctrl[CTRL_NLIST] * nb;
   const int tid = threadIdx.x, lane = tid & 63, wid = __builtin_amdgcn_readfirstlane(tid >> 6);
   for (int64_t u = blockIdx.x; u < n_units; u += gridDim.x) {
@@ -559,9 +559,58 @@ __global__ __launch_bounds__(256, 4) void append_rope_quant_kernel(PoolView P, i
       uint8_t* reg = P.fp8 + ph * fp8_region_bytes(D);
       float* sc = P.fp8_scales + ph * 2;
       const uint8_t* rows = reinterpret_cast<const uint8_t*>(k + ((int64_t)li * n_new_total + row0) * kts + (int64_t)h * D);
-      rope_quant_task<D, V, NEAR>(reg, sc, rows, kts, R, s_tab, t0, t1, lane);
+      rope_quant_task<D, V, NEAR>(reg, sc, rows, kts, R,
+                                  [&](int t, int j, int q) { return s_tab[t * m + q * (m / V) + j]; }, t0, t1, lane);
       quant_task<D, true>(reg, sc, v + (int64_t)li * n_new_total * vts + (int64_t)h * D, row0, t0, t1, vts, lane);
     }
+  }
+}
+
+// The same with fewer than four (layer, head) pairs, which would leave waves of a workgroup
+// idle behind the page's angles: a wave takes one page of one pair, and its lanes evaluate the
+// angles of the channels that they turn themselves.  One, two and three pairs at d = 128 (320 K,
+// 160 K and 100 K tokens): 108, 90 and 82 us, with the angles in LDS 207, 127 and 91; at d = 256
+// (160 K and 80 K) 89 and 81 against 178 and 112; four pairs there 150 against 145, eight at
+// d = 128 161 against 138.
+template <int D, int V, bool NEAR>
+__global__ __launch_bounds__(256, 4) void append_rope_own_kernel(PoolView P, int layer_sel, int n_lcall,
+                                                                 const int32_t* sb, const int32_t* cu, int n_new_total,
+                                                                 const uint16_t* k, const uint16_t* v, int64_t kts,
+                                                                 int64_t vts, RopeView R, const int32_t* pos) {
+  constexpr int LT = D / (2 * V);
+  __shared__ int s_pos[4][ROPE_MAX_AXES * PAGE];  // per wave: [axis][slot]
+  static_assert(ROPE_MAX_AXES * PAGE == 64, "a lane each");
+  if (P.ctrl[CTRL_ABORT]) return;
+  const int H = P.n_kv_heads, LH = n_lcall * H, m = R.rot / 2;
+  const int64_t n_tasks = (int64_t)P.ctrl[CTRL_NLIST] * LH;
+  const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  for (int64_t u = (int64_t)blockIdx.x * 4 + wid; u < n_tasks; u += (int64_t)gridDim.x * 4) {
+    const int e = (int)(u / LH), lh = (int)(u - (int64_t)e * LH);
+    const int r = P.list[4 * e], p = P.list[4 * e + 1], id = P.list[4 * e + 2];
+    const int s0 = sb[r], n = cu[r + 1] - cu[r];
+    const int t0 = max(0, s0 - p * PAGE), t1 = min(PAGE, s0 + n - p * PAGE);
+    const int64_t row0 = (int64_t)cu[r] + (int64_t)p * PAGE - s0;  // input row of slot t is row0 + t
+    int at = p * PAGE + (lane & 15);
+    if (pos && (lane & 15) >= t0 && (lane & 15) < t1 && lane / 16 < R.n_axes)
+      at = pos[(int64_t)(lane / 16) * n_new_total + row0 + (lane & 15)];
+    s_pos[wid][lane] = at;  // (read by this wave alone)
+    __builtin_amdgcn_wave_barrier();
+    RopeEntry en[V];
+#pragma unroll
+    for (int q = 0; q < V; ++q) en[q] = R.tab[min(V * (lane % LT) + q, m - 1)];
+    const int li = lh / H, h = lh - li * H, layer = layer_sel < 0 ? li : layer_sel;
+    const int64_t ph = ((int64_t)layer * P.n_fp8 + id) * H + h;
+    uint8_t* reg = P.fp8 + ph * fp8_region_bytes(D);
+    float* sc = P.fp8_scales + ph * 2;
+    const uint8_t* rows = reinterpret_cast<const uint8_t*>(k + ((int64_t)li * n_new_total + row0) * kts + (int64_t)h * D);
+    rope_quant_task<D, V, NEAR>(reg, sc, rows, kts, R, [&](int t, int j, int q) {
+      const RopeEntry f = LT <= 64 ? en[q] : R.tab[V * j + q];  // (two passes a token: two entries a lane)
+      double2 cs;
+      rope_cos_sin((double)s_pos[wid][f.axis * PAGE + t] * f.freq, R.scale, cs.x, cs.y);
+      return cs;
+    }, t0, t1, lane);
+    __builtin_amdgcn_wave_barrier();
+    quant_task<D, true>(reg, sc, v + (int64_t)li * n_new_total * vts + (int64_t)h * D, row0, t0, t1, vts, lane);
   }
 }
 
@@ -2114,9 +2163,25 @@ hipError_t launch_append_rope(const PoolView& P, const RopeView& R, int layer, i
   }
   hipLaunchKernelGGL(append_plan_kernel, dim3(1), dim3(1024), 0, s, n_req, bt, tags, max_pages, sb,
                      cu, P.ctrl, P.fp8_stack, P.list, P.n_fp8, n_new_total, P.rc8);
+  const int64_t pages_bound = (int64_t)n_new_total / PAGE + n_req + 1, lh = (int64_t)n_lcall * P.n_kv_heads;
+  const int V = rope_width(R.rot);
+  if (lh < 4) {
+    const int og = grid_for((pages_bound * lh + 3) / 4, 4096);
+    auto own = [&](auto kern) {
+      hipLaunchKernelGGL(kern, dim3(og), dim3(256), 0, s, P, layer, n_lcall, sb, cu, n_new_total, k, v, kts, vts, R, pos);
+    };
+    if (P.d == 256)
+      V == 4   ? R.interleaved ? own(append_rope_own_kernel<256, 4, true>) : own(append_rope_own_kernel<256, 4, false>)
+      : V == 2 ? R.interleaved ? own(append_rope_own_kernel<256, 2, true>) : own(append_rope_own_kernel<256, 2, false>)
+      : R.interleaved ? own(append_rope_own_kernel<256, 1, true>) : own(append_rope_own_kernel<256, 1, false>);
+    else
+      V == 4   ? R.interleaved ? own(append_rope_own_kernel<128, 4, true>) : own(append_rope_own_kernel<128, 4, false>)
+      : V == 2 ? R.interleaved ? own(append_rope_own_kernel<128, 2, true>) : own(append_rope_own_kernel<128, 2, false>)
+      : R.interleaved ? own(append_rope_own_kernel<128, 1, true>) : own(append_rope_own_kernel<128, 1, false>);
+    return hipGetLastError();
+  }
   // (layer, head) pairs per workgroup: enough to spread the page's angles over, as long as
   // that leaves about four workgroups per CU
-  const int64_t pages_bound = (int64_t)n_new_total / PAGE + n_req + 1, lh = (int64_t)n_lcall * P.n_kv_heads;
   int64_t hb = pages_bound * lh / 1024 / 4 * 4;
   hb = hb < 4 ? 4 : hb > 32 ? 32 : hb;
   const int grid = grid_for(pages_bound * ((lh + hb - 1) / hb), 4096);
@@ -2126,7 +2191,6 @@ hipError_t launch_append_rope(const PoolView& P, const RopeView& R, int layer, i
     hipLaunchKernelGGL(kern, dim3(grid), dim3(256), lds, s, P, layer, n_lcall, hbi, sb, cu, n_new_total, k, v, kts,
                        vts, R, pos);
   };
-  const int V = rope_width(R.rot);
   if (P.d == 256)
     V == 4   ? R.interleaved ? go(append_rope_quant_kernel<256, 4, true>) : go(append_rope_quant_kernel<256, 4, false>)
     : V == 2 ? R.interleaved ? go(append_rope_quant_kernel<256, 2, true>) : go(append_rope_quant_kernel<256, 2, false>)

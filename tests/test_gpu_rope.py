@@ -269,29 +269,30 @@ def test_append_special_values(turned):
     assert np.array_equal(ta.gpu.fp8_scales.cpu().numpy().view(np.uint32), tb.gpu.fp8_scales.cpu().numpy().view(np.uint32))
 
 
+@pytest.mark.parametrize("hkv", [1, 2, 3, 5])
 @pytest.mark.parametrize("d,rot,inter", [(256, 64, False), (256, 20, True), (256, 22, False), (128, 128, True),
                                          (128, 36, False), (128, 126, True)])
-def test_append_grown_pages_of_any_magnitude(d, rot, inter):
+def test_append_grown_pages_of_any_magnitude(d, rot, inter, hkv):
     """Pages that three large calls fill in turn, with values from bf16's subnormals up, equal, a
     little larger or much larger from call to call: the pages of a rotation and a plain append."""
     import paper_2608_23834_amd as mk
     torch = _torch()
     rng = np.random.default_rng(d + rot)
-    n_req, w = 96, _w(d, 4, 2, 96)
+    n_req, w = 96, _w(d, 2 * hkv, hkv, 96)
     ta, tb = _twin(w, [64] * n_req, 1), _twin(w, [64] * n_req, 1)
-    rope, _, _ = _rope(d, rot, 1, inter)
-    mag = 2.0 ** rng.integers(-134, 4, (n_req, 1, 2, 1))
+    rope, _, _ = _rope(d, rot, 2, inter)
+    mag = 2.0 ** rng.integers(-134, 4, (n_req, 1, hkv, 1))
     at = np.zeros(n_req, np.int32)
     for call in range(3):
         c = rng.integers(1, 21, n_req)
         cu = np.r_[0, np.cumsum(c)].astype(np.int32)
         n, r = int(cu[-1]), np.repeat(np.arange(n_req), c)
         assert n > 512
-        f = rng.choice([0.25, 1.0, 1.0, 1.01, 8.0], (n_req, 1, 2, 1))
+        f = rng.choice([0.25, 1.0, 1.0, 1.01, 8.0], (n_req, 1, hkv, 1))
         mag = mag * f
-        base = np.sign(rng.standard_normal((n, 2, d))) * rng.choice([0.5, 1.0, 0.01], (n, 2, d))
+        base = np.sign(rng.standard_normal((n, hkv, d))) * rng.choice([0.5, 1.0, 0.01], (n, hkv, d))
         K, V = (wl.bf16_round((base * mag[r][:, 0]).astype(np.float32)) for _ in range(2))
-        pos = np.where(rng.random((1, n)) < 0.5, 0, rng.integers(0, 5000, (1, n))).astype(np.int32)
+        pos = np.where(rng.random((2, n)) < 0.5, 0, rng.integers(0, 5000, (2, n))).astype(np.int32)
         kg, vg, pg, sb, cug = _i16(K), _i16(V), _gpu(pos), _gpu(at), _gpu(cu)
         mk.kv_append_fp8_rope(ta.gpu, rope, 0, ta.bt, ta.tags, sb, cug, pg, kg, vg)
         mk.kv_rope_apply(rope, kg, pg, kg)
