@@ -282,8 +282,9 @@ mkv_status paged_attn_decode_append(mkv_pool* pool, int32_t layer, int32_t n_req
  *    x_stride elements from one token to the next (queries inside packed q/k/v
  *    rows, say), into out.  In place (out == x, same stride) is allowed, any other
  *    overlap of the two ranges is refused.  x and out: 8-byte aligned, strides a
- *    multiple of 4 and at least n_heads * head_dim (MKV_EINVAL otherwise).
- *    n_tokens = 0 does nothing. */
+ *    multiple of 4 and at least n_heads * head_dim (MKV_EINVAL otherwise), at most
+ *    2^31, and n_heads * head_dim at most 2^30 (MKV_ERANGE).  n_tokens = 0 does
+ *    nothing. */
 typedef struct kv_rope kv_rope; /* opaque host handle */
 typedef struct kv_rope_desc {
   int32_t head_dim;       /* 128 or 256 */
@@ -310,8 +311,8 @@ mkv_status kv_rope_apply(const kv_rope* rope, int32_t n_tokens, int32_t n_heads,
  * [n_new_total], or NULL: a token's place in the cache, seq_lens_before[r] + i, on
  * every axis.  Row i of k starts k_stride elements after row i - 1 (v likewise;
  * with MKV_ALL_LAYERS layer l's rows follow layer l - 1's); k and v 8-byte
- * aligned, strides a multiple of 4 and at least n_kv_heads * head_dim.
- * MKV_EINVAL also when the rope's head_dim is not the pool's. */
+ * aligned, strides a multiple of 4 and at least n_kv_heads * head_dim, at most 2^26
+ * (MKV_ERANGE).  MKV_EINVAL also when the rope's head_dim is not the pool's. */
 mkv_status kv_append_fp8_rope(mkv_pool* pool, const kv_rope* rope, int32_t layer, int32_t n_req,
                               int32_t* block_table, uint8_t* tags, int32_t max_pages,
                               const int32_t* seq_lens_before, const int32_t* cu_new_tokens,
@@ -367,7 +368,11 @@ mkv_status paged_attn_decode_append_rope(mkv_pool* pool, const kv_rope* rope, in
  *    that entry is left out.  Other errors, buffers and the order of sums as
  *    paged_attn_decode; ws >= paged_attn_workspace_bytes(pool, n_req, n_select, 0)
  *    (one for more pages serves too).  Outputs carry the error of fp32 arithmetic, as
- *    paged_attn_decode_append_rope's do. */
+ *    paged_attn_decode_append_rope's do.
+ *  - All of them: n_req up to 65,535, max_pages up to 262,144 (MKV_ERANGE), codes
+ *    16-byte aligned, buffers that are too small MKV_ENOMEM.  paged_attn_decode_cohort_key
+ *    does not cover these calls nor the rotating ones: a captured step of them also
+ *    bakes in n_select, n_first, n_last and the rope. */
 mkv_status kv_page_bounds_bytes(const mkv_pool* pool, int32_t n_req, int32_t max_pages,
                                 size_t* code_bytes, size_t* scale_bytes);
 mkv_status kv_page_bounds_update(mkv_pool* pool, int32_t layer, int32_t n_req,
