@@ -572,7 +572,10 @@ __global__ __launch_bounds__(256, 4) void append_rope_quant_kernel(PoolView P, i
 // 160 K and 100 K tokens): 108, 90 and 82 us, with the angles in LDS 207, 127 and 91; at d = 256
 // (160 K and 80 K) 89 and 81 against 178 and 112; four pairs there 150 against 145, eight at
 // d = 128 161 against 138.
-template <int D, int V, bool NEAR>
+// TAB, rotations of up to a quarter of the channels: most lanes would wait while a few evaluate
+// every angle, so the wave evaluates them together, into LDS of its own (two pairs at d = 256, 80 K
+// tokens, 20 and 64 channels: 74 and 77 us against 85 and 81; 64 channels at d = 128 115 against 107).
+template <int D, int V, bool NEAR, bool TAB>
 __global__ __launch_bounds__(256, 4) void append_rope_own_kernel(PoolView P, int layer_sel, int n_lcall,
                                                                  const int32_t* sb, const int32_t* cu, int n_new_total,
                                                                  const uint16_t* k, const uint16_t* v, int64_t kts,
@@ -580,6 +583,7 @@ __global__ __launch_bounds__(256, 4) void append_rope_own_kernel(PoolView P, int
   constexpr int LT = D / (2 * V);
   __shared__ int s_pos[4][ROPE_MAX_AXES * PAGE];  // per wave: [axis][slot]
   static_assert(ROPE_MAX_AXES * PAGE == 64, "a lane each");
+  extern __shared__ __align__(16) double2 s_tab[];  // TAB: per wave [16][rot / 2]
   if (P.ctrl[CTRL_ABORT]) return;
   const int H = P.n_kv_heads, LH = n_lcall * H, m = R.rot / 2;
   const int64_t n_tasks = (int64_t)P.ctrl[CTRL_NLIST] * LH;
@@ -596,14 +600,27 @@ __global__ __launch_bounds__(256, 4) void append_rope_own_kernel(PoolView P, int
     s_pos[wid][lane] = at;  // (read by this wave alone)
     __builtin_amdgcn_wave_barrier();
     RopeEntry en[V];
+    double2* tab = s_tab + wid * PAGE * m;
+    if constexpr (TAB) {
+      for (int it = t0 * m + lane; it < t1 * m; it += 64) {
+        const int t = it / m, i = it - t * m;
+        const RopeEntry f = R.tab[i];
+        double c, s;
+        rope_cos_sin((double)s_pos[wid][f.axis * PAGE + t] * f.freq, R.scale, c, s);
+        tab[t * m + (i % V) * (m / V) + i / V] = make_double2(c, s);
+      }
+      __builtin_amdgcn_wave_barrier();
+    } else {
 #pragma unroll
-    for (int q = 0; q < V; ++q) en[q] = R.tab[min(V * (lane % LT) + q, m - 1)];
+      for (int q = 0; q < V; ++q) en[q] = R.tab[min(V * (lane % LT) + q, m - 1)];
+    }
     const int li = lh / H, h = lh - li * H, layer = layer_sel < 0 ? li : layer_sel;
     const int64_t ph = ((int64_t)layer * P.n_fp8 + id) * H + h;
     uint8_t* reg = P.fp8 + ph * fp8_region_bytes(D);
     float* sc = P.fp8_scales + ph * 2;
     const uint8_t* rows = reinterpret_cast<const uint8_t*>(k + ((int64_t)li * n_new_total + row0) * kts + (int64_t)h * D);
     rope_quant_task<D, V, NEAR>(reg, sc, rows, kts, R, [&](int t, int j, int q) {
+      if constexpr (TAB) return tab[t * m + q * (m / V) + j];
       const RopeEntry f = LT <= 64 ? en[q] : R.tab[V * j + q];  // (two passes a token: two entries a lane)
       double2 cs;
       rope_cos_sin((double)s_pos[wid][f.axis * PAGE + t] * f.freq, R.scale, cs.x, cs.y);
@@ -2167,17 +2184,24 @@ hipError_t launch_append_rope(const PoolView& P, const RopeView& R, int layer, i
   const int V = rope_width(R.rot);
   if (lh < 4) {
     const int og = grid_for((pages_bound * lh + 3) / 4, 4096);
+    const bool tab = 4 * R.rot <= P.d;
+    const size_t own_lds = tab ? 4 * (size_t)PAGE * (R.rot / 2) * sizeof(double2) : 0;
     auto own = [&](auto kern) {
-      hipLaunchKernelGGL(kern, dim3(og), dim3(256), 0, s, P, layer, n_lcall, sb, cu, n_new_total, k, v, kts, vts, R, pos);
+      hipLaunchKernelGGL(kern, dim3(og), dim3(256), own_lds, s, P, layer, n_lcall, sb, cu, n_new_total, k, v, kts, vts,
+                         R, pos);
     };
-    if (P.d == 256)
-      V == 4   ? R.interleaved ? own(append_rope_own_kernel<256, 4, true>) : own(append_rope_own_kernel<256, 4, false>)
-      : V == 2 ? R.interleaved ? own(append_rope_own_kernel<256, 2, true>) : own(append_rope_own_kernel<256, 2, false>)
-      : R.interleaved ? own(append_rope_own_kernel<256, 1, true>) : own(append_rope_own_kernel<256, 1, false>);
-    else
-      V == 4   ? R.interleaved ? own(append_rope_own_kernel<128, 4, true>) : own(append_rope_own_kernel<128, 4, false>)
-      : V == 2 ? R.interleaved ? own(append_rope_own_kernel<128, 2, true>) : own(append_rope_own_kernel<128, 2, false>)
-      : R.interleaved ? own(append_rope_own_kernel<128, 1, true>) : own(append_rope_own_kernel<128, 1, false>);
+    auto pick = [&](auto dc, auto vc) {
+      constexpr int DD = decltype(dc)::value, VV = decltype(vc)::value;
+      if (tab)
+        R.interleaved ? own(append_rope_own_kernel<DD, VV, true, true>) : own(append_rope_own_kernel<DD, VV, false, true>);
+      else
+        R.interleaved ? own(append_rope_own_kernel<DD, VV, true, false>) : own(append_rope_own_kernel<DD, VV, false, false>);
+    };
+    auto of_v = [&](auto dc) {
+      V == 4   ? pick(dc, std::integral_constant<int, 4>{})
+      : V == 2 ? pick(dc, std::integral_constant<int, 2>{}) : pick(dc, std::integral_constant<int, 1>{});
+    };
+    P.d == 256 ? of_v(std::integral_constant<int, 256>{}) : of_v(std::integral_constant<int, 128>{});
     return hipGetLastError();
   }
   // (layer, head) pairs per workgroup: enough to spread the page's angles over, as long as

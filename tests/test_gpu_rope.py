@@ -271,7 +271,8 @@ def test_append_special_values(turned):
 
 @pytest.mark.parametrize("hkv", [1, 2, 3, 5])
 @pytest.mark.parametrize("d,rot,inter", [(256, 64, False), (256, 20, True), (256, 22, False), (128, 128, True),
-                                         (128, 36, False), (128, 126, True)])
+                                         (128, 36, False), (128, 126, True), (256, 256, False), (256, 100, True),
+                                         (256, 250, False), (128, 32, False), (128, 12, True), (128, 6, False)])
 def test_append_grown_pages_of_any_magnitude(d, rot, inter, hkv):
     """Pages that three large calls fill in turn, with values from bf16's subnormals up, equal, a
     little larger or much larger from call to call: the pages of a rotation and a plain append."""
