@@ -364,8 +364,8 @@ mkv_status paged_attn_decode_append_rope(mkv_pool* pool, const kv_rope* rope, in
  *    (tokens below seq_lens[r]): pages [n_req][n_kv_heads][n_select], strictly
  *    ascending, counts of them.  A count of 0 gives zero outputs and lse = -inf.  A
  *    count outside [0, n_select]: RANGE and zero outputs for that KV head's queries;
- *    an entry that is not above the one before it, or past the sequence's end: RANGE,
- *    that entry is left out.  Other errors, buffers and the order of sums as
+ *    an entry that is negative, not above the one before it (left out or not), or past the
+ *    sequence's end: RANGE, that entry is left out.  Other errors, buffers and the order of sums as
  *    paged_attn_decode; ws >= paged_attn_workspace_bytes(pool, n_req, n_select, 0)
  *    (one for more pages serves too).  Outputs carry the error of fp32 arithmetic, as
  *    paged_attn_decode_append_rope's do.

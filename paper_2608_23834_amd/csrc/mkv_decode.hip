@@ -645,8 +645,8 @@ __global__ __launch_bounds__(DecodeCfg<PAIR>::NT, PAIR && D == 128 ? 4 : 2) void
       tg = TAG_R;
       if (id < 0) id = 0;  // fresh: placeholder until the append wave has popped the id
     }
-    if (SPARSE && pi < n_pg && !(up_w[k] && pg_lp[k] < (S + PAGE - 1) / PAGE)) {
-      // not above the entry before it, or past the end: left out
+    if (SPARSE && pi < n_pg && !(up_w[k] && pg_lp[k] >= 0 && pg_lp[k] < (S + PAGE - 1) / PAGE)) {
+      // not above the entry before it (which may itself be left out), negative, or past the end: left out
       if (wid == 0) atomicOr(&P.ctrl[CTRL_ERR], (int)MKV_DEVERR_RANGE);
       tg = -2;
     }
