@@ -192,6 +192,10 @@ constexpr float SCORE_ERR = 448.0f * 0x1p-16f;
 // Where products are subnormal or a subnormal query entry counts as 0: at most 448 * 2^-126
 // of each of 256 channels, 2^-109, over s_p; and 2^-126 for the product with s_p itself.
 constexpr float SCORE_SUB = 0x1p-109f;
+// Both hold as long as no sum leaves fp32's range: 448 sum |q| below 2^127.  Past that a head's
+// score may be an infinity or a NaN, which the maximum over the heads hides, where its true
+// score is neither.
+constexpr float SCORE_TOP = 0x1p118f;
 
 // Step 1: one wave per 16 pages and step of the grid.  A: lane (page l % 16, group l / 16)
 // loads 16 bytes of every 64 of its page's row; B: the same channels of head l % 16, in
@@ -465,14 +469,15 @@ __global__ __launch_bounds__(SEL_NT) void select_pick_kernel(int H, int G, const
     }
     const float E2 = 2.0f * (SCORE_ERR * l1 + SCORE_SUB) * sm + 0x1p-125f;
     // ---- 2. the bin of the need-th largest.  A range without a finite width, or of one at
-    // which bin() would lose its bits to the subnormals, or an error without one, leaves
-    // every page open
+    // which bin() would lose its bits to the subnormals, an error without one, or a query whose
+    // products may leave fp32's range leaves every page open
     const float width = mx - mn;
-    const bool bins = width > 0x1p-100f && width < INFINITY && E2 < INFINITY;
+    const bool bins = width > 0x1p-100f && width < INFINITY && E2 < INFINITY && l1 < SCORE_TOP;
     const float inv = bins ? (float)(SEL_BINS - 1) / width : 0.0f;
     auto bin = [&](float a) { return bins ? min(max((int)((a - mn) * inv), 0), SEL_BINS - 1) : 0; };
     float lo = -INFINITY;
-    if ((l1 == 0.0f || sm == 0.0f) && mn == mx && !nan) {  // a query or scales of zeros: every score is 0
+    // a query or scales of zeros: every score is 0
+    if ((l1 == 0.0f || sm == 0.0f) && l1 < SCORE_TOP && mn == mx && !nan) {
       lowest = need;
       lo = INFINITY;
     }

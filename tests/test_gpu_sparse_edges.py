@@ -37,3 +37,52 @@ def test_negative_entries_are_left_out():
             heads = slice(8 * h, 8 * h + 8)
             assert not got[0][r, heads].any() and np.all(got[1][r, heads] == -np.inf), entries
         sp._close(got, want)
+
+
+@pytest.mark.parametrize("top", [120, 117])
+def test_selection_of_queries_that_overflow_fp32(top):
+    """A head whose products leave fp32's range both ways (its fp32 sum is a NaN or an infinity, its true
+    score is neither) beside one whose scores are finite and spread widely: the choice is the fp64 scores'."""
+    import paper_2608_23834_amd as mk
+    rng = np.random.default_rng(top)
+    pool = mk.Pool(1, 2, 1, 128, 1, 1, 64, np.ones(128, np.int8))
+    n = 400
+    b = mk.PageBounds(pool, 1, n)
+    big = rng.integers(0x78, 0x7F, (n, 2)).astype(np.uint8)  # E4M3 256 .. 448
+    codes = np.zeros(b.codes.shape, np.uint8)
+    codes[0, 0, 0, :, :, :64] = big[:, None, :1]
+    codes[0, 0, 0, :, :, 64:] = 0x80 | big[:, None, 1:]
+    b.codes.copy_(sp._gpu(codes))
+    b.scales.fill_(1.0)
+    q = np.zeros((1, 2, 128), np.float32)
+    q[0, 0] = 2.0 ** top
+    q[0, 1, :64] = 2.0 ** 112
+    q = wl.bf16_round(q)
+    vals, sc = sp._values(b)
+    score = ref.scores(q, vals[0], sc[0])
+    assert np.isfinite(score).all()
+    for k, first, last in ((20, 0, 0), (130, 2, 3)):
+        want, cnt = ref.select(score, [n * PAGE], k, first, last)
+        got, gc = sp._select(pool, b, q, [n * PAGE], k, first, last)
+        assert np.array_equal(gc, cnt) and np.array_equal(got, want)
+
+
+def test_selection_of_zero_scales_and_infinite_queries():
+    """Scales of zero with an infinite query entry: a page where that entry meets a zero code, or where
+    the product with the scale is inf * 0, has a NaN for a score and comes after the zeros."""
+    import paper_2608_23834_amd as mk
+    rng = np.random.default_rng(4)
+    pool = mk.Pool(1, 2, 1, 128, 1, 1, 64, np.ones(128, np.int8))
+    b = sp._random_bounds(rng, pool, 1, 200)
+    codes = b.codes.cpu().numpy()
+    codes[0, 0, 0, :, :, 7] = np.where(rng.random((200, 1)) < 0.5, 0x00, 0xB8)  # 0 or -1
+    b.codes.copy_(sp._gpu(codes))
+    b.scales.zero_()
+    q = wl.bf16_round(rng.standard_normal((1, 2, 128)).astype(np.float32))
+    q[0, 0, 7] = 0x7F80
+    vals, sc = sp._values(b)
+    score = ref.scores(q, vals[0], sc[0])
+    assert np.isnan(score).any() and (score == 0).any()
+    want, _ = ref.select(score, [3200], 30, 0, 0)
+    got, _ = sp._select(pool, b, q, [3200], 30, 0, 0)
+    assert np.array_equal(got, want)
