@@ -398,8 +398,9 @@ def _rows(dev, t, shape):
     st = t.stride()
     if st[-1] != 1 or (heads > 1 and st[-2] != d):
         raise ValueError("rows are [heads][head_dim] without gaps")
-    stride = st[-3] if n > 1 else heads * d
-    if len(shape) == 4 and shape[0] > 1 and st[0] != n * stride:
+    layers = shape[0] if len(shape) == 4 else 1
+    stride = st[-3] if n > 1 else st[0] if layers > 1 else heads * d
+    if layers > 1 and st[0] != n * stride:
         raise ValueError("one layer's rows follow the other's")
     return stride
 
