@@ -481,7 +481,14 @@ class PageBounds:
         self.scales = torch.zeros(shape, dtype=torch.float32, device=device)
         assert self.codes.numel() == c.value and self.scales.numel() * 4 == s.value
 
-        self._args = (self.codes.data_ptr(), c.value, self.scales.data_ptr(), s.value)
+
+def _bounds(dev, b):
+    """The tensors that b holds now, as the library takes them (it checks their sizes)."""
+    codes, scales = b.codes, b.scales
+    if (codes.get_device() != dev or scales.get_device() != dev or not codes.is_contiguous() or not scales.is_contiguous()
+            or codes.element_size() != 1 or scales.element_size() != 4):
+        raise ValueError("bounds are contiguous codes of a byte and float32 scales on the current device")
+    return codes.data_ptr(), codes.numel(), scales.data_ptr(), 4 * scales.numel()
 
 
 def kv_page_bounds_update(pool: Pool, layer, block_table, tags, seq_lens_from, seq_lens, bounds: PageBounds,
@@ -491,10 +498,10 @@ def kv_page_bounds_update(pool: Pool, layer, block_table, tags, seq_lens_from, s
     n_req, max_pages = block_table.shape
     if n_req != bounds.n_req or max_pages != bounds.max_pages:
         raise ValueError("the bounds are those of another table shape")
-    _here(dev, block_table, tags, seq_lens_from, seq_lens, bounds.codes)
+    _here(dev, block_table, tags, seq_lens_from, seq_lens)
     _check("kv_page_bounds_update", lib().kv_page_bounds_update(
         pool.handle, layer, n_req, block_table.data_ptr(), tags.data_ptr(), max_pages, seq_lens_from.data_ptr(),
-        seq_lens.data_ptr(), *bounds._args, cur if stream is None else stream.cuda_stream))
+        seq_lens.data_ptr(), *_bounds(dev, bounds), cur if stream is None else stream.cuda_stream))
 
 
 def select_workspace(pool: Pool, n_req, max_pages, device="cuda"):
@@ -513,9 +520,9 @@ def paged_attn_select_pages(pool: Pool, layer, q, seq_lens, bounds: PageBounds, 
     n_req, H, n_select = pages.shape
     if n_req != bounds.n_req or H != pool.n_kv_heads or counts.shape != (n_req, H):
         raise ValueError("pages are [n_req][H][n_select], counts [n_req][H]")
-    _here(dev, q, seq_lens, bounds.codes, pages, counts, ws)
+    _here(dev, q, seq_lens, pages, counts, ws)
     _check("paged_attn_select_pages", lib().paged_attn_select_pages(
-        pool.handle, layer, n_req, q.data_ptr(), seq_lens.data_ptr(), bounds.max_pages, *bounds._args, n_select,
+        pool.handle, layer, n_req, q.data_ptr(), seq_lens.data_ptr(), bounds.max_pages, *_bounds(dev, bounds), n_select,
         n_first, n_last, pages.data_ptr(), counts.data_ptr(), ws.data_ptr(), ws.nbytes,
         cur if stream is None else stream.cuda_stream))
 
