@@ -8,6 +8,7 @@ built library is missing, loading fails loudly.
 from __future__ import annotations
 
 import ctypes
+import math
 import os
 
 import numpy as np
@@ -166,11 +167,43 @@ def _stream(stream=None):
     return _current()[1] if stream is None else stream.cuda_stream
 
 
+def _types():
+    """Types that (rows of bf16 bits, int32, float32) may come as; the first call loads torch."""
+    global _types
+    import torch
+    t = (torch.int16, torch.bfloat16, torch.uint16), (torch.int32,), (torch.float32,)
+
+    def _types():
+        return t
+    return t
+
+
 def _here(dev, *tensors):
     """Every tensor (None aside) lies on device dev, without gaps."""
     for t in tensors:
         if t is not None and (t.get_device() != dev or not t.is_contiguous()):
             raise ValueError("tensors are contiguous and on the current device")
+
+
+_WRONG_TYPE = "rows are bf16 (or its bits in int16), lengths and pages int32, out and lse float32"
+
+
+def _sizes(*pairs):
+    """(tensor, shape): of the shape, for more requests, or as many elements or more in fewer axes."""
+    for t, want in pairs:
+        s = t.shape
+        if s != want and (t.numel() < math.prod(want) or len(s) >= len(want) and s[-len(want) + 1:] != want[1:]):
+            raise ValueError(f"{want} is wanted, not {tuple(s)}")
+
+
+def _table(dev, pool, block_table, tags, i32):
+    n_req, max_pages = block_table.shape
+    if (block_table.dtype not in i32 or tags.element_size() != 1 or tags.numel() < n_req * max_pages
+            or not block_table.is_contiguous() or not tags.is_contiguous() or block_table.get_device() != dev
+            or tags.get_device() != dev or pool.device != dev):
+        raise ValueError("block_table int32 and tags uint8 are [n_req][max_pages], contiguous and with the pool on the "
+                         "current device")
+    return n_req, max_pages
 
 
 def pool_bytes(n_layers, n_q_heads, n_kv_heads, head_dim, n_fp8_pages, n_tq3_pages, recent_tokens):
@@ -197,6 +230,7 @@ class Pool:
         self.fp8_scales = torch.zeros(bs // 4, dtype=torch.float32, device=device)
         self.tq3 = torch.zeros(max(b3, 16), dtype=torch.uint8, device=device)
         self.ctrl = torch.zeros(bc // 4, dtype=torch.int32, device=device)
+        self.device = self.ctrl.get_device()
         sig = np.ascontiguousarray(rot_signs, dtype=np.int8)
         o8 = None if fp8_order is None else np.ascontiguousarray(fp8_order, dtype=np.int32)
         o3 = None if tq3_order is None else np.ascontiguousarray(tq3_order, dtype=np.int32)
@@ -390,8 +424,8 @@ class Rope:
 
 def _rows(dev, t, shape):
     """Elements from one row [heads][d] of t, of this shape, to the next; the heads lie together."""
-    if t.get_device() != dev:
-        raise ValueError("tensors are on the current device")
+    if t.get_device() != dev or t.dtype not in _types()[0]:
+        raise ValueError("rows are bf16 (or its bits in int16) on the current device")
     if t.is_contiguous():
         return shape[-2] * shape[-1]
     n, heads, d = shape[-3:]
@@ -410,7 +444,7 @@ def _positions(dev, rope, positions, n):
         raise ValueError("the rope's table is on another device")
     if positions is None:
         return None
-    if (positions.shape != (rope.n_axes, n) or positions.get_device() != dev or positions.element_size() != 4
+    if (positions.shape != (rope.n_axes, n) or positions.get_device() != dev or positions.dtype not in _types()[1]
             or not positions.is_contiguous()):
         raise ValueError(f"positions are contiguous int32 [{rope.n_axes}][{n}] on the current device")
     return positions.data_ptr()
@@ -434,7 +468,8 @@ def kv_append_fp8_rope(pool: Pool, rope: Rope, layer, block_table, tags, seq_len
     """kv_append_fp8 with the keys rotated on the way; k, v: [n][H][d] of one layer or
     [n_layers][n][H][d], tokens may be strided; positions: int32 [n_axes][n] or None."""
     dev, cur = _current()
-    n_req, max_pages = block_table.shape
+    i32 = _types()[1]
+    n_req, max_pages = _table(dev, pool, block_table, tags, i32)
     shape = k.shape
     ok = v.shape == shape
     if layer >= 0:
@@ -444,7 +479,11 @@ def kv_append_fp8_rope(pool: Pool, rope: Rope, layer, block_table, tags, seq_len
     if not ok or shape[-2] != pool.n_kv_heads or shape[-1] != pool.d:
         raise ValueError("k and v are [n][H][head_dim], with all layers [n_layers][n][H][head_dim]")
     n = shape[-3]
-    _here(dev, block_table, tags, seq_lens_before, cu_new_tokens)
+    _here(dev, seq_lens_before, cu_new_tokens)
+    if not (seq_lens_before.dtype in i32 and cu_new_tokens.dtype in i32):
+        raise ValueError(_WRONG_TYPE)
+    if seq_lens_before.numel() < n_req or cu_new_tokens.numel() <= n_req:
+        raise ValueError("seq_lens_before is [n_req], cu_new_tokens [n_req + 1]")
     _check("kv_append_fp8_rope", lib().kv_append_fp8_rope(
         pool.handle, rope.handle, layer, n_req, block_table.data_ptr(), tags.data_ptr(), max_pages,
         seq_lens_before.data_ptr(), cu_new_tokens.data_ptr(), n, _positions(dev, rope, positions, n), k.data_ptr(),
@@ -456,8 +495,17 @@ def paged_attn_decode_append_rope(pool: Pool, rope: Rope, layer, q, k_new, v_new
     """paged_attn_decode_append with q and k_new rotated in the launch; positions: int32
     [n_axes][n_req] or None (the token's place in the cache)."""
     dev, cur = _current()
-    n_req, max_pages = block_table.shape
-    _here(dev, q, k_new, v_new, block_table, tags, seq_lens_before, out, lse, ws)
+    rows, i32, f32 = _types()
+    n_req, max_pages = _table(dev, pool, block_table, tags, i32)
+    _here(dev, q, k_new, v_new, seq_lens_before, out, lse, ws)
+    if not (q.dtype in rows and k_new.dtype in rows and v_new.dtype in rows and seq_lens_before.dtype in i32
+            and out.dtype in f32 and (lse is None or lse.dtype in f32)):
+        raise ValueError(_WRONG_TYPE)
+    qs, ks = (n_req, pool.n_q_heads, pool.d), (n_req, pool.n_kv_heads, pool.d)
+    if q.shape != qs or out.shape != qs or k_new.shape != ks or v_new.shape != ks:
+        _sizes((q, qs), (out, qs), (k_new, ks), (v_new, ks))
+    if seq_lens_before.numel() < n_req or (lse is not None and lse.numel() < qs[0] * qs[1]):
+        raise ValueError("seq_lens_before is [n_req], lse [n_req][n_q_heads]")
     _check("paged_attn_decode_append_rope", lib().paged_attn_decode_append_rope(
         pool.handle, rope.handle, layer, n_req, q.data_ptr(), k_new.data_ptr(), v_new.data_ptr(),
         _positions(dev, rope, positions, n_req), block_table.data_ptr(), tags.data_ptr(), max_pages,
@@ -486,7 +534,7 @@ def _bounds(dev, b):
     """The tensors that b holds now, as the library takes them (it checks their sizes)."""
     codes, scales = b.codes, b.scales
     if (codes.get_device() != dev or scales.get_device() != dev or not codes.is_contiguous() or not scales.is_contiguous()
-            or codes.element_size() != 1 or scales.element_size() != 4):
+            or codes.element_size() != 1 or scales.dtype not in _types()[2]):
         raise ValueError("bounds are contiguous codes of a byte and float32 scales on the current device")
     return codes.data_ptr(), codes.numel(), scales.data_ptr(), 4 * scales.numel()
 
@@ -495,10 +543,15 @@ def kv_page_bounds_update(pool: Pool, layer, block_table, tags, seq_lens_from, s
                           stream=None):
     """Recompute the bounds of the pages that hold tokens [seq_lens_from, seq_lens)."""
     dev, cur = _current()
-    n_req, max_pages = block_table.shape
+    i32 = _types()[1]
+    n_req, max_pages = _table(dev, pool, block_table, tags, i32)
     if n_req != bounds.n_req or max_pages != bounds.max_pages:
         raise ValueError("the bounds are those of another table shape")
-    _here(dev, block_table, tags, seq_lens_from, seq_lens)
+    _here(dev, seq_lens_from, seq_lens)
+    if not (seq_lens_from.dtype in i32 and seq_lens.dtype in i32):
+        raise ValueError(_WRONG_TYPE)
+    if seq_lens_from.numel() < n_req or seq_lens.numel() < n_req:
+        raise ValueError("seq_lens_from and seq_lens are [n_req]")
     _check("kv_page_bounds_update", lib().kv_page_bounds_update(
         pool.handle, layer, n_req, block_table.data_ptr(), tags.data_ptr(), max_pages, seq_lens_from.data_ptr(),
         seq_lens.data_ptr(), *_bounds(dev, bounds), cur if stream is None else stream.cuda_stream))
@@ -520,7 +573,15 @@ def paged_attn_select_pages(pool: Pool, layer, q, seq_lens, bounds: PageBounds, 
     n_req, H, n_select = pages.shape
     if n_req != bounds.n_req or H != pool.n_kv_heads or counts.shape != (n_req, H):
         raise ValueError("pages are [n_req][H][n_select], counts [n_req][H]")
+    rows, i32, _ = _types()
     _here(dev, q, seq_lens, pages, counts, ws)
+    if not (q.dtype in rows and seq_lens.dtype in i32 and pages.dtype in i32 and counts.dtype in i32):
+        raise ValueError(_WRONG_TYPE)
+    qs = (n_req, pool.n_q_heads, pool.d)
+    if q.shape != qs:
+        _sizes((q, qs))
+    if seq_lens.numel() < n_req or pool.device != dev:
+        raise ValueError("seq_lens is [n_req], the pool on the current device")
     _check("paged_attn_select_pages", lib().paged_attn_select_pages(
         pool.handle, layer, n_req, q.data_ptr(), seq_lens.data_ptr(), bounds.max_pages, *_bounds(dev, bounds), n_select,
         n_first, n_last, pages.data_ptr(), counts.data_ptr(), ws.data_ptr(), ws.nbytes,
@@ -531,10 +592,19 @@ def paged_attn_decode_sparse(pool: Pool, layer, q, block_table, tags, seq_lens, 
                              stream=None):
     """paged_attn_decode over the listed logical pages of each request and KV head."""
     dev, cur = _current()
-    n_req, max_pages = block_table.shape
+    rows, i32, f32 = _types()
+    n_req, max_pages = _table(dev, pool, block_table, tags, i32)
     if pages.dim() != 3 or counts.shape != (n_req, pool.n_kv_heads) or pages.shape[:2] != counts.shape:
         raise ValueError("pages are [n_req][H][n_select], counts [n_req][H]")
-    _here(dev, q, block_table, tags, seq_lens, pages, counts, out, lse, ws)
+    _here(dev, q, seq_lens, pages, counts, out, lse, ws)
+    if not (q.dtype in rows and seq_lens.dtype in i32 and pages.dtype in i32 and counts.dtype in i32
+            and out.dtype in f32 and (lse is None or lse.dtype in f32)):
+        raise ValueError(_WRONG_TYPE)
+    qs = (n_req, pool.n_q_heads, pool.d)
+    if q.shape != qs or out.shape != qs:
+        _sizes((q, qs), (out, qs))
+    if seq_lens.numel() < n_req or (lse is not None and lse.numel() < qs[0] * qs[1]):
+        raise ValueError("seq_lens is [n_req], lse [n_req][n_q_heads]")
     _check("paged_attn_decode_sparse", lib().paged_attn_decode_sparse(
         pool.handle, layer, n_req, q.data_ptr(), block_table.data_ptr(), tags.data_ptr(), max_pages,
         seq_lens.data_ptr(), pages.shape[2], pages.data_ptr(), counts.data_ptr(), out.data_ptr(), _ptr(lse),

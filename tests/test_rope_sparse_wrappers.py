@@ -39,7 +39,7 @@ def rec(monkeypatch):
 
 def _pool(layers=1):
     return types.SimpleNamespace(handle=1, n_layers=layers, n_q_heads=HQ, n_kv_heads=H, d=D,
-                                 ctrl=torch.zeros(4, dtype=torch.int32))
+                                 device=-1)
 
 
 def _rope(axes=1):
@@ -113,3 +113,118 @@ def test_bounds_are_the_tensors_they_hold_now(rec):
     b.codes, b.scales = old[0][:, :1], old[1][:, :1]  # fewer than the library asks for: it has the true sizes
     _update(b)
     assert rec.calls[0][1][8:12] == (old[0].data_ptr(), old[0].numel() // 2, old[1].data_ptr(), 2 * old[1].numel())
+
+
+# ---------------------------------------------------------------- what is refused
+
+N, K, MP = 3, 5, 4
+BF16, F16, F32, F64, I64, U8 = torch.bfloat16, torch.float16, torch.float32, torch.float64, torch.int64, torch.uint8
+
+
+def _good(name):
+    """(call, its arguments) of a call that is taken."""
+    table = _table(N)
+    f32 = lambda *s: torch.zeros(s)  # noqa: E731
+    ws = torch.zeros(64, dtype=U8)
+    if name == "apply":
+        return mk.kv_rope_apply, dict(rope=_rope(2), x=_i16(N, HQ, D), positions=_i32(2, N), out=_i16(N, HQ, D))
+    if name == "append":
+        return mk.kv_append_fp8_rope, dict(pool=_pool(), rope=_rope(2), layer=0, **table, seq_lens_before=_i32(N),
+                                           cu_new_tokens=_i32(N + 1), positions=_i32(2, 7), k=_i16(7, H, D), v=_i16(7, H, D))
+    if name == "step":
+        return mk.paged_attn_decode_append_rope, dict(
+            pool=_pool(), rope=_rope(2), layer=0, q=_i16(N, HQ, D), k_new=_i16(N, H, D), v_new=_i16(N, H, D),
+            positions=_i32(2, N), **table, seq_lens_before=_i32(N), out=f32(N, HQ, D), lse=f32(N, HQ), ws=ws)
+    b = mk.PageBounds(_pool(), N, MP, device="cpu")
+    if name == "bounds":
+        return mk.kv_page_bounds_update, dict(pool=_pool(), layer=0, **table, seq_lens_from=_i32(N), seq_lens=_i32(N), bounds=b)
+    if name == "select":
+        return mk.paged_attn_select_pages, dict(pool=_pool(), layer=0, q=_i16(N, HQ, D), seq_lens=_i32(N), bounds=b, n_first=1,
+                                                n_last=1, pages=_i32(N, H, K), counts=_i32(N, H), ws=ws)
+    return mk.paged_attn_decode_sparse, dict(pool=_pool(), layer=0, q=_i16(N, HQ, D), **table, seq_lens=_i32(N),
+                                             pages=_i32(N, H, K), counts=_i32(N, H), out=f32(N, HQ, D), lse=f32(N, HQ), ws=ws)
+
+
+CALLS = ("apply", "append", "step", "bounds", "select", "sparse")
+
+
+@pytest.mark.parametrize("name", CALLS)
+def test_good_calls_are_taken(rec, name):
+    call, a = _good(name)
+    call(**a)
+    assert len(rec.calls) == 1
+    # bf16 tensors are rows as their bits are; more requests' room than there are requests is fine
+    more = {"q": _i16(N + 2, HQ, D).view(BF16), "out": torch.zeros(N + 2, HQ, D), "lse": torch.zeros(N + 2, HQ),
+            "seq_lens": _i32(N + 2), "seq_lens_before": _i32(N + 2), "seq_lens_from": _i32(N + 2), "cu_new_tokens": _i32(N + 9),
+            "k_new": _i16(N, H * D).view(BF16), "v_new": _i16(N * H * D)}
+    if name == "apply":
+        more = {"x": a["x"].view(BF16), "out": _i16(N, HQ, D).view(torch.uint16)}
+    call(**{**a, **{k: v for k, v in more.items() if k in a}})
+    if "lse" in a:
+        call(**{**a, "lse": None})
+    assert len(rec.calls) == (3 if "lse" in a else 2)
+
+
+def _short(t):
+    return t.flatten()[:-1]
+
+
+@pytest.mark.parametrize("name", CALLS)
+def test_wrong_types_are_refused(rec, name):
+    """Element types that the kernels would read as others, each argument for itself."""
+    call, good = _good(name)
+    for key, t in good.items():
+        if not isinstance(t, torch.Tensor) or key == "ws":
+            continue
+        bad = {torch.int16: (F32, F16, U8, torch.int32), torch.int32: (F32, I64, torch.int16), U8: (torch.int32, torch.int16),
+               F32: (F64, F16, torch.int32)}[t.dtype]
+        for dtype in bad:
+            with pytest.raises(ValueError):
+                call(**{**good, key: t.to(dtype)})
+            assert not rec.calls, (key, dtype)
+
+
+@pytest.mark.parametrize("name", CALLS)
+def test_short_tensors_are_refused(rec, name):
+    """Tensors of fewer elements than the kernels read or write."""
+    call, good = _good(name)
+    for key, t in good.items():
+        if not isinstance(t, torch.Tensor) or key in ("ws", "block_table"):
+            continue
+        with pytest.raises(ValueError):
+            call(**{**good, key: _short(t)})
+        assert not rec.calls, key
+
+
+@pytest.mark.parametrize("name", CALLS)
+def test_gaps_and_other_cards_are_refused(rec, name, monkeypatch):
+    call, good = _good(name)
+    for key, t in good.items():
+        if not isinstance(t, torch.Tensor) or (name, key) in (("apply", "x"), ("apply", "out")) or key in ("k", "v"):
+            continue
+        wide = torch.zeros((*t.shape[:-1], 2 * t.shape[-1]), dtype=t.dtype)[..., ::2]
+        with pytest.raises(ValueError):
+            call(**{**good, key: wide})
+        assert not rec.calls, key
+    if "pool" in good:  # the pool on another card than the current one
+        far = _pool()
+        far.device = 1
+        with pytest.raises(ValueError):
+            call(**{**good, "pool": far})
+    monkeypatch.setattr(mk, "_current", lambda: (0, 0))
+    with pytest.raises(ValueError):  # (the tensors are not on card 0)
+        call(**good)
+    assert not rec.calls
+
+
+@pytest.mark.parametrize("name,heads", [("step", HQ), ("select", HQ), ("sparse", HQ)])
+def test_wrong_heads_are_refused(rec, name, heads):
+    """Three axes of another head count or head dim than the pool's, also where that is more."""
+    call, good = _good(name)
+    for key in ("q", "k_new", "v_new", "out"):
+        if key in good:
+            n, h, d = good[key].shape
+            for shape in ((n, 2 * h, d), (n, h, 2 * d), (n, h // 2, 2 * d), (2 * n, h // 2, d)):
+                with pytest.raises(ValueError):
+                    call(**{**good, key: torch.zeros(shape, dtype=good[key].dtype)})
+                assert not rec.calls, (key, shape)
