@@ -406,7 +406,7 @@ class Rope:
         desc = RopeDesc(head_dim, self.rot_dim, n_axes, int(bool(interleaved)), float(scale), f.ctypes.data,
                         None if ax is None else ax.ctypes.data, self.table.data_ptr(), b.value)
         h = ctypes.c_void_p()
-        torch.cuda.synchronize()
+        torch.cuda.synchronize(self.table.device)
         _check("kv_rope_create", lib().kv_rope_create(ctypes.byref(desc), ctypes.byref(h)))
         self.handle = h
 

@@ -228,3 +228,15 @@ def test_wrong_heads_are_refused(rec, name, heads):
                 with pytest.raises(ValueError):
                     call(**{**good, key: torch.zeros(shape, dtype=good[key].dtype)})
                 assert not rec.calls, (key, shape)
+
+
+def test_rope_waits_for_the_card_of_its_table(rec, monkeypatch):
+    """The table is filled by a copy outside torch's streams: what torch still does to its memory has to
+    be over on the table's card, which need not be the current one."""
+    waited = []
+    monkeypatch.setattr(torch.cuda, "synchronize", lambda device=None: waited.append((device, len(rec.calls))))
+    rope = mk.Rope(D, np.ones(32), device="cpu")
+    names = [name for name, _ in rec.calls]
+    assert names == ["kv_rope_bytes", "kv_rope_create"]
+    assert waited == [(rope.table.device, 1)]  # before the second call, for that card
+    rope.handle = None
