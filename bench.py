@@ -321,7 +321,7 @@ class DenseControls:
             "timing": f"decode only (decode + merge per layer, no append, no Retier), "
                       f"{reps} sweeps of {n_layers} layers between two HIP events",
             "mixed": {**row(t_mixed, b_mixed), "seq_len": int(sl_h[0]),
-                      "kernel": "decode_kernel<256, true, true, false, false> + decode_merge_kernel"},
+                      "kernel": "decode_kernel<256, true, true, false, false, false, false> + decode_merge_kernel"},
             "all_fp8": {**row(t_fp8, b_fp8), "seq_len": self.lens[0],
                         "kernel": "the same kernels, every page FP8"},
             "all_bf16": {**row(t_bf16, b_bf16), "seq_len": self.lens[0],
@@ -657,7 +657,7 @@ def main():
                              "(decode, fused append, merge and the step's Retier share)",
         "roofline": {"bound": "hbm", "achieved": round(achieved / 1e9, 1), "peak": HBM_PEAK / 1e9,
                      "unit": "GB/s", "frac": round(achieved / HBM_PEAK, 4), "traffic": traffic,
-                     "kernel": "decode_kernel<256, true, true, true, false> (split scan with "
+                     "kernel": "decode_kernel<256, true, true, true, false, false, false> (split scan with "
                                "the fused append, one launch per layer)"},
         "counters": {k: int(v) for k, v in counters.items()},
         "setup_s": round(setup_s, 1),

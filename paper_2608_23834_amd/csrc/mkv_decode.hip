@@ -40,8 +40,8 @@
 // takes each KV head's pages from a list instead of the whole table.  The last
 // two answer with fp32's error (FINE, below).  24 / 4 heads, d = 256, window 1,024:
 // ROPE, 8 requests of 12,001 to 20,011 tokens (144 MB, 27.8 us of a copy's bandwidth):
-// 39.7 us a call, 4 of them the merge; SPARSE, 256 pages of each of 32 longer ones (170 MB,
-// 33.0 us): 40.8.
+// 40.0 us a call, 4 of them the merge; SPARSE, 256 pages of each of 32 longer ones (170 MB,
+// 33.0 us): 41.3.
 #include <hip/hip_ext.h>
 #include <hip/hip_runtime.h>
 

@@ -407,9 +407,9 @@ __global__ __launch_bounds__(256) void append_quant_kernel(PoolView P, int layer
 // filled, the lanes of its other slots take the nearest row, which changes no maximum, and
 // hold their stores.
 // 33 K tokens x 4 heads x 4 layers at d = 256 (0.8 GB, 158 us of a copy's bandwidth): the
-// call takes 197 us with 128 registers and four waves a SIMD, 249 with 233 and two (rows kept
+// call takes 193 us with 128 registers and four waves a SIMD, 249 with 233 and two (rows kept
 // unpacked); 214 with the partly filled pages in a loop over the tokens, which the launch
-// then waits for; the plain append of them takes 170.
+// then waits for; the plain append of them takes 172.
 __device__ __forceinline__ float wave_max(float x) {
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) x = fmaxf(x, __shfl_xor(x, o, 64));
