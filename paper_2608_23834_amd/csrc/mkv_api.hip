@@ -415,17 +415,17 @@ mkv_status kv_rope_create(const kv_rope_desc* desc, kv_rope** out) {
   if (desc->n_axes < 1 || desc->n_axes > ROPE_MAX_AXES) return MKV_EUNSUP;
   if (!(desc->scale > 0.0 && desc->scale <= 1e6)) return MKV_ERANGE;
   const int m = desc->rot_dim / 2;
-  std::vector<RopeEntry> tab((size_t)m);
+  RopeEntry tab[128];  // head_dim / 2 at most
   for (int i = 0; i < m; ++i) {
     const double f = desc->inv_freq[i];
     if (!(f >= -4.0 && f <= 4.0)) return MKV_ERANGE;  // (NaN too)
     const int ax = desc->axis ? desc->axis[i] : 0;
     if (ax >= desc->n_axes) return MKV_ERANGE;
-    tab[(size_t)i] = {f, ax, 0};
+    tab[i] = {f, ax, 0};
   }
   if (desc->table_bytes < (size_t)m * sizeof(RopeEntry)) return MKV_ENOMEM;
   if (!aligned16(desc->table)) return MKV_EINVAL;
-  if (hipMemcpy(desc->table, tab.data(), tab.size() * sizeof(RopeEntry), hipMemcpyHostToDevice) != hipSuccess)
+  if (hipMemcpy(desc->table, tab, (size_t)m * sizeof(RopeEntry), hipMemcpyHostToDevice) != hipSuccess)
     return MKV_EHIP;
   kv_rope* r = new (std::nothrow) kv_rope;
   if (!r) return MKV_ENOMEM;
