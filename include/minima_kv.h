@@ -395,6 +395,24 @@ mkv_status paged_attn_decode_sparse(mkv_pool* pool, int32_t layer, int32_t n_req
                                     const int32_t* pages, const int32_t* counts, float* out,
                                     float* lse, void* ws, size_t ws_bytes, hipStream_t stream);
 
+/* The cache read back: bf16 K and V rows of positions from[r] .. from[r] + n_r - 1 of
+ * every request, n_r = cu_tokens[r+1] - cu_tokens[r], as rows cu_tokens[r] .. of k and v
+ * (device int32 [n_req] and [n_req+1], cu[0] = 0, cu[n_req] = n_total).  A value is the one
+ * that attention reads (FP8: scale * code; TQ3: the reconstruction of kv_promote_to_fp8),
+ * evaluated in fp32 and rounded to bf16 (to nearest even).  For one layer k and v are
+ * [n_total][n_kv_heads][head_dim], with MKV_ALL_LAYERS [n_layers] of that; rows k_stride and
+ * v_stride elements apart (layer l's follow layer l - 1's), 8-byte aligned, strides a
+ * multiple of 4 and at least n_kv_heads * head_dim (MKV_EINVAL), at most 2^31 (MKV_ERANGE).
+ * Either of k and v may be NULL, not both; they may not be the same.  A range that does not
+ * lie in [0, 16 * max_pages]: RANGE, and its rows become zeros; so do the rows of a page that
+ * is not mapped or has another tag (BAD_TAG) or an id out of range (RANGE).  cu_tokens that do
+ * not begin with 0 or end with n_total: RANGE, and nothing is written; rows that no request's
+ * entries cover stay as they are.  n_total = 0 does nothing. */
+mkv_status kv_read_tokens(mkv_pool* pool, int32_t layer, int32_t n_req, const int32_t* block_table,
+                          const uint8_t* tags, int32_t max_pages, const int32_t* from,
+                          const int32_t* cu_tokens, int32_t n_total, uint16_t* k, int64_t k_stride,
+                          uint16_t* v, int64_t v_stride, hipStream_t stream);
+
 /* paged_attn_decode for callers that cannot allocate device memory (code
  * under HIP graph capture, tight serving loops, harnesses that forbid
  * hipMalloc): the same attention, with the split partials held in a fixed

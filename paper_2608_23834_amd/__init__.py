@@ -37,7 +37,7 @@ EXPORTS = ["kv_pool_bytes", "kv_pool_create", "kv_pool_destroy", "kv_append_fp8"
            "kv_rope_bytes", "kv_rope_create", "kv_rope_destroy", "kv_rope_apply", "kv_append_fp8_rope",
            "paged_attn_decode_append_rope", "kv_page_bounds_bytes", "kv_page_bounds_update",
            "paged_attn_select_workspace_bytes", "paged_attn_select_pages", "paged_attn_decode_sparse",
-           "mkv_status_string"]
+           "kv_read_tokens", "mkv_status_string"]
 
 _lib = None
 
@@ -131,6 +131,7 @@ def lib() -> ctypes.CDLL:
         L.paged_attn_select_pages.argtypes = [vp, i32, i32, vp, vp, i32, vp, sz, vp, sz, i32, i32, i32, vp, vp,
                                               vp, sz, vp]
         L.paged_attn_decode_sparse.argtypes = [vp, i32, i32, vp, vp, vp, i32, vp, i32, vp, vp, vp, vp, vp, sz, vp]
+        L.kv_read_tokens.argtypes = [vp, i32, i32, vp, vp, i32, vp, vp, i32, vp, i64, vp, i64, vp]
         L.mkv_control_bf16_write.argtypes = [vp, i32, i32, i32, i32, i32, i32, vp, i32, vp, vp, i32,
                                              vp, vp, vp]
         L.mkv_control_bf16_workspace_bytes.argtypes = [i32, i32, i32, i32, i32, vp]
@@ -609,6 +610,35 @@ def paged_attn_decode_sparse(pool: Pool, layer, q, block_table, tags, seq_lens, 
         pool.handle, layer, n_req, q.data_ptr(), block_table.data_ptr(), tags.data_ptr(), max_pages,
         seq_lens.data_ptr(), pages.shape[2], pages.data_ptr(), counts.data_ptr(), out.data_ptr(), _ptr(lse),
         ws.data_ptr(), ws.nbytes, cur if stream is None else stream.cuda_stream))
+
+
+def kv_read_tokens(pool: Pool, layer, block_table, tags, seq_from, cu_tokens, k, v, stream=None):
+    """bf16 K and V rows of positions seq_from[r] .. of every request (cu_tokens[r+1] - cu_tokens[r]
+    of them); k, v: [n][H][d] of one layer or [n_layers][n][H][d], tokens may be strided, either None."""
+    dev, cur = _current()
+    i32 = _types()[1]
+    n_req, max_pages = _table(dev, pool, block_table, tags, i32)
+    one = k if v is None else v
+    if one is None:
+        raise ValueError("k or v is wanted")
+    shape = one.shape
+    ok = k is None or k.shape == shape
+    if layer >= 0:
+        ok = ok and len(shape) == 3
+    else:
+        ok = ok and len(shape) == 4 and shape[0] == pool.n_layers
+    if not ok or shape[-2] != pool.n_kv_heads or shape[-1] != pool.d:
+        raise ValueError("k and v are [n][H][head_dim], with all layers [n_layers][n][H][head_dim]")
+    n = shape[-3]
+    _here(dev, seq_from, cu_tokens)
+    if not (seq_from.dtype in i32 and cu_tokens.dtype in i32):
+        raise ValueError(_WRONG_TYPE)
+    if seq_from.numel() < n_req or cu_tokens.numel() <= n_req:
+        raise ValueError("seq_from is [n_req], cu_tokens [n_req + 1]")
+    ks, vs = [0 if t is None else _rows(dev, t, shape) for t in (k, v)]
+    _check("kv_read_tokens", lib().kv_read_tokens(
+        pool.handle, layer, n_req, block_table.data_ptr(), tags.data_ptr(), max_pages, seq_from.data_ptr(),
+        cu_tokens.data_ptr(), n, _ptr(k), ks, _ptr(v), vs, cur if stream is None else stream.cuda_stream))
 
 
 def paged_attn_chunk(pool: Pool, layer, q, cu_q, block_table, tags, seq_lens, out, ws,

@@ -30,7 +30,7 @@ EXACT = {"mkv_pool_kernels.hip", "mkv_rope.hip", "mkv_sparse.hip"}
 # rarely taken rescale branch).
 EXTRA = {"mkv_chunk.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
 SOURCES = ["mkv_api.hip", "mkv_pool_kernels.hip", "mkv_decode.hip", "mkv_chunk.hip", "mkv_probe.hip",
-           "mkv_control.hip", "mkv_rope.hip", "mkv_sparse.hip"]
+           "mkv_control.hip", "mkv_rope.hip", "mkv_sparse.hip", "mkv_read.hip"]
 
 
 def _compile(src: str) -> str:

@@ -540,6 +540,27 @@ mkv_status paged_attn_select_pages(mkv_pool* pool, int32_t layer, int32_t n_req,
                                   n_first, n_last, pages, counts, ws, stream));
 }
 
+mkv_status kv_read_tokens(mkv_pool* pool, int32_t layer, int32_t n_req, const int32_t* block_table,
+                          const uint8_t* tags, int32_t max_pages, const int32_t* from, const int32_t* cu_tokens,
+                          int32_t n_total, uint16_t* k, int64_t k_stride, uint16_t* v, int64_t v_stride,
+                          hipStream_t stream) {
+  if (!pool || !block_table || !tags || !from || !cu_tokens) return MKV_EINVAL;
+  if (n_req < 1 || max_pages < 1 || n_total < 0) return MKV_EINVAL;
+  if (n_total > 0) {
+    if (k == v) return MKV_EINVAL;  // neither, or one memory for both
+    const int64_t width = (int64_t)pool->n_kv_heads * pool->d;
+    if (k_stride > ((int64_t)1 << 31) || v_stride > ((int64_t)1 << 31)) return MKV_ERANGE;
+    if ((k && !good_rows(k, k_stride, width)) || (v && !good_rows(v, v_stride, width))) return MKV_EINVAL;
+  }
+  if (layer != MKV_ALL_LAYERS && (layer < 0 || layer >= pool->n_layers)) return MKV_ERANGE;
+  if (max_pages > 1024 * 256) return MKV_ERANGE;
+  if (n_total == 0) return MKV_OK;
+  const PoolView P = view_of(pool);
+  if (read_tasks(P, layer, n_req, n_total) > ((int64_t)1 << 31)) return MKV_ERANGE;
+  return hip_status(launch_read_tokens(P, layer, n_req, block_table, tags, max_pages, from, cu_tokens, n_total, k,
+                                       k_stride, v, v_stride, stream));
+}
+
 mkv_status paged_attn_set_deterministic(mkv_pool* pool, int32_t enable) {
   if (!pool) return MKV_EINVAL;
   pool->deterministic = enable != 0;

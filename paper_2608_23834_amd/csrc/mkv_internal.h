@@ -136,6 +136,12 @@ hipError_t launch_select(const PoolView& P, int layer, int n_req, const uint16_t
                          int max_pages, const uint8_t* codes, const float* scales, int n_select, int n_first,
                          int n_last, int32_t* sel, int32_t* counts, void* ws, hipStream_t s);
 
+// mkv_read.hip
+int64_t read_tasks(const PoolView& P, int layer, int n_req, int n_total);
+hipError_t launch_read_tokens(const PoolView& P, int layer, int n_req, const int32_t* bt, const uint8_t* tags, int max_pages,
+                              const int32_t* from, const int32_t* cu, int n_total, uint16_t* k, int64_t kts, uint16_t* v,
+                              int64_t vts, hipStream_t s);
+
 // mkv_control.hip (dense bf16 control, measurement only)
 size_t control_bf16_ws_bytes(int n_req, int max_pages, int n_kv_heads, int group, int d);
 hipError_t launch_control_bf16_write(uint16_t* pages, int n_pages, int H, int d, int layer, int n_req,
