@@ -320,6 +320,39 @@ mkv_status kv_append_fp8_rope(mkv_pool* pool, const kv_rope* rope, int32_t layer
                               int64_t k_stride, const uint16_t* v, int64_t v_stride,
                               hipStream_t stream);
 
+/* Norms of query and key heads, in the same pass as the rotation.  Every head of a row
+ * becomes
+ *     y_c = x_c r (w_c + add),  r = 1 / sqrt(sum_c x_c^2 / head_dim + eps),
+ * and is then rotated as above, all in fp64 with one rounding to bf16 (to nearest even).  A
+ * NULL rope leaves the rotation out (positions are not read then), a rope's scale touches
+ * rotated channels only.  weight: device bf16, channel c of head h at h * head_stride + c, for
+ * an append of several layers layer l's at l * layer_stride more; strides 0: the same weights
+ * for all of them; NULL: all ones, add is not used.  The struct is read during the call.
+ *  - kv_norm_rope_apply: kv_rope_apply of normed rows; buffers, strides, in-place use and
+ *    errors as there.
+ *  - kv_append_fp8_norm_rope: kv_append_fp8_rope of normed keys (values are neither normed
+ *    nor rotated).  Pages, scales, table, tags and errors equal those of kv_norm_rope_apply on
+ *    the keys followed by kv_append_fp8 (a sum of squares that fp64 rounds differently in
+ *    another order crosses a bf16 rounding boundary once in 2^40).
+ * Errors also: EINVAL (head_dim differs from the rope's or the pool's, weight not 8-byte
+ * aligned, a stride negative or no multiple of 4), EUNSUP (head_dim), ERANGE (eps outside
+ * [1e-30, 1], add not a number or over 1e6, strides over 2^31). */
+typedef struct kv_head_norm {
+  int32_t head_dim;       /* 128 or 256 */
+  double eps;
+  double add;             /* added to every weight (1 for weights kept as differences from 1) */
+  const uint16_t* weight; /* device bf16 or NULL */
+  int64_t head_stride, layer_stride; /* elements */
+} kv_head_norm;
+mkv_status kv_norm_rope_apply(const kv_rope* rope, const kv_head_norm* norm, int32_t n_tokens, int32_t n_heads,
+                              const uint16_t* x, int64_t x_stride, const int32_t* positions, uint16_t* out,
+                              int64_t out_stride, hipStream_t stream);
+mkv_status kv_append_fp8_norm_rope(mkv_pool* pool, const kv_rope* rope, const kv_head_norm* norm, int32_t layer,
+                                   int32_t n_req, int32_t* block_table, uint8_t* tags, int32_t max_pages,
+                                   const int32_t* seq_lens_before, const int32_t* cu_new_tokens,
+                                   int32_t n_new_total, const int32_t* positions, const uint16_t* k,
+                                   int64_t k_stride, const uint16_t* v, int64_t v_stride, hipStream_t stream);
+
 /* paged_attn_decode_append of a query and key that come unrotated: both are
  * rotated by their token's positions (device int32 [n_axes][n_req], or NULL:
  * seq_lens_before[r] on every axis) and rounded to bf16 inside the launch.  State

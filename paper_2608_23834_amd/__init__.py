@@ -37,7 +37,7 @@ EXPORTS = ["kv_pool_bytes", "kv_pool_create", "kv_pool_destroy", "kv_append_fp8"
            "kv_rope_bytes", "kv_rope_create", "kv_rope_destroy", "kv_rope_apply", "kv_append_fp8_rope",
            "paged_attn_decode_append_rope", "kv_page_bounds_bytes", "kv_page_bounds_update",
            "paged_attn_select_workspace_bytes", "paged_attn_select_pages", "paged_attn_decode_sparse",
-           "kv_read_tokens", "mkv_status_string"]
+           "kv_read_tokens", "kv_norm_rope_apply", "kv_append_fp8_norm_rope", "mkv_status_string"]
 
 _lib = None
 
@@ -65,6 +65,11 @@ class RopeDesc(ctypes.Structure):
     _fields_ = [("head_dim", ctypes.c_int32), ("rot_dim", ctypes.c_int32), ("n_axes", ctypes.c_int32),
                 ("interleaved", ctypes.c_int32), ("scale", ctypes.c_double), ("inv_freq", ctypes.c_void_p),
                 ("axis", ctypes.c_void_p), ("table", ctypes.c_void_p), ("table_bytes", ctypes.c_size_t)]
+
+
+class HeadNormDesc(ctypes.Structure):
+    _fields_ = [("head_dim", ctypes.c_int32), ("eps", ctypes.c_double), ("add", ctypes.c_double),
+                ("weight", ctypes.c_void_p), ("head_stride", ctypes.c_int64), ("layer_stride", ctypes.c_int64)]
 
 
 class Counters(ctypes.Structure):
@@ -131,6 +136,8 @@ def lib() -> ctypes.CDLL:
         L.paged_attn_select_pages.argtypes = [vp, i32, i32, vp, vp, i32, vp, sz, vp, sz, i32, i32, i32, vp, vp,
                                               vp, sz, vp]
         L.paged_attn_decode_sparse.argtypes = [vp, i32, i32, vp, vp, vp, i32, vp, i32, vp, vp, vp, vp, vp, sz, vp]
+        L.kv_norm_rope_apply.argtypes = [vp, vp, i32, i32, vp, i64, vp, vp, i64, vp]
+        L.kv_append_fp8_norm_rope.argtypes = [vp, vp, vp, i32, i32, vp, vp, i32, vp, vp, i32, vp, vp, i64, vp, i64, vp]
         L.kv_read_tokens.argtypes = [vp, i32, i32, vp, vp, i32, vp, vp, i32, vp, i64, vp, i64, vp]
         L.mkv_control_bf16_write.argtypes = [vp, i32, i32, i32, i32, i32, i32, vp, i32, vp, vp, i32,
                                              vp, vp, vp]
@@ -464,11 +471,47 @@ def kv_rope_apply(rope: Rope, x, positions, out, stream=None):
         _rows(dev, out, shape), cur if stream is None else stream.cuda_stream))
 
 
-def kv_append_fp8_rope(pool: Pool, rope: Rope, layer, block_table, tags, seq_lens_before, cu_new_tokens,
-                       positions, k, v, stream=None):
-    """kv_append_fp8 with the keys rotated on the way; k, v: [n][H][d] of one layer or
-    [n_layers][n][H][d], tokens may be strided; positions: int32 [n_axes][n] or None."""
+class HeadNorm:
+    """Norm of query or key heads (kv_head_norm): rows times 1 / sqrt(mean x^2 + eps) and the weights,
+    bf16 (or its bits in int16) [head_dim], [heads][head_dim] or [layers][heads][head_dim]; None: ones.
+    unit_offset: the weights are kept as differences from one.  The object holds the tensor."""
+
+    def __init__(self, head_dim, weight=None, eps=1e-6, unit_offset=False):
+        self.head_dim, self.weight, self.eps, self.add = head_dim, weight, float(eps), 1.0 if unit_offset else 0.0
+        self._desc()
+
+    def _desc(self, heads=None, layers=1, dev=None):
+        """The description for rows of `heads` heads and `layers` layers on device dev."""
+        w, d = self.weight, self.head_dim
+        if w is None:
+            return HeadNormDesc(d, self.eps, self.add, None, 0, 0)
+        s = w.shape
+        if w.dtype not in _types()[0] or not w.is_contiguous() or not 1 <= len(s) <= 3 or s[-1] != d:
+            raise ValueError("weights are contiguous bf16 (or its bits in int16), [..][head_dim]")
+        if heads is not None and (w.get_device() != dev or (len(s) > 1 and s[-2] != heads)
+                                  or (len(s) > 2 and s[0] != layers)):
+            raise ValueError(f"weights are [head_dim], [{heads}][head_dim] or [{layers}][{heads}][head_dim] on the "
+                             "current device")
+        return HeadNormDesc(d, self.eps, self.add, w.data_ptr(), d if len(s) > 1 else 0, s[-2] * d if len(s) > 2 else 0)
+
+
+def kv_norm_rope_apply(rope, norm: HeadNorm, x, positions, out, stream=None):
+    """Every head of bf16 rows x [n][heads][head_dim] normed and rotated into out; rope None: normed
+    only (positions are not read).  positions: int32 [n_axes][n]."""
     dev, cur = _current()
+    shape = x.shape
+    n, heads, d = shape
+    if out.shape != shape or d != norm.head_dim or (rope is not None and d != rope.head_dim):
+        raise ValueError("x and out are [n][heads][head_dim]")
+    desc = norm._desc(heads, 1, dev)
+    _check("kv_norm_rope_apply", lib().kv_norm_rope_apply(
+        None if rope is None else rope.handle, ctypes.byref(desc), n, heads, x.data_ptr(), _rows(dev, x, shape),
+        None if rope is None else _positions(dev, rope, positions, n), out.data_ptr(), _rows(dev, out, shape),
+        cur if stream is None else stream.cuda_stream))
+
+
+def _append_rows(dev, pool, layer, block_table, tags, seq_lens_before, cu_new_tokens, k, v):
+    """(n_req, max_pages, shape of k and v) of an append of strided rows."""
     i32 = _types()[1]
     n_req, max_pages = _table(dev, pool, block_table, tags, i32)
     shape = k.shape
@@ -479,16 +522,39 @@ def kv_append_fp8_rope(pool: Pool, rope: Rope, layer, block_table, tags, seq_len
         ok = ok and len(shape) == 4 and shape[0] == pool.n_layers
     if not ok or shape[-2] != pool.n_kv_heads or shape[-1] != pool.d:
         raise ValueError("k and v are [n][H][head_dim], with all layers [n_layers][n][H][head_dim]")
-    n = shape[-3]
     _here(dev, seq_lens_before, cu_new_tokens)
     if not (seq_lens_before.dtype in i32 and cu_new_tokens.dtype in i32):
         raise ValueError(_WRONG_TYPE)
     if seq_lens_before.numel() < n_req or cu_new_tokens.numel() <= n_req:
         raise ValueError("seq_lens_before is [n_req], cu_new_tokens [n_req + 1]")
+    return n_req, max_pages, shape
+
+
+def kv_append_fp8_rope(pool: Pool, rope: Rope, layer, block_table, tags, seq_lens_before, cu_new_tokens,
+                       positions, k, v, stream=None):
+    """kv_append_fp8 with the keys rotated on the way; k, v: [n][H][d] of one layer or
+    [n_layers][n][H][d], tokens may be strided; positions: int32 [n_axes][n] or None."""
+    dev, cur = _current()
+    n_req, max_pages, shape = _append_rows(dev, pool, layer, block_table, tags, seq_lens_before, cu_new_tokens, k, v)
+    n = shape[-3]
     _check("kv_append_fp8_rope", lib().kv_append_fp8_rope(
         pool.handle, rope.handle, layer, n_req, block_table.data_ptr(), tags.data_ptr(), max_pages,
         seq_lens_before.data_ptr(), cu_new_tokens.data_ptr(), n, _positions(dev, rope, positions, n), k.data_ptr(),
         _rows(dev, k, shape), v.data_ptr(), _rows(dev, v, shape), cur if stream is None else stream.cuda_stream))
+
+
+def kv_append_fp8_norm_rope(pool: Pool, rope, norm: HeadNorm, layer, block_table, tags, seq_lens_before, cu_new_tokens,
+                            positions, k, v, stream=None):
+    """kv_append_fp8_rope with every key head normed before its rotation; rope None: normed only."""
+    dev, cur = _current()
+    n_req, max_pages, shape = _append_rows(dev, pool, layer, block_table, tags, seq_lens_before, cu_new_tokens, k, v)
+    n = shape[-3]
+    desc = norm._desc(pool.n_kv_heads, shape[0] if layer < 0 else 1, dev)
+    _check("kv_append_fp8_norm_rope", lib().kv_append_fp8_norm_rope(
+        pool.handle, None if rope is None else rope.handle, ctypes.byref(desc), layer, n_req, block_table.data_ptr(),
+        tags.data_ptr(), max_pages, seq_lens_before.data_ptr(), cu_new_tokens.data_ptr(), n,
+        None if rope is None else _positions(dev, rope, positions, n), k.data_ptr(), _rows(dev, k, shape), v.data_ptr(),
+        _rows(dev, v, shape), cur if stream is None else stream.cuda_stream))
 
 
 def paged_attn_decode_append_rope(pool: Pool, rope: Rope, layer, q, k_new, v_new, positions, block_table, tags,

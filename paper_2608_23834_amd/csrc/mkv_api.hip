@@ -445,25 +445,73 @@ mkv_status kv_rope_destroy(kv_rope* rope) {
   return MKV_OK;
 }
 
+static bool rows_overlap(int32_t n, int64_t width, const void* x, int64_t x_stride, const void* out, int64_t out_stride) {
+  if (x == out && x_stride == out_stride) return false;  // in place
+  const uintptr_t a = reinterpret_cast<uintptr_t>(x), b = reinterpret_cast<uintptr_t>(out);
+  const uintptr_t na = 2 * (uintptr_t)((n - 1) * x_stride + width);
+  const uintptr_t nb = 2 * (uintptr_t)((n - 1) * out_stride + width);
+  return a < b + nb && b < a + na;
+}
+
+// n_tokens rows of n_heads heads, from x to out
+static mkv_status check_rows(int32_t n_tokens, int32_t n_heads, int32_t head_dim, const uint16_t* x, int64_t x_stride,
+                             const uint16_t* out, int64_t out_stride) {
+  const int64_t width = (int64_t)n_heads * head_dim;
+  if (width > ((int64_t)1 << 30) || x_stride > ((int64_t)1 << 31) || out_stride > ((int64_t)1 << 31)) return MKV_ERANGE;
+  if (!good_rows(x, x_stride, width) || !good_rows(out, out_stride, width)) return MKV_EINVAL;
+  return rows_overlap(n_tokens, width, x, x_stride, out, out_stride) ? MKV_EINVAL : MKV_OK;
+}
+
 mkv_status kv_rope_apply(const kv_rope* rope, int32_t n_tokens, int32_t n_heads, const uint16_t* x,
                          int64_t x_stride, const int32_t* positions, uint16_t* out, int64_t out_stride,
                          hipStream_t stream) {
   if (!rope || n_tokens < 0 || n_heads < 1) return MKV_EINVAL;
   if (n_tokens == 0) return MKV_OK;
   if (!x || !positions || !out) return MKV_EINVAL;
-  if ((int64_t)n_heads * rope->head_dim > ((int64_t)1 << 30) || x_stride > ((int64_t)1 << 31) ||
-      out_stride > ((int64_t)1 << 31))
-    return MKV_ERANGE;
-  const int64_t width = (int64_t)n_heads * rope->head_dim;
-  if (!good_rows(x, x_stride, width) || !good_rows(out, out_stride, width)) return MKV_EINVAL;
-  if (!(x == out && x_stride == out_stride)) {  // in place, or apart
-    const uintptr_t a = reinterpret_cast<uintptr_t>(x), b = reinterpret_cast<uintptr_t>(out);
-    const uintptr_t na = 2 * (uintptr_t)((n_tokens - 1) * x_stride + width);
-    const uintptr_t nb = 2 * (uintptr_t)((n_tokens - 1) * out_stride + width);
-    if (a < b + nb && b < a + na) return MKV_EINVAL;
-  }
+  mkv_status st = check_rows(n_tokens, n_heads, rope->head_dim, x, x_stride, out, out_stride);
+  if (st != MKV_OK) return st;
   return hip_status(launch_rope_apply(rope->view, rope->head_dim, n_tokens, n_heads, x, x_stride, positions, out,
                                       out_stride, stream));
+}
+
+static RopeView no_rope() {
+  RopeView v = {};
+  v.scale = 1.0;
+  v.n_axes = 1;
+  return v;
+}
+
+// a norm and the rope behind it (which may be null) for heads of head_dim channels
+static mkv_status check_norm(const kv_head_norm* norm, const kv_rope* rope, int head_dim, NormView* N) {
+  if (!norm) return MKV_EINVAL;
+  if (norm->head_dim != 128 && norm->head_dim != 256) return MKV_EUNSUP;
+  if (norm->head_dim != head_dim || (rope && rope->head_dim != head_dim)) return MKV_EINVAL;
+  if (!(norm->eps >= 1e-30 && norm->eps <= 1.0) || !(norm->add >= -1e6 && norm->add <= 1e6)) return MKV_ERANGE;
+  if (norm->head_stride > ((int64_t)1 << 31) || norm->layer_stride > ((int64_t)1 << 31)) return MKV_ERANGE;
+  if (norm->head_stride < 0 || norm->head_stride % 4 || norm->layer_stride < 0 || norm->layer_stride % 4 ||
+      (reinterpret_cast<uintptr_t>(norm->weight) & 7))
+    return MKV_EINVAL;
+  N->w = norm->weight;
+  N->head = norm->weight ? norm->head_stride : 0;
+  N->layer = norm->layer_stride;
+  N->eps = norm->eps;
+  N->add = norm->weight ? norm->add : 0.0;
+  return MKV_OK;
+}
+
+mkv_status kv_norm_rope_apply(const kv_rope* rope, const kv_head_norm* norm, int32_t n_tokens, int32_t n_heads,
+                              const uint16_t* x, int64_t x_stride, const int32_t* positions, uint16_t* out,
+                              int64_t out_stride, hipStream_t stream) {
+  if (!norm || n_tokens < 0 || n_heads < 1) return MKV_EINVAL;
+  NormView N;
+  mkv_status st = check_norm(norm, rope, norm->head_dim, &N);
+  if (st != MKV_OK) return st;
+  if (n_tokens == 0) return MKV_OK;
+  if (!x || !out || (rope && !positions)) return MKV_EINVAL;
+  st = check_rows(n_tokens, n_heads, norm->head_dim, x, x_stride, out, out_stride);
+  if (st != MKV_OK) return st;
+  return hip_status(launch_norm_rope_apply(rope ? rope->view : no_rope(), N, norm->head_dim, n_tokens, n_heads, x, x_stride,
+                                           positions, out, out_stride, stream));
 }
 
 mkv_status kv_append_fp8_rope(mkv_pool* pool, const kv_rope* rope, int32_t layer, int32_t n_req,
@@ -483,6 +531,28 @@ mkv_status kv_append_fp8_rope(mkv_pool* pool, const kv_rope* rope, int32_t layer
   return hip_status(launch_append_rope(view_of(pool), rope->view, layer, n_req, block_table, tags, max_pages,
                                        seq_lens_before, cu_new_tokens, n_new_total, positions, k, k_stride, v,
                                        v_stride, stream));
+}
+
+mkv_status kv_append_fp8_norm_rope(mkv_pool* pool, const kv_rope* rope, const kv_head_norm* norm, int32_t layer,
+                                   int32_t n_req, int32_t* block_table, uint8_t* tags, int32_t max_pages,
+                                   const int32_t* seq_lens_before, const int32_t* cu_new_tokens,
+                                   int32_t n_new_total, const int32_t* positions, const uint16_t* k,
+                                   int64_t k_stride, const uint16_t* v, int64_t v_stride, hipStream_t stream) {
+  if (!pool || !block_table || !tags || !seq_lens_before || !cu_new_tokens) return MKV_EINVAL;
+  if (n_req < 1 || max_pages < 1 || n_new_total < 0) return MKV_EINVAL;
+  NormView N;
+  mkv_status st = check_norm(norm, rope, pool->d, &N);
+  if (st != MKV_OK) return st;
+  if (n_new_total > 0) {
+    if (!k || !v) return MKV_EINVAL;
+    const int64_t width = (int64_t)pool->n_kv_heads * pool->d;
+    if (k_stride > ((int64_t)1 << 26) || v_stride > ((int64_t)1 << 26)) return MKV_ERANGE;  // as kv_append_fp8_rope
+    if (!good_rows(k, k_stride, width) || !good_rows(v, v_stride, width)) return MKV_EINVAL;
+  }
+  if (layer != MKV_ALL_LAYERS && (layer < 0 || layer >= pool->n_layers)) return MKV_ERANGE;
+  return hip_status(launch_append_norm_rope(view_of(pool), rope ? rope->view : no_rope(), N, layer, n_req, block_table,
+                                            tags, max_pages, seq_lens_before, cu_new_tokens, n_new_total,
+                                            rope ? positions : nullptr, k, k_stride, v, v_stride, stream));
 }
 
 mkv_status kv_page_bounds_bytes(const mkv_pool* pool, int32_t n_req, int32_t max_pages, size_t* code_bytes,

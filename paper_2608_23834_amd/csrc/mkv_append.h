@@ -11,7 +11,7 @@
 
 #include "mkv_device.h"
 #include "mkv_internal.h"
-#include "mkv_rope.h"
+#include "mkv_norm.h"
 
 namespace mkv {
 
@@ -58,8 +58,11 @@ __device__ __forceinline__ void small_task_load_x(SmallTask<D>& T, int64_t kts, 
 // Rotate a key task's rows (x as loaded), through an LDS block of them [token][channel]
 // (xs, at least (t1 - t0) D bf16): one lane per (token, pair), so an angle is evaluated once
 // and any pairing is the same code.  cos_sin(t, i, c, s): those of token t0 + t, pair i.
-template <int D, class F>
-__device__ __forceinline__ void small_task_rotate(SmallTask<D>& T, const RopeView& R, uint16_t* xs, int lane, F cos_sin) {
+// NORM: every row is normed first, weight(c) the factor of channel c, s_rs an LDS array of 16
+// (R.rot may be 0 then).
+template <int D, bool NORM = false, class F, class W>
+__device__ __forceinline__ void small_task_rotate(SmallTask<D>& T, const RopeView& R, uint16_t* xs, int lane, F cos_sin,
+                                                  double eps, W weight, double* s_rs) {
   constexpr int D4 = SmallTask<D>::D4;
   const int nt = T.t1 - T.t0, n4 = nt * D4, m = R.rot / 2;
 #pragma unroll
@@ -68,8 +71,30 @@ __device__ __forceinline__ void small_task_rotate(SmallTask<D>& T, const RopeVie
     if (idx < n4) reinterpret_cast<uint2*>(xs)[idx] = T.x[j];
   }
   __builtin_amdgcn_wave_barrier();
+  if constexpr (NORM) {
+    double rs = 0.0;  // of token `lane`
+    for (int t = 0; t < nt; ++t) {
+      double sum = 0.0;
+#pragma unroll
+      for (int q = 0; q < D / 64; ++q) {
+        const double x = (double)bf16_to_f32(xs[t * D + D / 64 * lane + q]);
+        sum = __builtin_fma(x, x, sum);
+      }
+      sum = row_sum<64>(sum, lane);
+      rs = lane == t ? sum : rs;
+    }
+    if (lane < PAGE) s_rs[lane] = norm_rstd(rs, D, eps);
+    __builtin_amdgcn_wave_barrier();
+    // channels past the rotated ones (those are normed as they are turned)
+    const int nr = D - R.rot;
+    for (int it = lane; it < nt * nr; it += 64) {
+      const int t = it / nr, c = R.rot + it % nr;
+      xs[t * D + c] = (uint16_t)f64_to_bf16((double)bf16_to_f32(xs[t * D + c]) * s_rs[t] * weight(c));
+    }
+  }
   int t = 0, i = lane;  // pair lane, lane + 64, .. of the run of tokens
-  while (i >= m) {
+  if (NORM && m == 0) t = nt;
+  while (t < nt && i >= m) {
     i -= m;
     ++t;
   }
@@ -78,7 +103,12 @@ __device__ __forceinline__ void small_task_rotate(SmallTask<D>& T, const RopeVie
     cos_sin(t, i, c, s);
     const int2 pr = rope_pair(R, i);
     uint16_t* x = xs + t * D;
-    rope_rotate((double)bf16_to_f32(x[pr.x]), (double)bf16_to_f32(x[pr.y]), c, s, y0, y1);
+    double x0 = (double)bf16_to_f32(x[pr.x]), x1 = (double)bf16_to_f32(x[pr.y]);
+    if constexpr (NORM) {
+      x0 = x0 * s_rs[t] * weight(pr.x);
+      x1 = x1 * s_rs[t] * weight(pr.y);
+    }
+    rope_rotate(x0, x1, c, s, y0, y1);
     x[pr.x] = (uint16_t)f64_to_bf16(y0);
     x[pr.y] = (uint16_t)f64_to_bf16(y1);
     i += 64;
@@ -94,6 +124,11 @@ __device__ __forceinline__ void small_task_rotate(SmallTask<D>& T, const RopeVie
     if (idx < n4) T.x[j] = reinterpret_cast<const uint2*>(xs)[idx];
   }
   __builtin_amdgcn_wave_barrier();  // xs is free
+}
+
+template <int D, class F>
+__device__ __forceinline__ void small_task_rotate(SmallTask<D>& T, const RopeView& R, uint16_t* xs, int lane, F cos_sin) {
+  small_task_rotate<D, false>(T, R, xs, lane, cos_sin, 0.0, [](int) { return 1.0; }, nullptr);
 }
 
 // codes and scale of page-head (T.layer, id, T.h), part T.kv; only a page with

@@ -82,6 +82,10 @@ hipError_t launch_append_rope(const PoolView& P, const RopeView& R, int layer, i
                               uint8_t* tags, int max_pages, const int32_t* sb, const int32_t* cu,
                               int n_new_total, const int32_t* pos, const uint16_t* k, int64_t kts,
                               const uint16_t* v, int64_t vts, hipStream_t s);
+hipError_t launch_append_norm_rope(const PoolView& P, const RopeView& R, const NormView& N, int layer, int n_req,
+                                   int32_t* bt, uint8_t* tags, int max_pages, const int32_t* sb, const int32_t* cu,
+                                   int n_new_total, const int32_t* pos, const uint16_t* k, int64_t kts, const uint16_t* v,
+                                   int64_t vts, hipStream_t s);
 hipError_t launch_migrate(const PoolView& P, int n_req, int32_t* bt, uint8_t* tags, int max_pages,
                           const uint8_t* anchor, const int32_t* seq_lens, hipStream_t s);
 hipError_t launch_promote(const PoolView& P, int n_req, int32_t* bt, uint8_t* tags, int max_pages,
@@ -126,6 +130,9 @@ hipError_t launch_score_collect(int n_req, int n_q_heads, int max_pages, const i
 // mkv_rope.hip
 hipError_t launch_rope_apply(const RopeView& R, int d, int n_tokens, int n_heads, const uint16_t* x, int64_t xs,
                              const int32_t* pos, uint16_t* out, int64_t os, hipStream_t s);
+
+hipError_t launch_norm_rope_apply(const RopeView& R, const NormView& N, int d, int n_tokens, int n_heads, const uint16_t* x,
+                                  int64_t xs, const int32_t* pos, uint16_t* out, int64_t os, hipStream_t s);
 
 // mkv_sparse.hip
 hipError_t launch_page_bounds(const PoolView& P, int layer, int n_req, const int32_t* bt, const uint8_t* tags,

@@ -450,14 +450,19 @@ __device__ __attribute__((noinline)) void rope_requant(uint8_t* reg, int n, floa
 }
 
 // cos_sin(t, j, q): cosine and sine of slot t, pair V j + q
-template <int D, int V, bool NEAR, class F>
+// NORM: the rows are normed first, the head's weights at nw (null: ones), s_rs 16 doubles of
+// LDS for this wave: the sums over the lanes of a row come first, for all rows, then each
+// slot's factor once.
+template <int D, int V, bool NEAR, bool NORM = false, class F>
 __device__ __forceinline__ void rope_quant_task(uint8_t* reg, float* sc, const uint8_t* rows, int64_t tstride,
-                                                const RopeView& R, F cos_sin, int t0, int t1, int lane) {
+                                                const RopeView& R, F cos_sin, int t0, int t1, int lane,
+                                                const uint16_t* nw = nullptr, double eps = 0.0, double add = 0.0,
+                                                double* s_rs = nullptr) {
   typedef typename RopeGroup<V>::type group;
   // LT lanes a token; a pass of the wave holds 64 / LT tokens, or (D = 256, V = 1) half of one
   constexpr int LT = D / (2 * V), NP = PAGE * LT / 64;
   const int m = R.rot / 2;
-  const uint32_t ts = (uint32_t)(2 * tstride);
+  const uint32_t tw = (uint32_t)(2 * tstride);
   uint32_t w[NP][V];
   auto slot = [&](int i, int& t, int& j) {
     t = (64 * i) / LT + (LT < 64 ? lane / LT : 0);
@@ -469,9 +474,47 @@ __device__ __forceinline__ void rope_quant_task(uint8_t* reg, float* sc, const u
     slot(i, t, j);
     rope_lane<V>(R, j, ca, cb);
     t = min(max(t, t0), t1 - 1);
-    const uint8_t* row = rows + (int64_t)t * ts;
+    const uint8_t* row = rows + (int64_t)t * tw;
     const group a = *reinterpret_cast<const group*>(row + 2 * ca), b = *reinterpret_cast<const group*>(row + 2 * cb);
     rope_words(a, b, w[i]);
+  }
+  // NORM: the weights of the lane's channels (two sets where a row takes two passes)
+  constexpr int NW = NORM ? (LT > 64 ? 2 : 1) : 1, LW = LT > 64 ? 64 : LT;
+  [[maybe_unused]] uint32_t wt[NW][V];
+  if constexpr (NORM) {
+#pragma unroll
+    for (int u = 0; u < NW; ++u) {
+      int t, j, ca, cb;
+      slot(u, t, j);
+      rope_lane<V>(R, j, ca, cb);
+#pragma unroll
+      for (int q = 0; q < V; ++q) wt[u][q] = 0x3F803F80u;  // ones
+      if (nw) rope_words(*reinterpret_cast<const group*>(nw + ca), *reinterpret_cast<const group*>(nw + cb), wt[u]);
+    }
+    double sum = 0.0;
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+      if (NW == 1 || !(i & 1)) sum = 0.0;
+      float x[2 * V];
+      rope_unpack<V>(w[i], x);
+#pragma unroll
+      for (int b = 0; b < 2 * V; ++b) sum = __builtin_fma((double)x[b], (double)x[b], sum);
+      // (the words are read again below: the values in fp64 would fill the register file)
+#pragma unroll
+      for (int q = 0; q < V; ++q) asm volatile("" : "+v"(w[i][q]));
+      if (NW == 1 || (i & 1)) {
+        const double all = row_sum<LW>(sum, lane);
+        int t, j;
+        slot(i, t, j);
+        if (lane % LW == 0) s_rs[t] = all;
+      }
+      if (i & 1) __builtin_amdgcn_sched_barrier(0);  // two passes at a time: bounded register use
+    }
+    __builtin_amdgcn_wave_barrier();
+    const double r = norm_rstd(s_rs[lane & 15], D, eps);
+    __builtin_amdgcn_wave_barrier();
+    if (lane < PAGE) s_rs[lane] = r;
+    __builtin_amdgcn_wave_barrier();
   }
   float amax = 0.0f;
   asm volatile("" : "+v"(lane));  // each walk over the passes works its slots out again
@@ -479,10 +522,23 @@ __device__ __forceinline__ void rope_quant_task(uint8_t* reg, float* sc, const u
   for (int i = 0; i < NP; ++i) {
     int t, j;
     slot(i, t, j);
+    [[maybe_unused]] const int ts = t;
     t = min(max(t, t0), t1 - 1);
     float x[2 * V];
     rope_unpack<V>(w[i], x);
-    if (j < m / V) rope_turn<V, NEAR>(x, [&](int q) { return cos_sin(t, j, q); });
+    if constexpr (NORM) {
+      float f[2 * V];
+      double y[2 * V];
+#pragma unroll
+      for (int q = 0; q < V; ++q) asm volatile("" : "+v"(wt[i % NW][q]));
+      rope_unpack<V>(wt[i % NW], f);
+      const double r = s_rs[ts];
+#pragma unroll
+      for (int b = 0; b < 2 * V; ++b) y[b] = (double)x[b] * r * ((double)f[b] + add);
+      rope_turn_f64<V, NEAR>(y, x, j < m / V, [&](int q) { return cos_sin(t, j, q); });
+    } else {
+      if (j < m / V) rope_turn<V, NEAR>(x, [&](int q) { return cos_sin(t, j, q); });
+    }
     rope_pack<V>(x, w[i]);
 #pragma unroll
     for (int b = 0; b < 2 * V; ++b) amax = fmaxf(amax, fabsf(x[b]));
@@ -533,13 +589,15 @@ __device__ __attribute__((noinline)) void rope_fill_table(RopeView R, const int3
 // append_quant_kernel with the keys rotated.  A workgroup takes a listed page and up to hb
 // of the call's (layer, head) pairs: the cosines and sines of the page's 16 tokens are
 // computed once into LDS, then each wave quantizes K and V of one pair after the other.
-template <int D, int V, bool NEAR>
+// NORM: the keys normed first.
+template <int D, int V, bool NEAR, bool NORM>
 __global__ __launch_bounds__(256, 4) void append_rope_quant_kernel(PoolView P, int layer_sel, int n_lcall, int hb,
                                                                 const int32_t* sb, const int32_t* cu,
                                                                 int n_new_total, const uint16_t* k,
                                                                 const uint16_t* v, int64_t kts, int64_t vts,
-                                                                RopeView R, const int32_t* pos) {
+                                                                RopeView R, const int32_t* pos, NormView N) {
   extern __shared__ __align__(16) double2 s_tab[];  // [16][rot / 2]
+  __shared__ double s_rs[NORM ? 4 : 1][PAGE];
   if (P.ctrl[CTRL_ABORT]) return;
   const int H = P.n_kv_heads, LH = n_lcall * H, nb = (LH + hb - 1) / hb, m = R.rot / 2;
   const int64_t n_units = (int64_t)P.ctrl[CTRL_NLIST] * nb;
@@ -559,8 +617,9 @@ __global__ __launch_bounds__(256, 4) void append_rope_quant_kernel(PoolView P, i
       uint8_t* reg = P.fp8 + ph * fp8_region_bytes(D);
       float* sc = P.fp8_scales + ph * 2;
       const uint8_t* rows = reinterpret_cast<const uint8_t*>(k + ((int64_t)li * n_new_total + row0) * kts + (int64_t)h * D);
-      rope_quant_task<D, V, NEAR>(reg, sc, rows, kts, R,
-                                  [&](int t, int j, int q) { return s_tab[t * m + q * (m / V) + j]; }, t0, t1, lane);
+      rope_quant_task<D, V, NEAR, NORM>(reg, sc, rows, kts, R,
+                                        [&](int t, int j, int q) { return s_tab[t * m + q * (m / V) + j]; }, t0, t1, lane,
+                                        NORM ? norm_weights(N, li, h) : nullptr, N.eps, N.add, s_rs[NORM ? wid : 0]);
       quant_task<D, true>(reg, sc, v + (int64_t)li * n_new_total * vts + (int64_t)h * D, row0, t0, t1, vts, lane);
     }
   }
@@ -575,12 +634,14 @@ __global__ __launch_bounds__(256, 4) void append_rope_quant_kernel(PoolView P, i
 // TAB, rotations of up to a quarter of the channels: most lanes would wait while a few evaluate
 // every angle, so the wave evaluates them together, into LDS of its own (two pairs at d = 256, 80 K
 // tokens, 20 and 64 channels: 74 and 77 us against 85 and 81; 64 channels at d = 128 115 against 107).
-template <int D, int V, bool NEAR, bool TAB>
+template <int D, int V, bool NEAR, bool TAB, bool NORM>
 __global__ __launch_bounds__(256, 4) void append_rope_own_kernel(PoolView P, int layer_sel, int n_lcall,
                                                                  const int32_t* sb, const int32_t* cu, int n_new_total,
                                                                  const uint16_t* k, const uint16_t* v, int64_t kts,
-                                                                 int64_t vts, RopeView R, const int32_t* pos) {
+                                                                 int64_t vts, RopeView R, const int32_t* pos,
+                                                                 NormView N) {
   constexpr int LT = D / (2 * V);
+  __shared__ double s_rs[NORM ? 4 : 1][PAGE];
   __shared__ int s_pos[4][ROPE_MAX_AXES * PAGE];  // per wave: [axis][slot]
   static_assert(ROPE_MAX_AXES * PAGE == 64, "a lane each");
   extern __shared__ __align__(16) double2 s_tab[];  // TAB: per wave [16][rot / 2]
@@ -619,13 +680,13 @@ __global__ __launch_bounds__(256, 4) void append_rope_own_kernel(PoolView P, int
     uint8_t* reg = P.fp8 + ph * fp8_region_bytes(D);
     float* sc = P.fp8_scales + ph * 2;
     const uint8_t* rows = reinterpret_cast<const uint8_t*>(k + ((int64_t)li * n_new_total + row0) * kts + (int64_t)h * D);
-    rope_quant_task<D, V, NEAR>(reg, sc, rows, kts, R, [&](int t, int j, int q) {
+    rope_quant_task<D, V, NEAR, NORM>(reg, sc, rows, kts, R, [&](int t, int j, int q) {
       if constexpr (TAB) return tab[t * m + q * (m / V) + j];
       const RopeEntry f = LT <= 64 ? en[q] : R.tab[V * j + q];  // (two passes a token: two entries a lane)
       double2 cs;
       rope_cos_sin((double)s_pos[wid][f.axis * PAGE + t] * f.freq, R.scale, cs.x, cs.y);
       return cs;
-    }, t0, t1, lane);
+    }, t0, t1, lane, NORM ? norm_weights(N, li, h) : nullptr, N.eps, N.add, s_rs[NORM ? wid : 0]);
     __builtin_amdgcn_wave_barrier();
     quant_task<D, true>(reg, sc, v + (int64_t)li * n_new_total * vts + (int64_t)h * D, row0, t0, t1, vts, lane);
   }
@@ -653,13 +714,14 @@ constexpr int STEP_APPEND_MAX_WAVES = 4096;
 // ROPE: the key tasks rotate their rows by the rows' positions before anything else reads
 // them (rows of k and v are kts and vts elements apart); the frequencies come in with round
 // trip 1, the positions with the rows.
-template <int D, bool ROPE>
+// NORM (with ROPE): the rows are normed first, the head's weights come in with round trip 1.
+template <int D, bool ROPE, bool NORM = false>
 __global__ __launch_bounds__(64) void append_step_kernel(PoolView P, int layer_sel, int n_lcall,
                                                          int n_req, int32_t* bt, uint8_t* tags,
                                                          int max_pages, const int32_t* sb,
                                                          const int32_t* cu, int n_new_total,
                                                          const uint16_t* k, const uint16_t* v, int64_t kts,
-                                                         int64_t vts, RopeView R, const int32_t* pos) {
+                                                         int64_t vts, RopeView R, const int32_t* pos, NormView N) {
   constexpr int RQ = STEP_APPEND_MAX_REQ / 64, EQ = STEP_APPEND_MAX_TOKENS / 64;
   __shared__ int s_base[STEP_APPEND_MAX_REQ + 1];  // first list entry of request r
   __shared__ int s_cu[STEP_APPEND_MAX_REQ], s_n[STEP_APPEND_MAX_REQ], s_s0[STEP_APPEND_MAX_REQ];
@@ -668,12 +730,20 @@ __global__ __launch_bounds__(64) void append_step_kernel(PoolView P, int layer_s
   __shared__ __align__(16) uint16_t s_rows[ROPE ? PAGE * D : 8];
   __shared__ RopeEntry s_freq[ROPE ? D / 2 : 1];
   __shared__ int s_pos[ROPE ? ROPE_MAX_AXES * PAGE : 1];  // [axis][slot of the page]
+  __shared__ uint16_t s_w[NORM ? D : 1];
+  __shared__ double s_rs[NORM ? PAGE : 1];
   const int lane = threadIdx.x;
   const int H = P.n_kv_heads;
   // ---- round trip 1: rows, starts, free-list top
   if constexpr (ROPE) {
     if (!(blockIdx.x & 1))  // a key task
       for (int i = lane; i < R.rot / 2; i += 64) s_freq[i] = R.tab[i];
+  }
+  if constexpr (NORM) {
+    const int lh = (int)((blockIdx.x >> 1) % (unsigned)(n_lcall * H));  // (as the task below)
+    const uint16_t* nw = norm_weights(N, lh / H, lh % H);
+    if (!(blockIdx.x & 1))
+      for (int c = lane; c < D; c += 64) s_w[c] = nw ? nw[c] : (uint16_t)0x3F80u;
   }
   const int top = P.ctrl[CTRL_FP8_TOP];
   int bad = (cu[0] != 0 || cu[n_req] != n_new_total) ? (int)MKV_DEVERR_RANGE : 0;
@@ -798,10 +868,14 @@ __global__ __launch_bounds__(64) void append_step_kernel(PoolView P, int layer_s
     if constexpr (ROPE)
       if (!T.kv) {  // while the old codes are on their way
         s_pos[lane] = at;
-        small_task_rotate<D>(T, R, s_rows, lane, [&](int tt, int i, double& c, double& s) {
+        auto cos_sin = [&](int tt, int i, double& c, double& s) {
           const RopeEntry e = s_freq[i];
           rope_cos_sin((double)s_pos[e.axis * PAGE + T.t0 + tt] * e.freq, R.scale, c, s);
-        });
+        };
+        if constexpr (NORM)
+          small_task_rotate<D, true>(T, R, s_rows, lane, cos_sin, N.eps, [&](int c) { return norm_weight(N, s_w[c]); }, s_rs);
+        else
+          small_task_rotate<D>(T, R, s_rows, lane, cos_sin);
       }
     small_task_run<D>(T, P, id, s_img, s_lut, lane);
   }
@@ -2141,10 +2215,10 @@ hipError_t launch_append(const PoolView& P, int layer, int n_req, int32_t* bt, u
     const int64_t ts = (int64_t)P.n_kv_heads * P.d;
     if (P.d == 256)
       hipLaunchKernelGGL((append_step_kernel<256, false>), dim3(grid), dim3(64), 0, s, P, layer, n_lcall,
-                         n_req, bt, tags, max_pages, sb, cu, n_new_total, k, v, ts, ts, RopeView{}, nullptr);
+                         n_req, bt, tags, max_pages, sb, cu, n_new_total, k, v, ts, ts, RopeView{}, nullptr, NormView{});
     else
       hipLaunchKernelGGL((append_step_kernel<128, false>), dim3(grid), dim3(64), 0, s, P, layer, n_lcall,
-                         n_req, bt, tags, max_pages, sb, cu, n_new_total, k, v, ts, ts, RopeView{}, nullptr);
+                         n_req, bt, tags, max_pages, sb, cu, n_new_total, k, v, ts, ts, RopeView{}, nullptr, NormView{});
     return hipGetLastError();
   }
   hipLaunchKernelGGL(append_plan_kernel, dim3(1), dim3(1024), 0, s, n_req, bt, tags, max_pages, sb,
@@ -2161,7 +2235,8 @@ hipError_t launch_append(const PoolView& P, int layer, int n_req, int32_t* bt, u
   return hipGetLastError();
 }
 
-hipError_t launch_append_rope(const PoolView& P, const RopeView& R, int layer, int n_req, int32_t* bt,
+template <bool NORM>
+static hipError_t append_rope(const PoolView& P, const RopeView& R, const NormView& N, int layer, int n_req, int32_t* bt,
                               uint8_t* tags, int max_pages, const int32_t* sb, const int32_t* cu,
                               int n_new_total, const int32_t* pos, const uint16_t* k, int64_t kts,
                               const uint16_t* v, int64_t vts, hipStream_t s) {
@@ -2171,11 +2246,11 @@ hipError_t launch_append_rope(const PoolView& P, const RopeView& R, int layer, i
       step_waves <= STEP_APPEND_MAX_WAVES) {
     const int grid = step_waves < 1 ? 1 : (int)step_waves;
     if (P.d == 256)
-      hipLaunchKernelGGL((append_step_kernel<256, true>), dim3(grid), dim3(64), 0, s, P, layer, n_lcall,
-                         n_req, bt, tags, max_pages, sb, cu, n_new_total, k, v, kts, vts, R, pos);
+      hipLaunchKernelGGL((append_step_kernel<256, true, NORM>), dim3(grid), dim3(64), 0, s, P, layer, n_lcall,
+                         n_req, bt, tags, max_pages, sb, cu, n_new_total, k, v, kts, vts, R, pos, N);
     else
-      hipLaunchKernelGGL((append_step_kernel<128, true>), dim3(grid), dim3(64), 0, s, P, layer, n_lcall,
-                         n_req, bt, tags, max_pages, sb, cu, n_new_total, k, v, kts, vts, R, pos);
+      hipLaunchKernelGGL((append_step_kernel<128, true, NORM>), dim3(grid), dim3(64), 0, s, P, layer, n_lcall,
+                         n_req, bt, tags, max_pages, sb, cu, n_new_total, k, v, kts, vts, R, pos, N);
     return hipGetLastError();
   }
   hipLaunchKernelGGL(append_plan_kernel, dim3(1), dim3(1024), 0, s, n_req, bt, tags, max_pages, sb,
@@ -2188,14 +2263,14 @@ hipError_t launch_append_rope(const PoolView& P, const RopeView& R, int layer, i
     const size_t own_lds = tab ? 4 * (size_t)PAGE * (R.rot / 2) * sizeof(double2) : 0;
     auto own = [&](auto kern) {
       hipLaunchKernelGGL(kern, dim3(og), dim3(256), own_lds, s, P, layer, n_lcall, sb, cu, n_new_total, k, v, kts, vts,
-                         R, pos);
+                         R, pos, N);
     };
     auto pick = [&](auto dc, auto vc) {
       constexpr int DD = decltype(dc)::value, VV = decltype(vc)::value;
       if (tab)
-        R.interleaved ? own(append_rope_own_kernel<DD, VV, true, true>) : own(append_rope_own_kernel<DD, VV, false, true>);
+        R.interleaved ? own(append_rope_own_kernel<DD, VV, true, true, NORM>) : own(append_rope_own_kernel<DD, VV, false, true, NORM>);
       else
-        R.interleaved ? own(append_rope_own_kernel<DD, VV, true, false>) : own(append_rope_own_kernel<DD, VV, false, false>);
+        R.interleaved ? own(append_rope_own_kernel<DD, VV, true, false, NORM>) : own(append_rope_own_kernel<DD, VV, false, false, NORM>);
     };
     auto of_v = [&](auto dc) {
       V == 4   ? pick(dc, std::integral_constant<int, 4>{})
@@ -2213,17 +2288,31 @@ hipError_t launch_append_rope(const PoolView& P, const RopeView& R, int layer, i
   const int hbi = (int)hb;
   auto go = [&](auto kern) {
     hipLaunchKernelGGL(kern, dim3(grid), dim3(256), lds, s, P, layer, n_lcall, hbi, sb, cu, n_new_total, k, v, kts,
-                       vts, R, pos);
+                       vts, R, pos, N);
   };
   if (P.d == 256)
-    V == 4   ? R.interleaved ? go(append_rope_quant_kernel<256, 4, true>) : go(append_rope_quant_kernel<256, 4, false>)
-    : V == 2 ? R.interleaved ? go(append_rope_quant_kernel<256, 2, true>) : go(append_rope_quant_kernel<256, 2, false>)
-    : R.interleaved ? go(append_rope_quant_kernel<256, 1, true>) : go(append_rope_quant_kernel<256, 1, false>);
+    V == 4   ? R.interleaved ? go(append_rope_quant_kernel<256, 4, true, NORM>) : go(append_rope_quant_kernel<256, 4, false, NORM>)
+    : V == 2 ? R.interleaved ? go(append_rope_quant_kernel<256, 2, true, NORM>) : go(append_rope_quant_kernel<256, 2, false, NORM>)
+    : R.interleaved ? go(append_rope_quant_kernel<256, 1, true, NORM>) : go(append_rope_quant_kernel<256, 1, false, NORM>);
   else
-    V == 4   ? R.interleaved ? go(append_rope_quant_kernel<128, 4, true>) : go(append_rope_quant_kernel<128, 4, false>)
-    : V == 2 ? R.interleaved ? go(append_rope_quant_kernel<128, 2, true>) : go(append_rope_quant_kernel<128, 2, false>)
-    : R.interleaved ? go(append_rope_quant_kernel<128, 1, true>) : go(append_rope_quant_kernel<128, 1, false>);
+    V == 4   ? R.interleaved ? go(append_rope_quant_kernel<128, 4, true, NORM>) : go(append_rope_quant_kernel<128, 4, false, NORM>)
+    : V == 2 ? R.interleaved ? go(append_rope_quant_kernel<128, 2, true, NORM>) : go(append_rope_quant_kernel<128, 2, false, NORM>)
+    : R.interleaved ? go(append_rope_quant_kernel<128, 1, true, NORM>) : go(append_rope_quant_kernel<128, 1, false, NORM>);
   return hipGetLastError();
+}
+
+hipError_t launch_append_rope(const PoolView& P, const RopeView& R, int layer, int n_req, int32_t* bt,
+                              uint8_t* tags, int max_pages, const int32_t* sb, const int32_t* cu,
+                              int n_new_total, const int32_t* pos, const uint16_t* k, int64_t kts,
+                              const uint16_t* v, int64_t vts, hipStream_t s) {
+  return append_rope<false>(P, R, NormView{}, layer, n_req, bt, tags, max_pages, sb, cu, n_new_total, pos, k, kts, v, vts, s);
+}
+
+hipError_t launch_append_norm_rope(const PoolView& P, const RopeView& R, const NormView& N, int layer, int n_req,
+                                   int32_t* bt, uint8_t* tags, int max_pages, const int32_t* sb, const int32_t* cu,
+                                   int n_new_total, const int32_t* pos, const uint16_t* k, int64_t kts, const uint16_t* v,
+                                   int64_t vts, hipStream_t s) {
+  return append_rope<true>(P, R, N, layer, n_req, bt, tags, max_pages, sb, cu, n_new_total, pos, k, kts, v, vts, s);
 }
 
 hipError_t launch_migrate(const PoolView& P, int n_req, int32_t* bt, uint8_t* tags, int max_pages,

@@ -92,6 +92,30 @@ __device__ __forceinline__ double rope_pos(const int32_t* pos, int64_t n, int64_
   return (double)(pos ? pos[(int64_t)axis * n + row] : at);
 }
 
+// Head norms: y_c = x_c r (w_c + add), r = 1 / sqrt(sum x^2 / d + eps), in fp64 like the
+// rotation that follows, so that a normed and rotated value is rounded once, too.  The squares
+// of bf16 values are exact and their sum is within 2^-45 of the true one in any order.
+struct NormView {
+  const uint16_t* w;    // bf16 weights, head h of layer l of the call at w + l layer + h head; null: ones (and add 0)
+  int64_t head, layer;  // elements, 0: the same
+  double eps, add;
+};
+
+__device__ __forceinline__ double norm_rstd(double sum, int d, double eps) {
+#pragma clang fp contract(off)
+  const double a = sum * (1.0 / d) + eps, h = 0.5 * a;  // (d is a power of two)
+  double y = __builtin_amdgcn_rsq(a);  // 2^-23 or better, squared by each step
+  y = __builtin_fma(y, __builtin_fma(-(h * y), y, 0.5), y);
+  y = __builtin_fma(y, __builtin_fma(-(h * y), y, 0.5), y);
+  return a == __builtin_inf() ? 0.0 : y;  // (an infinite value: the finite ones become zeros)
+}
+__device__ __forceinline__ const uint16_t* norm_weights(const NormView& N, int li, int h) {
+  return N.w ? N.w + li * N.layer + h * N.head : nullptr;
+}
+__device__ __forceinline__ double norm_weight(const NormView& N, uint16_t w) {
+  return (double)__uint_as_float((uint32_t)w << 16) + N.add;
+}
+
 // where the pair of frequency i sits
 __device__ __forceinline__ int2 rope_pair(const RopeView& R, int i) {
   return R.interleaved ? make_int2(2 * i, 2 * i + 1) : make_int2(i, i + R.rot / 2);
@@ -174,6 +198,23 @@ template <int V, class F>
 __device__ __forceinline__ void rope_turn(float* x, bool interleaved, F cos_sin) {
   if (interleaved) rope_turn<V, true>(x, cos_sin);
   else rope_turn<V, false>(x, cos_sin);
+}
+
+// the same of values in fp64 (normed ones): rounded into x, turned where `turn`
+template <int V, bool NEAR, class F>
+__device__ __forceinline__ void rope_turn_f64(const double* y, float* x, bool turn, F cos_sin) {
+#pragma unroll
+  for (int q = 0; q < V; ++q) {
+    constexpr int step = NEAR ? 2 : 1, other = NEAR ? 1 : V;
+    double y0 = y[step * q], y1 = y[step * q + other];
+    if (turn) {
+      const double2 cs = cos_sin(q);
+      const double x0 = y0, x1 = y1;
+      rope_rotate(x0, x1, cs.x, cs.y, y0, y1);
+    }
+    x[step * q] = f64_round_bf16(y0);
+    x[step * q + other] = f64_round_bf16(y1);
+  }
 }
 
 }  // namespace mkv

@@ -1,8 +1,11 @@
 // Rotation of bf16 rows by their tokens' positions (queries; keys where the caller keeps
-// them elsewhere).  See mkv_rope.h for the mathematics and the precision.
+// them elsewhere), alone or behind a norm of every head.  See mkv_rope.h for the mathematics and the precision.
 #include <hip/hip_runtime.h>
 
+#include <type_traits>
+
 #include "mkv_internal.h"
+#include "mkv_norm.h"
 #include "mkv_rope.h"
 
 namespace mkv {
@@ -65,6 +68,104 @@ __global__ __launch_bounds__(256) void rope_apply_kernel(RopeView R, int64_t t0,
   }
 }
 
+// rope_apply_kernel with every head normed and weighted first.  The lanes of a row add up its
+// squares over lane exchanges; U = 2 where a row has more lanes than a wave (d = 256, pairs of
+// one): a lane then holds two of them.
+template <int D, int V, bool NEAR>
+__global__ __launch_bounds__(256, 4) void norm_rope_apply_kernel(RopeView R, NormView N, int64_t t0, int n_here, int n_tokens,
+                                                              int n_heads, int hb, const uint16_t* x, int64_t xs,
+                                                              const int32_t* pos, uint16_t* out, int64_t os) {
+  typedef typename RopeGroup<V>::type group;
+  constexpr int U = D / (2 * V) > 64 ? 2 : 1, LT = D / (2 * V) / U, HU = 4 / U;
+  const int nb = (n_heads + hb - 1) / hb;
+  const int64_t unit = (int64_t)blockIdx.x * (256 / LT) + threadIdx.x / LT;
+  if (unit >= (int64_t)n_here * nb) return;  // (all lanes of a row, so exchanges stay among those that are here)
+  const int lane = threadIdx.x & 63, j = threadIdx.x % LT;
+  const int64_t tu = unit / nb, t = t0 + tu;
+  const int h0 = (int)(unit - tu * nb) * hb, h1 = min(h0 + hb, n_heads);
+  int ca[U], cb[U];
+  bool turn[U];
+  double c[U][V], s[U][V];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    turn[u] = rope_lane<V>(R, j + u * LT, ca[u], cb[u]);
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      c[u][i] = 1.0;
+      s[u][i] = 0.0;
+      if (turn[u]) {
+        const RopeEntry e = R.tab[V * (j + u * LT) + i];
+        rope_cos_sin((double)pos[(int64_t)e.axis * n_tokens + t] * e.freq, R.scale, c[u][i], s[u][i]);
+      }
+    }
+  }
+  const uint16_t* xr = x + t * xs;
+  uint16_t* orow = out + t * os;
+  uint32_t ww[U][V];  // the weights of a head, of every head where they are the same
+  auto load_w = [&](int h) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+#pragma unroll
+      for (int q = 0; q < V; ++q) ww[u][q] = 0x3F803F80u;  // ones
+      if (N.w)
+        rope_words(*reinterpret_cast<const group*>(N.w + h * N.head + ca[u]),
+                   *reinterpret_cast<const group*>(N.w + h * N.head + cb[u]), ww[u]);
+    }
+  };
+  if (!N.head) load_w(0);
+  for (int hu = h0; hu < h1; hu += HU) {
+    uint32_t w[HU][U][V];
+#pragma unroll
+    for (int k = 0; k < HU; ++k)
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const uint16_t* xh = xr + (int64_t)min(hu + k, h1 - 1) * D;
+        rope_words(*reinterpret_cast<const group*>(xh + ca[u]), *reinterpret_cast<const group*>(xh + cb[u]), w[k][u]);
+      }
+    double rs[HU];
+#pragma unroll
+    for (int k = 0; k < HU; ++k) {
+      rs[k] = 0.0;
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        float v[2 * V];
+        rope_unpack<V>(w[k][u], v);
+#pragma unroll
+        for (int i = 0; i < 2 * V; ++i) rs[k] = __builtin_fma((double)v[i], (double)v[i], rs[k]);
+        // (the words are read again below: the values in fp64 would fill the registers)
+#pragma unroll
+        for (int q = 0; q < V; ++q) asm volatile("" : "+v"(w[k][u][q]));
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < HU; ++k) rs[k] = norm_rstd(row_sum<LT>(rs[k], lane), D, N.eps);
+#pragma unroll
+    for (int k = 0; k < HU; ++k) {
+      if (hu + k >= h1) break;
+      if (N.head) load_w(hu + k);
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        float v[2 * V], f[2 * V];
+        rope_unpack<V>(w[k][u], v);
+#pragma unroll
+        for (int q = 0; q < V; ++q) asm volatile("" : "+v"(ww[u][q]));
+        rope_unpack<V>(ww[u], f);
+        double y[2 * V];
+#pragma unroll
+        for (int i = 0; i < 2 * V; ++i) y[i] = (double)v[i] * rs[k] * ((double)f[i] + N.add);
+        rope_turn_f64<V, NEAR>(y, v, turn[u], [&](int i) { return make_double2(c[u][i], s[u][i]); });
+        rope_pack<V>(v, w[k][u]);
+        group a, b;
+        rope_groups<V>(w[k][u], a, b);
+        uint16_t* oh = orow + (int64_t)(hu + k) * D;
+        *reinterpret_cast<group*>(oh + ca[u]) = a;
+        *reinterpret_cast<group*>(oh + cb[u]) = b;
+      }
+      __builtin_amdgcn_sched_barrier(0);  // one head at a time: bounded register use
+    }
+  }
+}
+
 hipError_t launch_rope_apply(const RopeView& R, int d, int n_tokens, int n_heads, const uint16_t* x, int64_t xs,
                              const int32_t* pos, uint16_t* out, int64_t os, hipStream_t s) {
   // heads per lane group: all of them once that fills the chip (eight waves per SIMD), so
@@ -87,6 +188,33 @@ hipError_t launch_rope_apply(const RopeView& R, int d, int n_tokens, int n_heads
     V == 4 ? go(rope_apply_kernel<256, 4>) : V == 2 ? go(rope_apply_kernel<256, 2>) : go(rope_apply_kernel<256, 1>);
   else
     V == 4 ? go(rope_apply_kernel<128, 4>) : V == 2 ? go(rope_apply_kernel<128, 2>) : go(rope_apply_kernel<128, 1>);
+  return hipGetLastError();
+}
+
+hipError_t launch_norm_rope_apply(const RopeView& R, const NormView& N, int d, int n_tokens, int n_heads, const uint16_t* x,
+                                  int64_t xs, const int32_t* pos, uint16_t* out, int64_t os, hipStream_t s) {
+  // (lane groups and launches as launch_rope_apply's)
+  const int V = rope_width(R.rot), lt = d / (2 * V) > 64 ? 64 : d / (2 * V), per = 256 / lt;
+  int64_t nb = ((int64_t)8192 * 64 / lt + n_tokens - 1) / n_tokens;
+  if (nb > n_heads) nb = n_heads;
+  const int hb = (int)((n_heads + nb - 1) / nb);
+  auto go = [&](auto kern) {
+    for (int64_t t0 = 0; t0 < n_tokens; t0 += 1 << 22) {
+      const int n_here = (int)(n_tokens - t0 < 1 << 22 ? n_tokens - t0 : 1 << 22);
+      const int64_t units = (int64_t)n_here * ((n_heads + hb - 1) / hb);
+      hipLaunchKernelGGL(kern, dim3((unsigned)((units + per - 1) / per)), dim3(256), 0, s, R, N, t0, n_here, n_tokens,
+                         n_heads, hb, x, xs, pos, out, os);
+    }
+  };
+  auto pick = [&](auto dc, auto vc) {
+    constexpr int DD = decltype(dc)::value, VV = decltype(vc)::value;
+    R.interleaved ? go(norm_rope_apply_kernel<DD, VV, true>) : go(norm_rope_apply_kernel<DD, VV, false>);
+  };
+  auto of_v = [&](auto dc) {
+    V == 4   ? pick(dc, std::integral_constant<int, 4>{})
+    : V == 2 ? pick(dc, std::integral_constant<int, 2>{}) : pick(dc, std::integral_constant<int, 1>{});
+  };
+  d == 256 ? of_v(std::integral_constant<int, 256>{}) : of_v(std::integral_constant<int, 128>{});
   return hipGetLastError();
 }
 
