@@ -302,7 +302,7 @@ def prepare(case, seed):
         s["axis"] = s["axis"].long()
         if own:
             import paper_2608_23834_amd as mk
-            s["nq"], s["nk"] = _norm(c, s["wq"]), _norm(c, s["wk"])
+            s["norm_q"], s["norm_k"] = _norm(c, s["wq"]), _norm(c, s["wk"])
             s["rope"] = mk.Rope(d, *_turn(c), c["axes"], interleaved=c["pairs"] == "neighbours", scale=1.0) if c["rot"] else None
     if kind == "rows":
         n = sum(lens)
@@ -384,16 +384,16 @@ def run(state):
     if own:
         import paper_2608_23834_amd as mk
         if kind == "rows":
-            mk.kv_norm_rope_apply(s["rope"], s["nq"], _bits(s["x"]), s["pos"] if s["rope"] else None, _bits(s["out"]))
+            mk.kv_norm_rope_apply(s["rope"], s["norm_q"], _bits(s["x"]), s["pos"] if s["rope"] else None, _bits(s["out"]))
         elif kind == "append":
-            mk.kv_append_fp8_norm_rope(s["pool"], s["rope"], s["nk"], -1, s["bt"], s["tags"], s["before"], s["cu"],
+            mk.kv_append_fp8_norm_rope(s["pool"], s["rope"], s["norm_k"], -1, s["bt"], s["tags"], s["before"], s["cu"],
                                        s["pos"] if s["rope"] else None, _bits(s["k"]), _bits(s["v"]))
         elif kind == "decode":
             mk.paged_attn_decode_shaped(s["pool"], s["shaping"], 0, _bits(s["q"]), s["bt"], s["tags"], s["seq"],
                                         s["out"], s["lse"], s["ws"])
         elif kind == "step":
-            mk.paged_attn_decode_append_shaped(s["pool"], s["shaping"], s["rope"], s["nq"], s["nk"], 0, _bits(s["q"]),
-                                               _bits(s["k"][0]), _bits(s["v"][0]), s["pos"] if s["rope"] else None,
+            mk.paged_attn_decode_append_shaped(s["pool"], s["shaping"], s["rope"], s["norm_q"], s["norm_k"], 0,
+                                               _bits(s["q"]), _bits(s["k"][0]), _bits(s["v"][0]), s["pos"] if s["rope"] else None,
                                                s["bt"], s["tags"], s["before"], s["out"], s["lse"], s["ws"])
         elif kind == "chunk":
             mk.paged_attn_chunk_shaped(s["pool"], s["shaping"], 0, _bits(s["q"]), s["cu"], s["bt"], s["tags"], s["seq"],
