@@ -535,7 +535,8 @@ __device__ __forceinline__ void rope_quant_task(uint8_t* reg, float* sc, const u
       const double r = s_rs[ts];
 #pragma unroll
       for (int b = 0; b < 2 * V; ++b) y[b] = (double)x[b] * r * ((double)f[b] + add);
-      rope_turn_f64<V, NEAR>(y, x, j < m / V, [&](int q) { return cos_sin(t, j, q); });
+      const int jt = min(j, max(m / V - 1, 0));  // (asked for every channel, used for the turned ones)
+      rope_turn_f64<V, NEAR>(y, x, j < m / V, [&](int q) { return cos_sin(t, jt, q); });
     } else {
       if (j < m / V) rope_turn<V, NEAR>(x, [&](int q) { return cos_sin(t, j, q); });
     }
@@ -2260,7 +2261,7 @@ static hipError_t append_rope(const PoolView& P, const RopeView& R, const NormVi
   if (lh < 4) {
     const int og = grid_for((pages_bound * lh + 3) / 4, 4096);
     const bool tab = 4 * R.rot <= P.d;
-    const size_t own_lds = tab ? 4 * (size_t)PAGE * (R.rot / 2) * sizeof(double2) : 0;
+    const size_t own_lds = tab ? 4 * (size_t)PAGE * max(1, R.rot / 2) * sizeof(double2) : 0;
     auto own = [&](auto kern) {
       hipLaunchKernelGGL(kern, dim3(og), dim3(256), own_lds, s, P, layer, n_lcall, sb, cu, n_new_total, k, v, kts, vts,
                          R, pos, N);
@@ -2284,7 +2285,8 @@ static hipError_t append_rope(const PoolView& P, const RopeView& R, const NormVi
   int64_t hb = pages_bound * lh / 1024 / 4 * 4;
   hb = hb < 4 ? 4 : hb > 32 ? 32 : hb;
   const int grid = grid_for(pages_bound * ((lh + hb - 1) / hb), 4096);
-  const size_t lds = (size_t)PAGE * (R.rot / 2) * sizeof(double2);
+  // (one entry where nothing is turned: it is read, though not used)
+  const size_t lds = (size_t)max(1, PAGE * (R.rot / 2)) * sizeof(double2);
   const int hbi = (int)hb;
   auto go = [&](auto kern) {
     hipLaunchKernelGGL(kern, dim3(grid), dim3(256), lds, s, P, layer, n_lcall, hbi, sb, cu, n_new_total, k, v, kts,
