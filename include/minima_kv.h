@@ -428,6 +428,47 @@ mkv_status paged_attn_decode_sparse(mkv_pool* pool, int32_t layer, int32_t n_req
                                     const int32_t* pages, const int32_t* counts, float* out,
                                     float* lse, void* ws, size_t ws_bytes, hipStream_t stream);
 
+/* Attention with other scores and other masks.  With p the position of a query and t
+ * that of a key,
+ *     s(p, t) = C(scale q.k_t) - slopes[hq] |p - t|,   C(x) = cap tanh(x / cap),
+ * over the tokens t that the query sees,
+ *     t >= max(p - window + 1, first_keys[row])  and  t <= p, or t < prefix_lens[r] where
+ *     p < prefix_lens[r] (a prefix seen from both sides),
+ * and below the sequence's end; every head's sink logit takes its share of the softmax as a
+ * token without a value: out = sum e^s v / (e^sink + sum e^s).  A query that sees no token has
+ * zero outputs, its lse is the sink (-inf without one).  The struct is read during the call,
+ * the device arrays when the kernels run (a captured call bakes in the rest of the struct).
+ *  - paged_attn_decode_shaped is paged_attn_decode with them, rows = requests; prefix_lens is
+ *    not read (a query at the end sees the whole prefix).  Pages wholly outside the window, or
+ *    before first_keys, are not read (nor checked).  Outputs carry the error of fp32 arithmetic, as
+ *    paged_attn_decode_append_rope's do.  Buffers, workspace and errors as paged_attn_decode.
+ *  - paged_attn_decode_append_shaped is paged_attn_decode_append_rope with them, and with the
+ *    query and key heads normed before the rotation (q_norm, k_norm, each may be NULL: not
+ *    normed; rope NULL: not rotated).  The appended token is stored whether or not its query
+ *    sees it.  State afterwards as by kv_append_fp8_norm_rope.
+ * Errors also: EINVAL (shaping NULL, window negative), ERANGE (cap neither 0 nor in [1e-6, 1e6],
+ * scale neither 0 nor in [1e-6, 1e6]).  Slopes and sinks are finite, or a sink -inf. */
+typedef struct paged_attn_shaping {
+  float scale;                /* softmax scale; 0: 1 / sqrt(head_dim) */
+  float cap;                  /* 0: none */
+  int32_t window;             /* 0: all */
+  const float* slopes;        /* device fp32 [n_q_heads] or NULL */
+  const float* sinks;         /* device fp32 [n_q_heads] or NULL */
+  const int32_t* first_keys;  /* device int32, one per query row, or NULL */
+  const int32_t* prefix_lens; /* device int32 [n_req] or NULL */
+} paged_attn_shaping;
+mkv_status paged_attn_decode_shaped(mkv_pool* pool, const paged_attn_shaping* shaping, int32_t layer,
+                                    int32_t n_req, const uint16_t* q, const int32_t* block_table,
+                                    const uint8_t* tags, int32_t max_pages, const int32_t* seq_lens,
+                                    float* out, float* lse, void* ws, size_t ws_bytes, hipStream_t stream);
+mkv_status paged_attn_decode_append_shaped(mkv_pool* pool, const paged_attn_shaping* shaping,
+                                           const kv_rope* rope, const kv_head_norm* q_norm,
+                                           const kv_head_norm* k_norm, int32_t layer, int32_t n_req,
+                                           const uint16_t* q, const uint16_t* k_new, const uint16_t* v_new,
+                                           const int32_t* positions, int32_t* block_table, uint8_t* tags,
+                                           int32_t max_pages, const int32_t* seq_lens_before, float* out,
+                                           float* lse, void* ws, size_t ws_bytes, hipStream_t stream);
+
 /* The cache read back: bf16 K and V rows of positions from[r] .. from[r] + n_r - 1 of
  * every request, n_r = cu_tokens[r+1] - cu_tokens[r], as rows cu_tokens[r] .. of k and v
  * (device int32 [n_req] and [n_req+1], cu[0] = 0, cu[n_req] = n_total).  A value is the one

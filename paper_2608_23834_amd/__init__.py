@@ -37,7 +37,8 @@ EXPORTS = ["kv_pool_bytes", "kv_pool_create", "kv_pool_destroy", "kv_append_fp8"
            "kv_rope_bytes", "kv_rope_create", "kv_rope_destroy", "kv_rope_apply", "kv_append_fp8_rope",
            "paged_attn_decode_append_rope", "kv_page_bounds_bytes", "kv_page_bounds_update",
            "paged_attn_select_workspace_bytes", "paged_attn_select_pages", "paged_attn_decode_sparse",
-           "kv_read_tokens", "kv_norm_rope_apply", "kv_append_fp8_norm_rope", "mkv_status_string"]
+           "kv_read_tokens", "kv_norm_rope_apply", "kv_append_fp8_norm_rope",
+           "paged_attn_decode_shaped", "paged_attn_decode_append_shaped", "mkv_status_string"]
 
 _lib = None
 
@@ -70,6 +71,12 @@ class RopeDesc(ctypes.Structure):
 class HeadNormDesc(ctypes.Structure):
     _fields_ = [("head_dim", ctypes.c_int32), ("eps", ctypes.c_double), ("add", ctypes.c_double),
                 ("weight", ctypes.c_void_p), ("head_stride", ctypes.c_int64), ("layer_stride", ctypes.c_int64)]
+
+
+class ShapingDesc(ctypes.Structure):
+    _fields_ = [("scale", ctypes.c_float), ("cap", ctypes.c_float), ("window", ctypes.c_int32),
+                ("slopes", ctypes.c_void_p), ("sinks", ctypes.c_void_p), ("first_keys", ctypes.c_void_p),
+                ("prefix_lens", ctypes.c_void_p)]
 
 
 class Counters(ctypes.Structure):
@@ -138,6 +145,9 @@ def lib() -> ctypes.CDLL:
         L.paged_attn_decode_sparse.argtypes = [vp, i32, i32, vp, vp, vp, i32, vp, i32, vp, vp, vp, vp, vp, sz, vp]
         L.kv_norm_rope_apply.argtypes = [vp, vp, i32, i32, vp, i64, vp, vp, i64, vp]
         L.kv_append_fp8_norm_rope.argtypes = [vp, vp, vp, i32, i32, vp, vp, i32, vp, vp, i32, vp, vp, i64, vp, i64, vp]
+        L.paged_attn_decode_shaped.argtypes = [vp, vp, i32, i32, vp, vp, vp, i32, vp, vp, vp, vp, sz, vp]
+        L.paged_attn_decode_append_shaped.argtypes = [vp, vp, vp, vp, vp, i32, i32, vp, vp, vp, vp, vp, vp, i32, vp, vp,
+                                                      vp, vp, sz, vp]
         L.kv_read_tokens.argtypes = [vp, i32, i32, vp, vp, i32, vp, vp, i32, vp, i64, vp, i64, vp]
         L.mkv_control_bf16_write.argtypes = [vp, i32, i32, i32, i32, i32, i32, vp, i32, vp, vp, i32,
                                              vp, vp, vp]
@@ -676,6 +686,76 @@ def paged_attn_decode_sparse(pool: Pool, layer, q, block_table, tags, seq_lens, 
         pool.handle, layer, n_req, q.data_ptr(), block_table.data_ptr(), tags.data_ptr(), max_pages,
         seq_lens.data_ptr(), pages.shape[2], pages.data_ptr(), counts.data_ptr(), out.data_ptr(), _ptr(lse),
         ws.data_ptr(), ws.nbytes, cur if stream is None else stream.cuda_stream))
+
+
+class Shaping:
+    """Scores and masks of shaped attention (paged_attn_shaping): softmax scale (0: 1 / sqrt(head_dim)),
+    cap of the scores by a tanh (0: none), window of visible tokens (0: all), and device tensors or None:
+    slopes float32 [n_q_heads] (bias -slope * distance), sinks float32 [n_q_heads], first_keys int32 [rows]
+    (first token each query row sees), prefix_lens int32 [n_req] (tokens seen from both sides; chunks)."""
+
+    def __init__(self, scale=0.0, cap=0.0, window=0, slopes=None, sinks=None, first_keys=None, prefix_lens=None):
+        self.scale, self.cap, self.window = scale, cap, window
+        self.slopes, self.sinks, self.first_keys, self.prefix_lens = slopes, sinks, first_keys, prefix_lens
+
+    def _desc(self, dev, n_q_heads, rows, n_req):
+        _, i32, f32 = _types()
+        for t, n, types in ((self.slopes, n_q_heads, f32), (self.sinks, n_q_heads, f32), (self.first_keys, rows, i32),
+                            (self.prefix_lens, n_req, i32)):
+            if t is not None and (t.get_device() != dev or t.dtype not in types or t.numel() < n or not t.is_contiguous()):
+                raise ValueError("slopes and sinks are float32 [n_q_heads], first_keys int32 [rows], prefix_lens int32 "
+                                 "[n_req], contiguous and on the current device")
+        return ShapingDesc(self.scale, self.cap, self.window, _ptr(self.slopes), _ptr(self.sinks), _ptr(self.first_keys),
+                           _ptr(self.prefix_lens))
+
+
+def paged_attn_decode_shaped(pool: Pool, shaping: Shaping, layer, q, block_table, tags, seq_lens, out, lse, ws,
+                             stream=None):
+    """paged_attn_decode with shaped scores and masks."""
+    dev, cur = _current()
+    rows, i32, f32 = _types()
+    n_req, max_pages = _table(dev, pool, block_table, tags, i32)
+    _here(dev, q, seq_lens, out, lse, ws)
+    if not (q.dtype in rows and seq_lens.dtype in i32 and out.dtype in f32 and (lse is None or lse.dtype in f32)):
+        raise ValueError(_WRONG_TYPE)
+    qs = (n_req, pool.n_q_heads, pool.d)
+    if q.shape != qs or out.shape != qs:
+        _sizes((q, qs), (out, qs))
+    if seq_lens.numel() < n_req or (lse is not None and lse.numel() < qs[0] * qs[1]):
+        raise ValueError("seq_lens is [n_req], lse [n_req][n_q_heads]")
+    desc = shaping._desc(dev, pool.n_q_heads, n_req, n_req)
+    _check("paged_attn_decode_shaped", lib().paged_attn_decode_shaped(
+        pool.handle, ctypes.byref(desc), layer, n_req, q.data_ptr(), block_table.data_ptr(), tags.data_ptr(), max_pages,
+        seq_lens.data_ptr(), out.data_ptr(), _ptr(lse), ws.data_ptr(), ws.nbytes,
+        cur if stream is None else stream.cuda_stream))
+
+
+def paged_attn_decode_append_shaped(pool: Pool, shaping: Shaping, rope, q_norm, k_norm, layer, q, k_new, v_new, positions,
+                                    block_table, tags, seq_lens_before, out, lse, ws, stream=None):
+    """A decode step of one layer: query and key heads normed (q_norm, k_norm: HeadNorm or None) and rotated
+    (rope or None), the token appended, attention with shaped scores; positions as in
+    paged_attn_decode_append_rope."""
+    dev, cur = _current()
+    rows, i32, f32 = _types()
+    n_req, max_pages = _table(dev, pool, block_table, tags, i32)
+    _here(dev, q, k_new, v_new, seq_lens_before, out, lse, ws)
+    if not (q.dtype in rows and k_new.dtype in rows and v_new.dtype in rows and seq_lens_before.dtype in i32
+            and out.dtype in f32 and (lse is None or lse.dtype in f32)):
+        raise ValueError(_WRONG_TYPE)
+    qs, ks = (n_req, pool.n_q_heads, pool.d), (n_req, pool.n_kv_heads, pool.d)
+    if q.shape != qs or out.shape != qs or k_new.shape != ks or v_new.shape != ks:
+        _sizes((q, qs), (out, qs), (k_new, ks), (v_new, ks))
+    if seq_lens_before.numel() < n_req or (lse is not None and lse.numel() < qs[0] * qs[1]):
+        raise ValueError("seq_lens_before is [n_req], lse [n_req][n_q_heads]")
+    desc = shaping._desc(dev, pool.n_q_heads, n_req, n_req)
+    qd = None if q_norm is None else q_norm._desc(pool.n_q_heads, 1, dev)
+    kd = None if k_norm is None else k_norm._desc(pool.n_kv_heads, 1, dev)
+    _check("paged_attn_decode_append_shaped", lib().paged_attn_decode_append_shaped(
+        pool.handle, ctypes.byref(desc), None if rope is None else rope.handle, None if qd is None else ctypes.byref(qd),
+        None if kd is None else ctypes.byref(kd), layer, n_req, q.data_ptr(), k_new.data_ptr(), v_new.data_ptr(),
+        None if rope is None else _positions(dev, rope, positions, n_req), block_table.data_ptr(), tags.data_ptr(),
+        max_pages, seq_lens_before.data_ptr(), out.data_ptr(), _ptr(lse), ws.data_ptr(), ws.nbytes,
+        cur if stream is None else stream.cuda_stream))
 
 
 def kv_read_tokens(pool: Pool, layer, block_table, tags, seq_from, cu_tokens, k, v, stream=None):

@@ -610,6 +610,76 @@ mkv_status paged_attn_select_pages(mkv_pool* pool, int32_t layer, int32_t n_req,
                                   n_first, n_last, pages, counts, ws, stream));
 }
 
+static mkv_status check_shaping(const paged_attn_shaping* sh, ShapeView* v) {
+  if (!sh || sh->window < 0) return MKV_EINVAL;
+  auto in = [](float x) { return x == 0.0f || (x >= 1e-6f && x <= 1e6f); };
+  if (!in(sh->cap) || !in(sh->scale)) return MKV_ERANGE;  // (NaN too)
+  v->cap = sh->cap * LOG2E_F;
+  v->icap = sh->cap != 0.0f ? 1.0f / v->cap : 0.0f;
+  v->scale = sh->scale;
+  v->window = sh->window;
+  v->slopes = sh->slopes;
+  v->sinks = sh->sinks;
+  v->first = sh->first_keys;
+  v->prefix = sh->prefix_lens;
+  return MKV_OK;
+}
+
+static mkv_status decode_shaped(mkv_pool* pool, const ShapeView& v, int32_t layer, int32_t n_req, const uint16_t* q,
+                                const int32_t* block_table, const uint8_t* tags, int32_t max_pages,
+                                const int32_t* seq_lens, float* out, float* lse, void* ws, size_t ws_bytes,
+                                hipStream_t stream, const uint16_t* k_new, const uint16_t* v_new, int32_t* bt_w,
+                                uint8_t* tags_w, const RopeView* rope, const int32_t* positions, const NormView* qn,
+                                const NormView* kn) {
+  if (!q || !block_table || !tags || !seq_lens || !out || !ws) return MKV_EINVAL;
+  if (n_req < 1 || max_pages < 1) return MKV_EINVAL;
+  if (!aligned16(q) || !aligned16(out) || !aligned16(ws)) return MKV_EINVAL;
+  if (layer < 0 || layer >= pool->n_layers) return MKV_ERANGE;
+  if (n_req > 65535 || max_pages > 1024 * 256) return MKV_ERANGE;
+  if (ws_bytes < decode_ws_bytes(n_req, decode_see(max_pages, v.window), pool->n_kv_heads, pool->group, pool->d, pool->recent))
+    return MKV_ENOMEM;
+  mkv_status st = hip_status(launch_decode(view_of(pool), layer, n_req, q, block_table, tags, max_pages, seq_lens, out, lse,
+                                           ws, stream, pool->timing ? pool->timing_ev : nullptr, k_new, v_new, bt_w, tags_w,
+                                           nullptr, rope, positions, nullptr, nullptr, 0, &v, qn, kn));
+  if (st == MKV_OK) {
+    pool->decode_routes++;
+    if (pool->timing) pool->timed = 1;
+  }
+  return st;
+}
+
+mkv_status paged_attn_decode_shaped(mkv_pool* pool, const paged_attn_shaping* shaping, int32_t layer, int32_t n_req,
+                                    const uint16_t* q, const int32_t* block_table, const uint8_t* tags, int32_t max_pages,
+                                    const int32_t* seq_lens, float* out, float* lse, void* ws, size_t ws_bytes,
+                                    hipStream_t stream) {
+  ShapeView v;
+  if (!pool) return MKV_EINVAL;
+  mkv_status st = check_shaping(shaping, &v);
+  if (st != MKV_OK) return st;
+  return decode_shaped(pool, v, layer, n_req, q, block_table, tags, max_pages, seq_lens, out, lse, ws, ws_bytes, stream,
+                       nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr);
+}
+
+mkv_status paged_attn_decode_append_shaped(mkv_pool* pool, const paged_attn_shaping* shaping, const kv_rope* rope,
+                                           const kv_head_norm* q_norm, const kv_head_norm* k_norm, int32_t layer,
+                                           int32_t n_req, const uint16_t* q, const uint16_t* k_new, const uint16_t* v_new,
+                                           const int32_t* positions, int32_t* block_table, uint8_t* tags,
+                                           int32_t max_pages, const int32_t* seq_lens_before, float* out, float* lse,
+                                           void* ws, size_t ws_bytes, hipStream_t stream) {
+  ShapeView v;
+  NormView qn, kn;
+  if (!pool || !k_new || !v_new || (rope && rope->head_dim != pool->d)) return MKV_EINVAL;
+  mkv_status st = check_shaping(shaping, &v);
+  if (st == MKV_OK && q_norm) st = check_norm(q_norm, rope, pool->d, &qn);
+  if (st == MKV_OK && k_norm) st = check_norm(k_norm, rope, pool->d, &kn);
+  if (st != MKV_OK) return st;
+  if ((reinterpret_cast<uintptr_t>(k_new) | reinterpret_cast<uintptr_t>(v_new)) & 7) return MKV_EINVAL;
+  const RopeView rv = rope ? rope->view : no_rope();
+  return decode_shaped(pool, v, layer, n_req, q, block_table, tags, max_pages, seq_lens_before, out, lse, ws, ws_bytes,
+                       stream, k_new, v_new, block_table, tags, &rv, rope ? positions : nullptr, q_norm ? &qn : nullptr,
+                       k_norm ? &kn : nullptr);
+}
+
 mkv_status kv_read_tokens(mkv_pool* pool, int32_t layer, int32_t n_req, const int32_t* block_table,
                           const uint8_t* tags, int32_t max_pages, const int32_t* from, const int32_t* cu_tokens,
                           int32_t n_total, uint16_t* k, int64_t k_stride, uint16_t* v, int64_t v_stride,

@@ -37,8 +37,10 @@
 // of one token per request into the launch; SCORE also records every page's
 // local softmax mass for the attention-score collector; ROPE (with APP) turns
 // the query and the new key by the token's positions on their way in; SPARSE
-// takes each KV head's pages from a list instead of the whole table.  The last
-// two answer with fp32's error (FINE, below).  24 / 4 heads, d = 256, window 1,024:
+// takes each KV head's pages from a list instead of the whole table; SHAPE caps
+// and biases the scores and hides the tokens outside a window or a document, whose
+// pages it does not read (with APP and ROPE: the query and key heads are normed,
+// too, where asked).  The last three answer with fp32's error (FINE, below).  24 / 4 heads, d = 256, window 1,024:
 // ROPE, 8 requests of 12,001 to 20,011 tokens (144 MB, 27.8 us of a copy's bandwidth):
 // 40.0 us a call, 4 of them the merge; SPARSE, 256 pages of each of 32 longer ones (170 MB,
 // 33.0 us): 41.3.
@@ -53,6 +55,7 @@
 #include "mkv_attn.h"
 #include "mkv_internal.h"
 #include "mkv_rope.h"
+#include "mkv_shape.h"
 #include "../../include/minima_kv.h"
 
 namespace mkv {
@@ -123,6 +126,12 @@ struct DecodeArgs {
   const int32_t* sel;
   const int32_t* sel_count;
   int n_sel;
+  // SHAPE instance: the scores' shape; pages of the table that a request can see at most, from the
+  // one that holds the first token it sees.  With APP: norms of the query (bit 0 of `norm`) and key
+  // heads (bit 1)
+  ShapeView shape;
+  int n_see, norm;
+  NormView qn, kn;
 };
 
 // Cost of a request's pages: n_old pages wholly outside the Recent window and
@@ -172,6 +181,10 @@ DecodeShape decode_shape(int n_req, int max_pages, int n_kv_heads, int recent, i
   s.cunits = (int)u;
   s.max_chunks = (int)((tmax + u - 1) / u);
   return s;
+}
+// pages that a query with a window can see at most (its tokens may begin and end inside a page)
+int decode_see(int max_pages, int window) {
+  return window > 0 && window / PAGE + 2 < max_pages ? window / PAGE + 2 : max_pages;
 }
 // workspace: the partials, one (O_j[G][d], m_j[G], l_j[G]) block per chunk
 // slot, padded to a multiple of 4 floats (16-byte aligned O rows); every slot
@@ -308,12 +321,14 @@ __device__ __forceinline__ void p_operand(const float* p, bool row_is_b, half8& 
 // columns [0, 8) scoring page a and [8, 16) page b.  G6: at most six heads
 // (see head_of_col).
 // ROPE, SPARSE: see DecodeArgs.
-template <int D, bool PAIR, bool G6, bool APP, bool SCORE = false, bool ROPE = false, bool SPARSE = false>
+template <int D, bool PAIR, bool G6, bool APP, bool SCORE = false, bool ROPE = false, bool SPARSE = false,
+          bool SHAPE = false>
 __global__ __launch_bounds__(DecodeCfg<PAIR>::NT, PAIR && D == 128 ? 4 : 2) void decode_kernel(DecodeArgs a) {
   static_assert(!(APP && SCORE), "the scoring instance has no fused append");
   static_assert(APP || !ROPE, "rotation comes with the append");
   static_assert(!SPARSE || (!APP && !SCORE), "a page list comes with neither");
-  constexpr bool FINE = ROPE || SPARSE;  // outputs as exact as fp32 attention's
+  static_assert(!SHAPE || (!SCORE && !SPARSE && APP == ROPE), "shaped scores come alone or with the rotating append");
+  constexpr bool FINE = ROPE || SPARSE || SHAPE;  // outputs as exact as fp32 attention's
   constexpr int NW = DecodeCfg<PAIR>::NW, NT = DecodeCfg<PAIR>::NT, SLOTS = DecodeCfg<PAIR>::SLOTS;
   constexpr int NCH = NCH_OF(PAIR);  // query heads a score tile holds
   constexpr int CL = D / 16, NDW = 3 * D / 128, CB = 3 * D / 32, NS = D / 32, QV = D / 64;
@@ -381,7 +396,8 @@ __global__ __launch_bounds__(DecodeCfg<PAIR>::NT, PAIR && D == 128 ? 4 : 2) void
   // and the other half of each of the wave's pairs
   [[maybe_unused]] double turn_f = 0.0;
   [[maybe_unused]] int turn_axis = 0, turn_pos[ROPE_MAX_AXES] = {0, 0, 0, 0};
-  [[maybe_unused]] uint16_t turn_x[2][QV];
+  [[maybe_unused]] uint16_t turn_x[2][QV], norm_w[2][QV], norm_p[2][QV];  // SHAPE: the channels' weights
+  [[maybe_unused]] int turn_c[QV];
   if constexpr (ROPE) {
 #pragma unroll
     for (int ps = 0; ps < 2; ++ps) {
@@ -393,7 +409,17 @@ __global__ __launch_bounds__(DecodeCfg<PAIR>::NT, PAIR && D == 128 ? 4 : 2) void
         bool up;
         if (pc < a.rope.rot) rope_of_channel(a.rope, QV * lane + i, f, pc, up);
         turn_x[ps][i] = qh[pc];
+        if constexpr (SHAPE) turn_c[i] = pc;
       }
+      if constexpr (SHAPE)
+        if (a.norm & 1) {
+          const uint16_t* nw = norm_weights(a.qn, 0, h * G + (hd >= 0 && hd < G ? hd : 0));
+#pragma unroll
+          for (int i = 0; i < QV; ++i) {
+            norm_w[ps][i] = nw ? nw[QV * lane + i] : (uint16_t)0x3F80u;
+            norm_p[ps][i] = nw ? nw[turn_c[i]] : (uint16_t)0x3F80u;
+          }
+        }
     }
     if (tid < a.rope.rot / 2) {
       const RopeEntry e = a.rope.tab[tid];
@@ -416,12 +442,29 @@ __global__ __launch_bounds__(DecodeCfg<PAIR>::NT, PAIR && D == 128 ? 4 : 2) void
   // ids are loaded together; pages at or past the request's end are dropped
   // once the length is in (chunk < max_chunks, so the range is not empty)
   // (a page list: ranges of its entries, all at the cost of an old page)
-  const int n_ent = SPARSE ? a.n_sel : mp;
-  const int n_old_t = SPARSE ? a.n_sel : (int)old_pages((int64_t)mp * PAGE, P.recent);
+  const int n_ent = SPARSE ? a.n_sel : SHAPE ? a.n_see : mp;
+  const int n_old_t = SPARSE ? a.n_sel : (int)old_pages((int64_t)n_ent * PAGE, P.recent);
   const int64_t c0 = (int64_t)chunk * a.cunits;
-  const int p0 = page_at_cost(c0, n_old_t);
-  const int p1 = page_at_cost(min(request_cost(n_ent, n_old_t), c0 + a.cunits), n_old_t);
-  const int n_pr = p1 - p0;
+  int p0 = page_at_cost(c0, n_old_t);
+  int p1 = page_at_cost(min(request_cost(n_ent, n_old_t), c0 + a.cunits), n_old_t);
+  int n_pr = p1 - p0;
+  // SHAPE: the first token that the request's query sees, and the ranges counted from its page
+  // (with the append from the new token's at the latest)
+  int lo = 0;
+  if constexpr (SHAPE) {
+    if (a.shape.window || a.shape.first) {  // else no load has to come before the table's
+      const int at = max(a.seq_lens[r], 0) - (APP ? 0 : 1);  // the query's position
+      if (a.shape.window) lo = max(0, at - a.shape.window + 1);
+      if (a.shape.first) lo = max(lo, a.shape.first[r]);
+      int pg = lo / PAGE;
+      if constexpr (APP) pg = min(pg, max(at, 0) / PAGE);
+      pg = min(pg, mp - 1);
+      p0 += pg;
+      p1 = min(p1 + pg, mp);
+      if (p0 >= mp) p0 = mp - 1, p1 = p0;  // past the table: no pages
+      n_pr = max(p1 - p0, 1);
+    }
+  }
   // ---- 2. per-format compact lists of the chunk (logical order) -> stages.
   // Every wave reads the tags and ids of the whole chunk (lane l holds pages
   // l + 64 k), so each finds its first stages from its own ballots and starts
@@ -489,6 +532,16 @@ __global__ __launch_bounds__(DecodeCfg<PAIR>::NT, PAIR && D == 128 ? 4 : 2) void
       rope_cos_sin((double)(a.pos ? at : s_in) * turn_f, a.rope.scale, c, s);
       s_turn[tid] = make_double2(c, s);
     }
+    [[maybe_unused]] double norm_r[2] = {0.0, 0.0};  // SHAPE: the factors of the wave's heads
+    if constexpr (SHAPE)
+      if (a.norm & 1) {
+#pragma unroll
+        for (int ps = 0; ps < 2; ++ps) {
+#pragma unroll
+          for (int i = 0; i < QV; ++i) norm_r[ps] = __builtin_fma((double)qx[ps][i], (double)qx[ps][i], norm_r[ps]);
+          norm_r[ps] = norm_rstd(row_sum<64>(norm_r[ps], lane), D, a.qn.eps);
+        }
+      }
     __syncthreads();
 #pragma unroll
     for (int ps = 0; ps < 2; ++ps) {
@@ -497,11 +550,18 @@ __global__ __launch_bounds__(DecodeCfg<PAIR>::NT, PAIR && D == 128 ? 4 : 2) void
 #pragma unroll
       for (int i = 0; i < QV; ++i) {
         const int ch = QV * lane + i;
+        [[maybe_unused]] double nx = (double)qx[ps][i], np = (double)bf16_to_f32(turn_x[ps][i]);
+        if constexpr (SHAPE)
+          if (a.norm & 1) {
+            nx = nx * norm_r[ps] * norm_weight(a.qn, norm_w[ps][i]);
+            np = np * norm_r[ps] * norm_weight(a.qn, norm_p[ps][i]);
+            if (ch >= a.rope.rot) qx[ps][i] = f64_round_bf16(nx);
+          }
         if (ch < a.rope.rot) {
           int f, pc;
           bool up;
           rope_of_channel(a.rope, ch, f, pc, up);
-          const double x = (double)qx[ps][i], xp = (double)bf16_to_f32(turn_x[ps][i]);
+          const double x = SHAPE ? nx : (double)qx[ps][i], xp = SHAPE ? np : (double)bf16_to_f32(turn_x[ps][i]);
           const double2 cs = s_turn[f];
           double y0, y1;
           rope_rotate(up ? xp : x, up ? x : xp, cs.x, cs.y, y0, y1);
@@ -875,15 +935,28 @@ __global__ __launch_bounds__(DecodeCfg<PAIR>::NT, PAIR && D == 128 ? 4 : 2) void
       T.li = 0;
       T.h = h;
       small_task_load_x<D>(T, (int64_t)H * D, (int64_t)H * D, a.n_req, a.k_new, a.v_new, lane);
+      [[maybe_unused]] const uint16_t* kw = SHAPE ? norm_weights(a.kn, 0, h) : nullptr;
       small_task_load_old<D>(T, P, id, lane);
       if constexpr (ROPE)
         if (!kv) {  // while the old codes are on their way
           const double2* s_turn = reinterpret_cast<const double2*>(ring + TURN_AT);
-          small_task_rotate<D>(T, a.rope, reinterpret_cast<uint16_t*>(own), lane, [&](int, int i, double& c, double& s) {
+          auto cos_sin = [&](int, int i, double& c, double& s) {
             const double2 cs = s_turn[i];
             c = cs.x;
             s = cs.y;
-          });
+          };
+          uint16_t* xs = reinterpret_cast<uint16_t*>(own);
+          if (SHAPE && (a.norm & 2)) {
+            // (behind the row: its factor and the weights)
+            static_assert(2 * D <= 1024 && 1152 + 2 * D <= PAGE * D, "row, factors and weights fit");
+            uint16_t* sw = reinterpret_cast<uint16_t*>(own + 1152);
+            for (int c = lane; c < D; c += 64) sw[c] = kw ? kw[c] : (uint16_t)0x3F80u;
+            __builtin_amdgcn_wave_barrier();
+            small_task_rotate<D, true>(T, a.rope, xs, lane, cos_sin, a.kn.eps, [&](int c) { return norm_weight(a.kn, sw[c]); },
+                                       reinterpret_cast<double*>(own + 1024));
+          } else if (!SHAPE || a.rope.rot) {
+            small_task_rotate<D>(T, a.rope, xs, lane, cos_sin);
+          }
         }
       small_task_run<D>(T, P, id, reinterpret_cast<uint32_t*>(own), own + PAGE * D, lane);
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the token's codes and scale are stored
@@ -952,6 +1025,24 @@ __global__ __launch_bounds__(DecodeCfg<PAIR>::NT, PAIR && D == 128 ? 4 : 2) void
     const float ms = sum4rows((w[0] + w[1]) + (w[2] + w[3]));
     if (lg == 0 && col_valid && lp < (S + PAGE - 1) / PAGE)
       a.page_mass[((int64_t)r * mp + lp) * Hq + h * G + col_head] = make_float2(ms, st.m_run);
+  };
+  // SHAPE: the scores of tokens 4 lg .. + 3 of page lp capped, biased by their distance (capped
+  // first) and hidden before the first token; bias: a padding column's -inf, which no cap may lift
+  [[maybe_unused]] float slope = 0.0f;
+  if constexpr (SHAPE)
+    if (a.shape.slopes && col_valid) slope = a.shape.slopes[h * G + col_head] * LOG2E_F;
+  [[maybe_unused]] auto shape_scores = [&](float* s, int lp, float bias) {
+    const int t = lp * PAGE + 4 * lg;
+    if (a.shape.cap != 0.0f) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s[i] = shape_cap(a.shape, s[i]);
+    }
+    if (a.shape.slopes) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s[i] = fmaf(slope, (float)(t + i - (S - 1)), s[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) s[i] = t + i < lo ? -INFINITY : s[i] + bias;
   };
   int k_st = 0;  // stages begun by this wave; stage k sits in slot k % SLOTS
   while (jc < st3) {
@@ -1032,7 +1123,8 @@ __global__ __launch_bounds__(DecodeCfg<PAIR>::NT, PAIR && D == 128 ? 4 : 2) void
     {
       const _Float16* gh = reinterpret_cast<const _Float16*>(&gw);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) sc[i] = fmaf((col_b ? sb[i] : sa[i]) * qinv, (float)gh[i], col_bias);
+      for (int i = 0; i < 4; ++i) sc[i] = fmaf((col_b ? sb[i] : sa[i]) * qinv, (float)gh[i], SHAPE ? 0.0f : col_bias);
+      if constexpr (SHAPE) shape_scores(sc, col_b ? e.z : e.x, col_bias);
       // tokens at or past the end: only in a stage that holds the request's
       // last page or a masked page b
       if ((e.x + 1) * PAGE > S || (pair && (e.z + 1) * PAGE > S)) {
@@ -1130,7 +1222,8 @@ __global__ __launch_bounds__(DecodeCfg<PAIR>::NT, PAIR && D == 128 ? 4 : 2) void
     {
       const float kk = FINE ? ksv.x * smk * pinv : ksv.x * smk;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) sc[i] = fmaf(sa[i], kk, fp8_bias);
+      for (int i = 0; i < 4; ++i) sc[i] = fmaf(sa[i], kk, SHAPE ? 0.0f : fp8_bias);
+      if constexpr (SHAPE) shape_scores(sc, e.x, fp8_bias);
       if ((e.x + 1) * PAGE > S) {
         const int vcnt = S - e.x * PAGE;
 #pragma unroll
@@ -1293,7 +1386,7 @@ __global__ __launch_bounds__(64 * W) void decode_merge_kernel(int G, int H, int 
                                                              float* lse, const int32_t* app_rec,
                                                              int32_t* bt_w, uint8_t* tags_w,
                                                              int max_pages, const int32_t* seq_lens,
-                                                             int32_t* ctrl, int32_t* rc8) {
+                                                             int32_t* ctrl, int32_t* rc8, const float* sinks) {
   constexpr int NC = D / 64;
   typedef float vec __attribute__((ext_vector_type(NC)));
   static_assert(B <= 64, "lane j holds slot j's (m, l)");
@@ -1390,6 +1483,15 @@ __global__ __launch_bounds__(64 * W) void decode_merge_kernel(int G, int H, int 
   }
   const int64_t row = (int64_t)r * Hq + h * G + n;
   if (poisoned) L = 0.0f;
+  if (sinks && !poisoned) {  // (shaped scores) the head's sink: a token without a value
+    const float s2 = sinks[h * G + n] * LOG2E_F, Ms = fmaxf(L > 0.0f ? M : -INFINITY, s2);
+    if (Ms != -INFINITY) {
+      const float f = L > 0.0f ? exp2f(M - Ms) : 0.0f;
+      O *= f;
+      L = fmaf(L, f, exp2f(s2 - Ms));
+      M = Ms;
+    }
+  }
   const float inv = L > 0.0f ? 1.0f / L : 0.0f;
   vec res = 0.0f;
   if (L > 0.0f) {
@@ -1455,15 +1557,15 @@ static constexpr size_t lds_limit() {
   return 160 * 1024 - sizeof(int4) * MAX_CHUNK_PAGES - 2 * 16 * NW_MAX * sizeof(float) - 256;
 }
 
-template <bool APP, bool SCORE = false, bool ROPE = false, bool SPARSE = false>
+template <bool APP, bool SCORE = false, bool ROPE = false, bool SPARSE = false, bool SHAPE = false>
 static const void* decode_instance(int d, bool pair, bool g6) {
   if (d == 256)
-    return g6 ? (const void*)decode_kernel<256, true, true, APP, SCORE, ROPE, SPARSE>
-                : pair ? (const void*)decode_kernel<256, true, false, APP, SCORE, ROPE, SPARSE>
-                       : (const void*)decode_kernel<256, false, false, APP, SCORE, ROPE, SPARSE>;
-  return g6 ? (const void*)decode_kernel<128, true, true, APP, SCORE, ROPE, SPARSE>
-              : pair ? (const void*)decode_kernel<128, true, false, APP, SCORE, ROPE, SPARSE>
-                     : (const void*)decode_kernel<128, false, false, APP, SCORE, ROPE, SPARSE>;
+    return g6 ? (const void*)decode_kernel<256, true, true, APP, SCORE, ROPE, SPARSE, SHAPE>
+                : pair ? (const void*)decode_kernel<256, true, false, APP, SCORE, ROPE, SPARSE, SHAPE>
+                       : (const void*)decode_kernel<256, false, false, APP, SCORE, ROPE, SPARSE, SHAPE>;
+  return g6 ? (const void*)decode_kernel<128, true, true, APP, SCORE, ROPE, SPARSE, SHAPE>
+              : pair ? (const void*)decode_kernel<128, true, false, APP, SCORE, ROPE, SPARSE, SHAPE>
+                     : (const void*)decode_kernel<128, false, false, APP, SCORE, ROPE, SPARSE, SHAPE>;
 }
 
 hipError_t launch_decode(const PoolView& P, int layer, int n_req, const uint16_t* q,
@@ -1472,13 +1574,16 @@ hipError_t launch_decode(const PoolView& P, int layer, int n_req, const uint16_t
                          hipStream_t s, hipEvent_t* ev, const uint16_t* k_new,
                          const uint16_t* v_new, int32_t* bt_w, uint8_t* tags_w,
                          float2* page_mass, const RopeView* rope, const int32_t* pos, const int32_t* sel,
-                         const int32_t* sel_count, int n_sel) {
+                         const int32_t* sel_count, int n_sel, const ShapeView* shape, const NormView* qn,
+                         const NormView* kn) {
   const bool app = k_new != nullptr;
   const bool score = page_mass != nullptr;
-  const bool turn = rope != nullptr, sparse = sel != nullptr;
+  const bool turn = rope != nullptr, sparse = sel != nullptr, shaped = shape != nullptr;
   if ((app && score) || (turn && !app) || (sparse && (app || score))) return hipErrorInvalidValue;
+  if (shaped ? score || sparse || app != turn : qn || kn) return hipErrorInvalidValue;
+  const int n_see = shaped ? decode_see(max_pages, shape->window) : max_pages;
   const DecodeShape sh = sparse ? decode_shape(n_req, n_sel, P.n_kv_heads, 0, P.group, P.d)
-                                : decode_shape(n_req, max_pages, P.n_kv_heads, P.recent, P.group, P.d);
+                                : decode_shape(n_req, n_see, P.n_kv_heads, P.recent, P.group, P.d);
   DecodeArgs a;
   a.P = P;
   a.layer = layer;
@@ -1493,7 +1598,12 @@ hipError_t launch_decode(const PoolView& P, int layer, int n_req, const uint16_t
   a.partials = reinterpret_cast<float*>(ws);
   a.cunits = sh.cunits;
   a.max_chunks = sh.max_chunks;
-  a.sm_log2 = 1.4426950408889634f / sqrtf((float)P.d);
+  a.sm_log2 = shaped && shape->scale > 0.0f ? shape->scale * LOG2E_F : 1.4426950408889634f / sqrtf((float)P.d);
+  a.shape = shaped ? *shape : ShapeView{};
+  a.n_see = n_see;
+  a.norm = (qn ? 1 : 0) | (kn ? 2 : 0);
+  a.qn = qn ? *qn : NormView{};
+  a.kn = kn ? *kn : NormView{};
   a.k_new = k_new;
   a.v_new = v_new;
   a.bt_w = bt_w;
@@ -1511,22 +1621,24 @@ hipError_t launch_decode(const PoolView& P, int layer, int n_req, const uint16_t
   const bool pair = P.group <= 8;
   const int nw = pair ? DecodeCfg<true>::NW : DecodeCfg<false>::NW;
   const int slots = pair ? DecodeCfg<true>::SLOTS : DecodeCfg<false>::SLOTS;
-  const size_t qop_b = (size_t)query_bytes(turn || sparse, P.d);
+  const size_t qop_b = (size_t)query_bytes(turn || sparse || shaped, P.d);
   const size_t ring_b = (size_t)nw * slots * 2 * tq3_region_bytes(P.d);
   const size_t lds = qop_b + ring_b;  // the epilogue reuses each wave's ring slot
   if (lds > lds_limit()) return hipErrorInvalidValue;
   const bool g6 = pair && P.group <= 6;
-  const void* kern = sparse  ? decode_instance<false, false, false, true>(P.d, pair, g6)
+  const void* kern = shaped  ? app ? decode_instance<true, false, true, false, true>(P.d, pair, g6)
+                                   : decode_instance<false, false, false, false, true>(P.d, pair, g6)
+                     : sparse  ? decode_instance<false, false, false, true>(P.d, pair, g6)
                      : turn  ? decode_instance<true, false, true>(P.d, pair, g6)
                      : app   ? decode_instance<true>(P.d, pair, g6)
                      : score ? decode_instance<false, true>(P.d, pair, g6)
                              : decode_instance<false>(P.d, pair, g6);
   // the dynamic-LDS limit is raised once per kernel instance and device
-  static std::atomic<uint32_t> attr_done[64];
+  static std::atomic<uint64_t> attr_done[64];
   int dev = 0;
   hipError_t e = hipGetDevice(&dev);
   if (e != hipSuccess) return e;
-  const uint32_t bit = 1u << ((sparse ? 24 : turn ? 18 : app ? 6 : score ? 12 : 0) + (P.d == 256 ? 3 : 0) + (g6 ? 2 : pair ? 1 : 0));
+  const uint64_t bit = 1ull << ((shaped ? app ? 36 : 30 : sparse ? 24 : turn ? 18 : app ? 6 : score ? 12 : 0) + (P.d == 256 ? 3 : 0) + (g6 ? 2 : pair ? 1 : 0));
   if (dev < 0 || dev >= 64 || !(attr_done[dev].load() & bit)) {
     e = hipFuncSetAttribute(kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds_limit());
     if (e != hipSuccess) return e;
@@ -1546,7 +1658,8 @@ hipError_t launch_decode(const PoolView& P, int layer, int n_req, const uint16_t
   const int32_t* rec = a.app_rec;
   int32_t* ctrl = P.ctrl;
   int32_t* rc8 = P.rc8;
-  void* margs[] = {&G, &H, &mc, &pa, &out, &lse, &rec, &bt_w, &tags_w, &mpg, &seq_lens, &ctrl, &rc8};
+  const float* sinks = a.shape.sinks;
+  void* margs[] = {&G, &H, &mc, &pa, &out, &lse, &rec, &bt_w, &tags_w, &mpg, &seq_lens, &ctrl, &rc8, &sinks};
   // merge shape: one round trip for the slots of one call, and no more waves
   // than that takes.  One wave with rounds of 32 slots took 6.0 us on 63 slots
   // (24 rows), 4.6 on 32 (48 rows); so 4.6 and 4.0.  Few slots stay at one or two

@@ -7,6 +7,7 @@
 
 #include "mkv_device.h"
 #include "mkv_rope.h"
+#include "mkv_shape.h"
 
 struct kv_rope {
   int head_dim;
@@ -121,7 +122,10 @@ hipError_t launch_decode(const PoolView& P, int layer, int n_req, const uint16_t
                          const uint16_t* v_new = nullptr, int32_t* bt_w = nullptr,
                          uint8_t* tags_w = nullptr, float2* page_mass = nullptr,
                          const RopeView* rope = nullptr, const int32_t* pos = nullptr,
-                         const int32_t* sel = nullptr, const int32_t* sel_count = nullptr, int n_sel = 0);
+                         const int32_t* sel = nullptr, const int32_t* sel_count = nullptr, int n_sel = 0,
+                         const ShapeView* shape = nullptr, const NormView* qn = nullptr,
+                         const NormView* kn = nullptr);
+int decode_see(int max_pages, int window);
 hipError_t launch_score_collect(int n_req, int n_q_heads, int max_pages, const int32_t* seq_lens,
                                 const float* lse, const float2* page_mass,
                                 const uint8_t* head_mask, float beta, float* a_io, float* r_out,
