@@ -446,6 +446,9 @@ mkv_status paged_attn_decode_sparse(mkv_pool* pool, int32_t layer, int32_t n_req
  *    query and key heads normed before the rotation (q_norm, k_norm, each may be NULL: not
  *    normed; rope NULL: not rotated).  The appended token is stored whether or not its query
  *    sees it.  State afterwards as by kv_append_fp8_norm_rope.
+ *  - paged_attn_chunk_shaped is paged_attn_chunk with them, rows = queries, and with rows of
+ *    bf16 out ([n_q_total][n_q_heads][d], what the next matrix product takes).  A block of 128
+ *    rows reads the pages from the first to the last that any of its rows sees.
  * Errors also: EINVAL (shaping NULL, window negative), ERANGE (cap neither 0 nor in [1e-6, 1e6],
  * scale neither 0 nor in [1e-6, 1e6]).  Slopes and sinks are finite, or a sink -inf. */
 typedef struct paged_attn_shaping {
@@ -468,6 +471,12 @@ mkv_status paged_attn_decode_append_shaped(mkv_pool* pool, const paged_attn_shap
                                            const int32_t* positions, int32_t* block_table, uint8_t* tags,
                                            int32_t max_pages, const int32_t* seq_lens_before, float* out,
                                            float* lse, void* ws, size_t ws_bytes, hipStream_t stream);
+
+mkv_status paged_attn_chunk_shaped(mkv_pool* pool, const paged_attn_shaping* shaping, int32_t layer,
+                                   int32_t n_req, const uint16_t* q, const int32_t* cu_q, int32_t n_q_total,
+                                   const int32_t* block_table, const uint8_t* tags, int32_t max_pages,
+                                   const int32_t* seq_lens, uint16_t* out, void* ws, size_t ws_bytes,
+                                   hipStream_t stream);
 
 /* The cache read back: bf16 K and V rows of positions from[r] .. from[r] + n_r - 1 of
  * every request, n_r = cu_tokens[r+1] - cu_tokens[r], as rows cu_tokens[r] .. of k and v

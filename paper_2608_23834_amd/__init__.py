@@ -38,7 +38,8 @@ EXPORTS = ["kv_pool_bytes", "kv_pool_create", "kv_pool_destroy", "kv_append_fp8"
            "paged_attn_decode_append_rope", "kv_page_bounds_bytes", "kv_page_bounds_update",
            "paged_attn_select_workspace_bytes", "paged_attn_select_pages", "paged_attn_decode_sparse",
            "kv_read_tokens", "kv_norm_rope_apply", "kv_append_fp8_norm_rope",
-           "paged_attn_decode_shaped", "paged_attn_decode_append_shaped", "mkv_status_string"]
+           "paged_attn_decode_shaped", "paged_attn_decode_append_shaped", "paged_attn_chunk_shaped",
+           "mkv_status_string"]
 
 _lib = None
 
@@ -148,6 +149,7 @@ def lib() -> ctypes.CDLL:
         L.paged_attn_decode_shaped.argtypes = [vp, vp, i32, i32, vp, vp, vp, i32, vp, vp, vp, vp, sz, vp]
         L.paged_attn_decode_append_shaped.argtypes = [vp, vp, vp, vp, vp, i32, i32, vp, vp, vp, vp, vp, vp, i32, vp, vp,
                                                       vp, vp, sz, vp]
+        L.paged_attn_chunk_shaped.argtypes = [vp, vp, i32, i32, vp, vp, i32, vp, vp, i32, vp, vp, vp, sz, vp]
         L.kv_read_tokens.argtypes = [vp, i32, i32, vp, vp, i32, vp, vp, i32, vp, i64, vp, i64, vp]
         L.mkv_control_bf16_write.argtypes = [vp, i32, i32, i32, i32, i32, i32, vp, i32, vp, vp, i32,
                                              vp, vp, vp]
@@ -794,6 +796,26 @@ def paged_attn_chunk(pool: Pool, layer, q, cu_q, block_table, tags, seq_lens, ou
         pool.handle, layer, n_req, _ptr(q), _ptr(cu_q), int(q.shape[0]), _ptr(block_table),
         _ptr(tags), max_pages, _ptr(seq_lens), _ptr(out), _ptr(ws), ws.numel() * ws.element_size(),
         _stream(stream)))
+
+
+def paged_attn_chunk_shaped(pool: Pool, shaping: Shaping, layer, q, cu_q, block_table, tags, seq_lens, out, ws,
+                            stream=None):
+    """paged_attn_chunk with shaped scores and masks; out: bf16 (or its bits in int16) [n][n_q_heads][head_dim]."""
+    dev, cur = _current()
+    rows, i32, _ = _types()
+    n_req, max_pages = _table(dev, pool, block_table, tags, i32)
+    _here(dev, q, cu_q, seq_lens, out, ws)
+    if not (q.dtype in rows and out.dtype in rows and cu_q.dtype in i32 and seq_lens.dtype in i32):
+        raise ValueError("q and out are bf16 (or its bits in int16), lengths int32")
+    if q.shape != (q.shape[0], pool.n_q_heads, pool.d) or out.shape != q.shape:
+        raise ValueError("q and out are [n][n_q_heads][head_dim]")
+    if cu_q.numel() <= n_req or seq_lens.numel() < n_req:
+        raise ValueError("cu_q is [n_req + 1], seq_lens [n_req]")
+    desc = shaping._desc(dev, pool.n_q_heads, q.shape[0], n_req)
+    _check("paged_attn_chunk_shaped", lib().paged_attn_chunk_shaped(
+        pool.handle, ctypes.byref(desc), layer, n_req, q.data_ptr(), cu_q.data_ptr(), q.shape[0], block_table.data_ptr(),
+        tags.data_ptr(), max_pages, seq_lens.data_ptr(), out.data_ptr(), ws.data_ptr(), ws.nbytes,
+        cur if stream is None else stream.cuda_stream))
 
 
 def kv_partition_pages(block_table, tags, seq_lens, list8, list3, counts, stream=None):

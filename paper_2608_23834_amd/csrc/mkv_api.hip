@@ -738,10 +738,10 @@ mkv_status paged_attn_last_times(mkv_pool* pool, float* scan_us, float* merge_us
   return MKV_OK;
 }
 
-mkv_status paged_attn_chunk(mkv_pool* pool, int32_t layer, int32_t n_req, const uint16_t* q,
-                            const int32_t* cu_q, int32_t n_q_total, const int32_t* block_table,
-                            const uint8_t* tags, int32_t max_pages, const int32_t* seq_lens,
-                            float* out, void* ws, size_t ws_bytes, hipStream_t stream) {
+static mkv_status chunk(mkv_pool* pool, const ShapeView* shape, int32_t layer, int32_t n_req, const uint16_t* q,
+                        const int32_t* cu_q, int32_t n_q_total, const int32_t* block_table, const uint8_t* tags,
+                        int32_t max_pages, const int32_t* seq_lens, void* out, void* ws, size_t ws_bytes,
+                        hipStream_t stream) {
   if (!pool || !q || !cu_q || !block_table || !tags || !seq_lens || !out || !ws) return MKV_EINVAL;
   if (n_req < 1 || max_pages < 1 || n_q_total < 1) return MKV_EINVAL;
   if (!aligned16(q) || !aligned16(out) || !aligned16(ws)) return MKV_EINVAL;
@@ -750,11 +750,31 @@ mkv_status paged_attn_chunk(mkv_pool* pool, int32_t layer, int32_t n_req, const 
   if ((int64_t)n_q_total * pool->group > ((int64_t)1 << 31) / 2) return MKV_ERANGE;
   if (ws_bytes < chunk_ws_least(n_req, max_pages)) return MKV_ENOMEM;
   hipError_t e = launch_chunk(view_of(pool), layer, n_req, q, cu_q, n_q_total, block_table, tags,
-                              max_pages, seq_lens, out, ws, ws_bytes, stream);
+                              max_pages, seq_lens, out, ws, ws_bytes, stream, shape);
   if (e == hipErrorNotSupported) return MKV_EUNSUP;
   mkv_status st = hip_status(e);
   if (st == MKV_OK) pool->chunk_routes++;
   return st;
+}
+
+mkv_status paged_attn_chunk(mkv_pool* pool, int32_t layer, int32_t n_req, const uint16_t* q,
+                            const int32_t* cu_q, int32_t n_q_total, const int32_t* block_table,
+                            const uint8_t* tags, int32_t max_pages, const int32_t* seq_lens,
+                            float* out, void* ws, size_t ws_bytes, hipStream_t stream) {
+  return chunk(pool, nullptr, layer, n_req, q, cu_q, n_q_total, block_table, tags, max_pages, seq_lens, out, ws,
+               ws_bytes, stream);
+}
+
+mkv_status paged_attn_chunk_shaped(mkv_pool* pool, const paged_attn_shaping* shaping, int32_t layer, int32_t n_req,
+                                   const uint16_t* q, const int32_t* cu_q, int32_t n_q_total,
+                                   const int32_t* block_table, const uint8_t* tags, int32_t max_pages,
+                                   const int32_t* seq_lens, uint16_t* out, void* ws, size_t ws_bytes,
+                                   hipStream_t stream) {
+  ShapeView v;
+  mkv_status st = check_shaping(shaping, &v);
+  if (st != MKV_OK) return st;
+  return chunk(pool, &v, layer, n_req, q, cu_q, n_q_total, block_table, tags, max_pages, seq_lens, out, ws, ws_bytes,
+               stream);
 }
 
 mkv_status paged_attn_decode_cohort_key(const mkv_pool* pool, int32_t n_req, int32_t max_pages,

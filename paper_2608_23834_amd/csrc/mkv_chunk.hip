@@ -38,6 +38,8 @@
 // few bits where FP8 keys carry large norms) and fold the pages' V scales, less
 // their powers of two, into the weights; the PV waves read the pages' values from
 // the ring and scale them by those.  The
+// SHAPE instances cap, bias and mask the scores as they are finished and read only the
+// pages that some row of the block sees.  The
 // workgroups of one (request, KV head) read the same pages at about the same
 // time, so the page bytes come from L2 after the first reader.
 #include <hip/hip_runtime.h>
@@ -47,6 +49,7 @@
 
 #include "mkv_attn.h"
 #include "mkv_internal.h"
+#include "mkv_shape.h"
 #include "../../include/minima_kv.h"
 
 namespace mkv {
@@ -65,13 +68,14 @@ struct ChunkArgs {
   const uint16_t* q;
   const int32_t* cu_q;
   const int32_t* seq_lens;
-  float* out;
+  void* out;           // fp32 rows, SHAPE: bf16
   const int2* list8;   // [n_req][stride] (logical page, physical id), in pairs
   const int2* list3;
   const int32_t* hdr;  // [0] work items, [1] blocks cut into parts
   const int4* items;   // two per work item, see chunk_plan_kernel
   float* parts;        // the parts of cut blocks, see chunk_part_floats
   float sm_log2;       // log2(e) / sqrt(d)
+  ShapeView shape;     // SHAPE instances
 };
 
 static size_t al256(size_t b) { return (b + 255) / 256 * 256; }
@@ -244,10 +248,11 @@ __global__ __launch_bounds__(1024) void chunk_plan_kernel(int n_req, const int32
                                                           int group, int grid, int b0, int n_items, int share,
                                                           int may_cut, int max_slots, int stride, const int2* cum,
                                                           int32_t* rbo, int32_t* hdr, int4* items,
-                                                          int4* splits, int32_t* err) {
+                                                          int4* splits, int32_t* err, int window,
+                                                          const int32_t* first, const int32_t* prefix) {
   __shared__ int scratch[32];
   __shared__ int s_rbo[1025];
-  __shared__ int s_r[MAX_ITEMS], s_x[MAX_ITEMS], s_t3[MAX_ITEMS], s_f8[MAX_ITEMS];
+  __shared__ int s_r[MAX_ITEMS], s_x[MAX_ITEMS], s_t3[MAX_ITEMS], s_f8[MAX_ITEMS], s_a3[MAX_ITEMS], s_a8[MAX_ITEMS];
   __shared__ int s_max, s_est[16], s_u[16];
   const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
   const int per = (n_req + 1023) / 1024;
@@ -290,8 +295,8 @@ __global__ __launch_bounds__(1024) void chunk_plan_kernel(int n_req, const int32
     }
     return;
   }
-  // block b -> request, block of the request, TQ3 and FP8 pairs it reads
-  auto locate = [&](int b, int& r, int& x, int& t3, int& f8) {
+  // block b -> request, block of the request, TQ3 and FP8 pairs it reads, from which on
+  auto locate = [&](int b, int& r, int& x, int& t3, int& f8, int& a3, int& a8) {
     int lo = 0, hi = n_req - 1;  // the last request whose first block is <= b
     while (lo < hi) {
       const int mid = (lo + hi + 1) >> 1;
@@ -300,22 +305,36 @@ __global__ __launch_bounds__(1024) void chunk_plan_kernel(int n_req, const int32
     }
     r = lo;
     x = b - (in_lds ? s_rbo[lo] : rbo[lo]);
-    t3 = f8 = 0;
+    t3 = f8 = a3 = a8 = 0;
     const int q0 = cu_q[r], q1 = cu_q[r + 1], nq = q1 - q0, S = seq_lens[r];
     if (q0 < 0 || nq < 1 || q1 > n_q_total || S < nq || S > (int64_t)max_pages * PAGE) return;
     const int last = min(nq * group, (x + 1) * (NSW * 32)) - 1;  // the block's last row
-    const int2 c = cum[(int64_t)r * stride + (S - nq + last / group) / PAGE];
-    t3 = (c.y + 1) / 2;
-    f8 = (c.x + 1) / 2;
+    const int i0 = x * (NSW * 32) / group, i1 = last / group, p0 = S - nq;  // its queries, the first one's position
+    int to = p0 + i1, from = 0;  // what its rows see at most
+    if (prefix && p0 + i0 < prefix[r]) to = max(to, min(prefix[r], S) - 1);
+    if (first) {
+      from = 0x7FFFFFFF;
+      for (int i = i0; i <= i1; ++i) from = min(from, first[q0 + i]);
+    }
+    if (window) from = max(from, p0 + i0 - window + 1);
+    const int2 c = cum[(int64_t)r * stride + to / PAGE];
+    const int pg = min(max(from, 0), to) / PAGE;
+    if (pg > 0) {
+      const int2 c0 = cum[(int64_t)r * stride + pg - 1];
+      a3 = c0.y / 2;
+      a8 = c0.x / 2;
+    }
+    t3 = (c.y + 1) / 2 - a3;
+    f8 = (c.x + 1) / 2 - a8;
   };
   const bool cut = may_cut && nblk <= 2 * share;
   if (!cut || b0 > 0) {
     const int n = max(0, min(nblk - b0, n_items));  // (none after a call's cut blocks)
     for (int b = tid; b < n; b += 1024) {
-      int r, x, t3, f8;
-      locate(b0 + b, r, x, t3, f8);
-      items[2 * b] = make_int4(r, x, 0, t3);
-      items[2 * b + 1] = make_int4(0, f8, -1, 0);
+      int r, x, t3, f8, a3, a8;
+      locate(b0 + b, r, x, t3, f8, a3, a8);
+      items[2 * b] = make_int4(r, x, a3, t3);
+      items[2 * b + 1] = make_int4(a8, f8, -1, 0);
     }
     if (tid == 0) {
       hdr[0] = n;
@@ -325,7 +344,7 @@ __global__ __launch_bounds__(1024) void chunk_plan_kernel(int n_req, const int32
   }
   int cost = 0;
   if (tid < nblk) {  // nblk <= 2 * share <= MAX_ITEMS
-    locate(tid, s_r[tid], s_x[tid], s_t3[tid], s_f8[tid]);
+    locate(tid, s_r[tid], s_x[tid], s_t3[tid], s_f8[tid], s_a3[tid], s_a8[tid]);
     cost = COST3 * s_t3[tid] + COST8 * s_f8[tid];
     atomicMax(&s_max, cost);
   }
@@ -334,8 +353,8 @@ __global__ __launch_bounds__(1024) void chunk_plan_kernel(int n_req, const int32
   const int cmax = s_max;
   if (cmax <= CUT_FROM) {  // workgroup-uniform
     if (tid < nblk) {
-      items[2 * tid] = make_int4(s_r[tid], s_x[tid], 0, s_t3[tid]);
-      items[2 * tid + 1] = make_int4(0, s_f8[tid], -1, 0);
+      items[2 * tid] = make_int4(s_r[tid], s_x[tid], s_a3[tid], s_t3[tid]);
+      items[2 * tid + 1] = make_int4(s_a8[tid], s_f8[tid], -1, 0);
     }
     if (tid == 0) {
       hdr[0] = nblk;
@@ -381,8 +400,8 @@ __global__ __launch_bounds__(1024) void chunk_plan_kernel(int n_req, const int32
     for (int k = 0; k < ns; ++k) {
       const int j1 = k + 1 == ns ? t3 + f8 : pass_at((int)((int64_t)cost * (k + 1) / ns));
       const int a3 = min(j0, t3), b3 = min(j1, t3), a8 = max(j0 - t3, 0), b8 = max(j1 - t3, 0);
-      items[2 * (it0 + k)] = make_int4(r, x, a3, b3 - a3);
-      items[2 * (it0 + k) + 1] = make_int4(a8, b8 - a8, ns > 1 ? sl0 + k : -1, 0);
+      items[2 * (it0 + k)] = make_int4(r, x, s_a3[tid] + a3, b3 - a3);
+      items[2 * (it0 + k) + 1] = make_int4(s_a8[tid] + a8, b8 - a8, ns > 1 ? sl0 + k : -1, 0);
       j0 = j1;
     }
     if (ns > 1) splits[sp0] = make_int4(r, x, sl0, ns);
@@ -458,9 +477,27 @@ struct ChunkLds {
   static_assert(TOTAL <= 160 * 1024, "one workgroup's LDS");
 };
 
+// 2 NBW neighbouring channels of an output row, from element i on
+template <int NBW, bool BF16>
+__device__ __forceinline__ void store_out(void* out, int64_t i, const float* y) {
+  if constexpr (BF16) {
+    typedef __bf16 bf2 __attribute__((ext_vector_type(2)));
+    uint32_t w[NBW];
+#pragma unroll
+    for (int b = 0; b < NBW; ++b) w[b] = __builtin_bit_cast(uint32_t, bf2{(__bf16)y[2 * b], (__bf16)y[2 * b + 1]});
+    if constexpr (NBW == 2) *reinterpret_cast<uint2*>(static_cast<uint16_t*>(out) + i) = make_uint2(w[0], w[1]);
+    else *reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(out) + i) = w[0];
+  } else if constexpr (NBW == 2) {
+    *reinterpret_cast<float4*>(static_cast<float*>(out) + i) = make_float4(y[0], y[1], y[2], y[3]);
+  } else {
+    *reinterpret_cast<float2*>(static_cast<float*>(out) + i) = make_float2(y[0], y[1]);
+  }
+}
+
 // One work item: passes of the 128-row block xb of request r and KV head h (the
 // body of a chunk workgroup; every wave of the workgroup runs it).
-template <int D>
+// SHAPE: 1 biased and masked scores, 2 capped ones as well; bf16 rows out.
+template <int D, int SHAPE>
 __device__ __forceinline__ void chunk_block(const ChunkArgs& a, int4 it0, int4 it1, int h, uint8_t* smem) {
   constexpr int NDW = 3 * D / 128, CL = D / 16, QQ = D / 4;
   constexpr int NKS = D / 16;   // k-steps of the FP8-page score product (16 channels each)
@@ -505,8 +542,11 @@ __device__ __forceinline__ void chunk_block(const ChunkArgs& a, int4 it0, int4 i
     // rows that can be located get zeros
     const int rho = rb + li;
     if (score_wave && rho < rows_r) {
-      float* o = a.out + ((int64_t)(q0 + rho / G) * Hq + h * G + rho % G) * D;
-      for (int c = lg; c < D; c += 2) o[c] = 0.0f;
+      const int64_t o = ((int64_t)(q0 + rho / G) * Hq + h * G + rho % G) * D;
+      for (int c = lg; c < D; c += 2) {
+        if constexpr (SHAPE) static_cast<uint16_t*>(a.out)[o + c] = 0;
+        else static_cast<float*>(a.out)[o + c] = 0.0f;
+      }
     }
     return;
   }
@@ -517,7 +557,30 @@ __device__ __forceinline__ void chunk_block(const ChunkArgs& a, int4 it0, int4 i
   // this lane's query row rb + li: last token it may see, min(S - 1,
   // position); -1 for rows past the request's rows (all masked)
   const int rho_l = rb + li;
-  const int lim = rho_l < rows_r ? min(S - 1, P0 + rho_l / G) : -1;
+  int lim = rho_l < rows_r ? min(S - 1, P0 + rho_l / G) : -1;
+  // SHAPE: the first token the row may see, its position, its head's slope; the wave's largest
+  // first token (rows past the request's rows see what they like: they are not stored)
+  [[maybe_unused]] int lo = 0, lo_max = 0;
+  [[maybe_unused]] float posf = 0.0f, slope = 0.0f;
+  if constexpr (SHAPE) {
+    if (lim >= 0) {
+      if (a.shape.window) lo = max(0, lim - a.shape.window + 1);
+      if (a.shape.first) lo = max(lo, a.shape.first[q0 + rho_l / G]);
+      if (a.shape.slopes) slope = -LOG2E_F * a.shape.slopes[h * G + rho_l % G];
+      posf = (float)lim;
+      if (a.shape.prefix && lim < a.shape.prefix[r]) lim = max(lim, min(a.shape.prefix[r], S) - 1);
+    }
+    lo_max = lo;
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) lo_max = max(lo_max, __shfl_xor(lo_max, o, 64));
+    lo_max = __builtin_amdgcn_readfirstlane(lo_max);
+  }
+  // score v (base 2) of token t shaped; t0f the token's number less u
+  [[maybe_unused]] auto shaped = [&](float v, float t0f, int u) {
+    if constexpr (SHAPE == 2) v = shape_cap(a.shape, v);
+    return fmaf(slope, fabsf(t0f + (float)u - posf), v);
+  };
+  auto sees = [&](int t) { return t <= lim && (!SHAPE || t >= lo); };
   float* const part = slot_out < 0 ? nullptr : a.parts + ((int64_t)slot_out * H + h) * chunk_part_floats(D);
   uint8_t* const kbuf = smem + LY::KB0;
   uint8_t* const vbuf = smem + LY::VB0;
@@ -930,9 +993,10 @@ __device__ __forceinline__ void chunk_block(const ChunkArgs& a, int4 it0, int4 i
         const int t0 = (e4 < 2 ? e.x : e.z) * PAGE + 8 * (e4 & 1) + 4 * lg;
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
-          const float v = st[4 * e4 + u] * qinv * (float)reinterpret_cast<const _Float16*>(&gw[e4])[u];
+          float v = st[4 * e4 + u] * qinv * (float)reinterpret_cast<const _Float16*>(&gw[e4])[u];
+          if constexpr (SHAPE) v = shaped(v, (float)t0, u);
           if constexpr (decltype(masked)::value)
-            sc[4 * e4 + u] = t0 + u <= lim ? v : -INFINITY;
+            sc[4 * e4 + u] = sees(t0 + u) ? v : -INFINITY;
           else
             sc[4 * e4 + u] = v;
         }
@@ -947,7 +1011,10 @@ __device__ __forceinline__ void chunk_block(const ChunkArgs& a, int4 it0, int4 i
       w.z = h8u(zh, zl, 0u, 0u);  // (R_a, R_b) hi, then lo
     };
     // a pair whose pages both end before the chunk's first query needs no mask
-    auto unmasked = [&](const int4& e) { return (max(e.x, e.z) + 1) * PAGE <= P0 + 1; };
+    // (SHAPE: and its first page not before any row's first token)
+    auto unmasked = [&](const int4& e) {
+      return (max(e.x, e.z) + 1) * PAGE <= P0 + 1 && (!SHAPE || min(e.x, e.z) * PAGE >= lo_max);
+    };
 
     // ---- passes over the TQ3 pairs.  Pass p (after barrier p + 1) issues
     // the score product of pair p (keys unpacked in pass p - 1) and, while
@@ -997,9 +1064,11 @@ __device__ __forceinline__ void chunk_block(const ChunkArgs& a, int4 it0, int4 i
         for (int u = 0; u < 4; ++u) {
           // st * gamma as one mixed-precision FMA; the power-of-two row
           // factor qinv enters with the max and the exponent (exact)
-          const float v = __builtin_fmaf((float)reinterpret_cast<const _Float16*>(&gw[e4])[u], st_prev[4 * e4 + u], 0.0f);
+          // (SHAPE: here already, as cap and bias need the score itself)
+          float v = __builtin_fmaf((float)reinterpret_cast<const _Float16*>(&gw[e4])[u], st_prev[4 * e4 + u], 0.0f);
+          if constexpr (SHAPE) v = shaped(v * qinv, (float)t0, u);
           if constexpr (decltype(masked)::value)
-            sc[4 * e4 + u] = t0 + u <= lim ? v : -INFINITY;
+            sc[4 * e4 + u] = sees(t0 + u) ? v : -INFINITY;
           else
             sc[4 * e4 + u] = v;
         }
@@ -1008,7 +1077,7 @@ __device__ __forceinline__ void chunk_block(const ChunkArgs& a, int4 it0, int4 i
       auto ex = [&](int k0, int k1) {
 #pragma unroll
         for (int k = k0; k < k1; ++k) {
-          sc[k] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[k], qinv, -m_new));  // -inf -> 0
+          sc[k] = __builtin_amdgcn_exp2f(SHAPE ? sc[k] - m_new : __builtin_fmaf(sc[k], qinv, -m_new));  // -inf -> 0
           lsum += sc[k];
         }
       };
@@ -1026,7 +1095,7 @@ __device__ __forceinline__ void chunk_block(const ChunkArgs& a, int4 it0, int4 i
         float mx = sc[0];
 #pragma unroll
         for (int k = 1; k < 16; ++k) mx = fmaxf(mx, sc[k]);
-        mx = fmaxf(mx, lane_xor<32>(mx, lane)) * qinv;
+        mx = fmaxf(mx, lane_xor<32>(mx, lane)) * (SHAPE ? 1.0f : qinv);
         m_new = mx > m_run + 8.0f ? mx : m_run;
         alpha = __builtin_amdgcn_exp2f(m_run - m_new);
         m_run = m_new;
@@ -1186,7 +1255,11 @@ __device__ __forceinline__ void chunk_block(const ChunkArgs& a, int4 it0, int4 i
             const int t0 = (e4 < 2 ? e_prev.x : e_prev.z) * PAGE + 8 * (e4 & 1) + 4 * lg;
             const float kk = (e4 < 2 ? ksa_prev.x : ksb_prev.x) * smk;
 #pragma unroll
-            for (int u = 0; u < 4; ++u) sc[4 * e4 + u] = t0 + u <= lim ? st_prev[4 * e4 + u] * kk : -INFINITY;
+            for (int u = 0; u < 4; ++u) {
+              float v = st_prev[4 * e4 + u] * kk;
+              if constexpr (SHAPE) v = shaped(v, (float)t0, u);
+              sc[4 * e4 + u] = sees(t0 + u) ? v : -INFINITY;
+            }
           };
           auto ex = [&](int k0) {
 #pragma unroll
@@ -1245,7 +1318,9 @@ __device__ __forceinline__ void chunk_block(const ChunkArgs& a, int4 it0, int4 i
       }
     }
     barrier();  // the PV waves' last pass
-    const float L = l_run + lane_xor<32>(l_run, lane);
+    float L = l_run + lane_xor<32>(l_run, lane);
+    if constexpr (SHAPE)  // the head's sink (cut blocks: in their merge); a row that saw nothing: 1 / inf
+      if (a.shape.sinks && !part) L += exp2f(a.shape.sinks[h * G + rho_l % G] * LOG2E_F - m_run);
     if (lg == 0) {
       if (part) reinterpret_cast<float2*>(part + 128 * D)[sw * 32 + li] = make_float2(m_run, L);
       else lbuf[sw * 32 + li] = L;
@@ -1489,19 +1564,18 @@ __device__ __forceinline__ void chunk_block(const ChunkArgs& a, int4 it0, int4 i
       if (rho < rows_r) {
         const float L = lbuf[g * 32 + li];
         const float inv = L > 0.0f ? 1.0f / L : 0.0f;
-        float* o = a.out + ((int64_t)(q0 + rho / G) * Hq + h * G + rho % G) * D + 2 * NBW * pv;
+        const int64_t o = ((int64_t)(q0 + rho / G) * Hq + h * G + rho % G) * D + 2 * NBW * pv;
 #pragma unroll
         for (int kk = 0; kk < 2; ++kk)
 #pragma unroll
           for (int u = 0; u < 4; ++u) {
-            const int rr = 8 * kk + 4 * lg + u;
-            if constexpr (NBW == 2)
-              *reinterpret_cast<float4*>(o + CL * rr) =
-                  make_float4(acc[0][g][4 * kk + u] * inv, acc[0][g][4 * kk + 8 + u] * inv,
-                              acc[1][g][4 * kk + u] * inv, acc[1][g][4 * kk + 8 + u] * inv);
-            else
-              *reinterpret_cast<float2*>(o + CL * rr) =
-                  make_float2(acc[0][g][4 * kk + u] * inv, acc[0][g][4 * kk + 8 + u] * inv);
+            float y[2 * NBW];
+#pragma unroll
+            for (int b = 0; b < NBW; ++b) {
+              y[2 * b] = acc[b][g][4 * kk + u] * inv;
+              y[2 * b + 1] = acc[b][g][4 * kk + 8 + u] * inv;
+            }
+            store_out<NBW, SHAPE != 0>(a.out, o + CL * (8 * kk + 4 * lg + u), y);
           }
       }
     }
@@ -1509,18 +1583,18 @@ __device__ __forceinline__ void chunk_block(const ChunkArgs& a, int4 it0, int4 i
 }
 
 // Grid (work item, KV head).
-template <int D>
+template <int D, int SHAPE>
 __global__ __launch_bounds__(64 * CW, 1) void chunk_kernel(ChunkArgs a) {
   extern __shared__ __align__(16) uint8_t smem[];
   const int gb = blockIdx.x;
   const int4 it0 = a.items[2 * gb], it1 = a.items[2 * gb + 1];  // (in the table whether planned or not)
   if (gb >= a.hdr[0]) return;
-  chunk_block<D>(a, it0, it1, blockIdx.y, smem);
+  chunk_block<D, SHAPE>(a, it0, it1, blockIdx.y, smem);
 }
 
 // Merge of the parts of cut blocks (Eq. softmax-merge): grid (cut block, KV
 // head, score wave), one thread per lane of a PV wave, with its accumulators' layout.
-template <int D>
+template <int D, bool SHAPE>
 __global__ __launch_bounds__(64 * NSW) void chunk_merge_kernel(ChunkArgs a, const int4* splits) {
   constexpr int CL = D / 16, NBW = D / 32 / NSW;
   if ((int)blockIdx.x >= a.hdr[1]) return;
@@ -1562,8 +1636,13 @@ __global__ __launch_bounds__(64 * NSW) void chunk_merge_kernel(ChunkArgs a, cons
       }
   }
   if (rho >= rows_r) return;
+  if constexpr (SHAPE)  // (M = -inf: a row that saw nothing; 1 / inf, unless the sink is -inf too)
+    if (a.shape.sinks) {
+      const float s2 = a.shape.sinks[h * G + rho % G] * LOG2E_F;
+      if (s2 != -INFINITY) L += exp2f(s2 - M);
+    }
   const float inv = L > 0.0f ? 1.0f / L : 0.0f;
-  float* dst = a.out + ((int64_t)(q0 + rho / G) * Hq + h * G + rho % G) * D + 2 * NBW * pv;
+  const int64_t dst = ((int64_t)(q0 + rho / G) * Hq + h * G + rho % G) * D + 2 * NBW * pv;
   // element 4 k' + u of block b is tile row 8 k' + 4 lg + u: chunk row rr = 8 kk +
   // 4 lg + u of half hh, k' = kk + 2 hh, channel CL rr + 2 b + hh of this wave's
   auto el = [](const float4& v, int u) { return u == 0 ? v.x : u == 1 ? v.y : u == 2 ? v.z : v.w; };
@@ -1572,18 +1651,20 @@ __global__ __launch_bounds__(64 * NSW) void chunk_merge_kernel(ChunkArgs a, cons
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
       const int rr = 8 * kk + 4 * lg + u;
-      if constexpr (NBW == 2)
-        *reinterpret_cast<float4*>(dst + CL * rr) = make_float4(el(o[0][kk], u) * inv, el(o[0][kk + 2], u) * inv,
-                                                                el(o[1][kk], u) * inv, el(o[1][kk + 2], u) * inv);
-      else
-        *reinterpret_cast<float2*>(dst + CL * rr) = make_float2(el(o[0][kk], u) * inv, el(o[0][kk + 2], u) * inv);
+      float y[2 * NBW];
+#pragma unroll
+      for (int b = 0; b < NBW; ++b) {
+        y[2 * b] = el(o[b][kk], u) * inv;
+        y[2 * b + 1] = el(o[b][kk + 2], u) * inv;
+      }
+      store_out<NBW, SHAPE>(a.out, dst + CL * rr, y);
     }
 }
 
 hipError_t launch_chunk(const PoolView& P, int layer, int n_req, const uint16_t* q,
                         const int32_t* cu_q, int n_q_total, const int32_t* bt, const uint8_t* tags,
-                        int max_pages, const int32_t* seq_lens, float* out, void* ws,
-                        size_t ws_bytes, hipStream_t s) {
+                        int max_pages, const int32_t* seq_lens, void* out, void* ws,
+                        size_t ws_bytes, hipStream_t s, const ShapeView* shape) {
   ChunkArgs a;
   a.P = P;
   a.layer = layer;
@@ -1609,19 +1690,23 @@ hipError_t launch_chunk(const PoolView& P, int layer, int n_req, const uint16_t*
   a.hdr = hdr;
   a.items = items;
   a.parts = reinterpret_cast<float*>(w + wl.parts);
-  a.sm_log2 = 1.4426950408889634f / sqrtf((float)P.d);
+  a.sm_log2 = shape && shape->scale > 0.0f ? shape->scale * LOG2E_F : 1.4426950408889634f / sqrtf((float)P.d);
+  a.shape = shape ? *shape : ShapeView{};
   hipLaunchKernelGGL(chunk_lists_kernel, dim3(n_req), dim3(LIST_NT), 0, s, bt, tags, max_pages, wl.stride,
                      seq_lens, P.n_fp8, P.n_tq3, list8, list3, cum, P.ctrl + CTRL_ERR);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const size_t lds = P.d == 256 ? (size_t)ChunkLds<256>::TOTAL : (size_t)ChunkLds<128>::TOTAL;
-  const void* kern = P.d == 256 ? (const void*)chunk_kernel<256> : (const void*)chunk_kernel<128>;
+  const int kind = !shape ? 0 : shape->cap != 0.0f ? 2 : 1;
+  const void* kerns[2][3] = {{(const void*)chunk_kernel<128, 0>, (const void*)chunk_kernel<128, 1>, (const void*)chunk_kernel<128, 2>},
+                             {(const void*)chunk_kernel<256, 0>, (const void*)chunk_kernel<256, 1>, (const void*)chunk_kernel<256, 2>}};
+  const void* kern = kerns[P.d == 256][kind];
   // the dynamic-LDS limit is raised once per kernel instance and device
   static std::atomic<uint32_t> attr_done[64];
   int dev = 0;
   e = hipGetDevice(&dev);
   if (e != hipSuccess) return e;
-  const uint32_t bit = P.d == 256 ? 2u : 1u;
+  const uint32_t bit = (P.d == 256 ? 2u : 1u) << 2 * kind;
   if (dev < 0 || dev >= 64 || !(attr_done[dev].load() & bit)) {
     e = hipFuncSetAttribute(kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
     if (e != hipSuccess) return e;
@@ -1637,7 +1722,7 @@ hipError_t launch_chunk(const PoolView& P, int layer, int n_req, const uint16_t*
   for (int b0 = 0; b0 < blocks; b0 += wl.n_items) {  // one turn where the workspace holds the call's items
     hipLaunchKernelGGL(chunk_plan_kernel, dim3(1), dim3(1024), 0, s, n_req, cu_q, n_q_total, seq_lens, max_pages,
                        P.group, blocks, b0, wl.n_items, share, cut ? 1 : 0, wl.n_parts, wl.stride, cum, rbo, hdr,
-                       items, splits, P.ctrl + CTRL_ERR);
+                       items, splits, P.ctrl + CTRL_ERR, a.shape.window, a.shape.first, a.shape.prefix);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
     int n = blocks - b0 < wl.n_items ? blocks - b0 : wl.n_items;
@@ -1647,10 +1732,9 @@ hipError_t launch_chunk(const PoolView& P, int layer, int n_req, const uint16_t*
     if (e != hipSuccess) return e;
     if (!cut || b0 > 0) continue;
     const dim3 mgrid(blocks < share ? blocks : share, P.n_kv_heads, NSW);
-    if (P.d == 256)
-      hipLaunchKernelGGL(chunk_merge_kernel<256>, mgrid, dim3(64 * NSW), 0, s, a, splits);
-    else
-      hipLaunchKernelGGL(chunk_merge_kernel<128>, mgrid, dim3(64 * NSW), 0, s, a, splits);
+    auto merge = [&](auto k) { hipLaunchKernelGGL(k, mgrid, dim3(64 * NSW), 0, s, a, splits); };
+    if (P.d == 256) shape ? merge(chunk_merge_kernel<256, true>) : merge(chunk_merge_kernel<256, false>);
+    else shape ? merge(chunk_merge_kernel<128, true>) : merge(chunk_merge_kernel<128, false>);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
   }

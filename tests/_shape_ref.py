@@ -72,3 +72,50 @@ def decode(orc, layer, q, bt, tags, lens, kw):
             for j in range(h * g, (h + 1) * g):
                 out[r, j], lse[r, j], to[r, j], tl[r, j] = attend_row(q[r, j], k, v, n - 1, **shape_of(kw, j, r, r))
     return out, lse, to, tl
+
+
+def chunk(orc, layer, q, cu, bt, tags, lens, kw):
+    """Chunk attention: out [n][hq][d] in 64 bits and a bound on the 2-norm of each row's error in bf16.
+
+    The rotated query is held in three E4M3 terms, 2^-14 of an entry each (or of the row's largest
+    entries where that is more): errors of independent signs, so a score is off by eta = 2^-14 B rms at
+    most, B the largest of |s|, the root of the sum of (q k)^2 and |q| |k| / sqrt d, all times the softmax
+    scale; the cap, the bias and the exponent add 2^-20 (|s| + |bias|).  The output moves by
+    sqrt(sum w^2 eta^2 |v - o|^2) rms, of which three times is never reached over a row's many signs; each
+    entry then rounds to bf16, 2^-8 of it, and a few weights that share all of a row are few signs:
+    2^-13 max|v - o| on top."""
+    hq, d = q.shape[1:]
+    g = hq // orc.n_kv_heads
+    out, tol = np.zeros(q.shape), np.zeros(q.shape[:2])
+    for r, n in enumerate(lens):
+        rows = np.arange(cu[r], cu[r + 1])
+        pos = n - len(rows) + np.arange(len(rows))
+        for h in range(orc.n_kv_heads):
+            k, v = orc.reconstruct(layer, r, h, bt, tags, n)
+            for j in range(h * g, (h + 1) * g):
+                f = shape_of({**kw, "first_keys": None}, j, 0, r)
+                scale = float(np.float32(f["scale"])) if f["scale"] else 1 / np.sqrt(d)
+                x = q[rows, j]
+                s = x @ k.T * scale
+                b = np.maximum(np.abs(s), np.sqrt((x * x) @ (k * k).T) * scale)
+                b = np.maximum(b, np.outer(np.linalg.norm(x, axis=1), np.linalg.norm(k, axis=1)) / np.sqrt(d) * scale)
+                if f["cap"]:
+                    s = f["cap"] * np.tanh(s / f["cap"])
+                bias = f.get("slope", 0.0) * np.abs(pos[:, None] - np.arange(n))
+                eta = 2.0 ** -14 * b + 2.0 ** -20 * (np.abs(s) + np.abs(bias))
+                s = s - bias
+                first = np.zeros(len(rows), int) if kw.get("first_keys") is None else np.asarray(kw["first_keys"])[rows]
+                for i in range(len(rows)):
+                    s[i, ~visible(pos[i], n, f["window"], int(first[i]), f.get("prefix", 0))] = -np.inf
+                top = np.maximum(s.max(1), f.get("sink", -np.inf))
+                top = np.where(top == -np.inf, 0.0, top)[:, None]
+                w = np.exp(s - top)
+                z = w.sum(1, keepdims=True) + np.exp(f.get("sink", -np.inf) - top)
+                w = w / np.where(z > 0, z, 1.0)
+                o = w @ v
+                away2 = (v * v).sum(1) - 2 * o @ v.T + (o * o).sum(1)[:, None]  # |v - o|^2
+                out[rows, j] = o
+                far = np.sqrt(np.where(w > 0, away2, 0.0).max(1, initial=0.0).clip(min=0.0))
+                tol[rows, j] = (3 * np.sqrt((w * w * eta * eta * away2.clip(min=0.0)).sum(1)) + 2.0 ** -13 * far
+                                + 2.0 ** -8 * np.linalg.norm(o, axis=1))
+    return out, tol
