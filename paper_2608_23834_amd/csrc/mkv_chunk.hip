@@ -448,6 +448,10 @@ __device__ __forceinline__ float vscale_rest(float s) {  // s over its power of 
 }
 constexpr float CM_INIT = -1.0e30f;  // running max before the first score (finite: no inf - inf)
 
+// kinds of a chunk instance, see chunk_block
+enum { SHAPE_MASK = 1, SHAPE_BIAS = 2, SHAPE_CAP = 3, SHAPE_ALL = 4 };
+constexpr float CAP_FAST = 128.0f;  // largest cap of SHAPE_CAP
+
 // LDS of a chunk workgroup (bytes): the ring of raw stages, two buffers of
 // unpacked key operands, two of unpacked value operands, two of the weights
 // the score waves hand to the PV waves, the rows' softmax denominators for
@@ -496,7 +500,14 @@ __device__ __forceinline__ void store_out(void* out, int64_t i, const float* y) 
 
 // One work item: passes of the 128-row block xb of request r and KV head h (the
 // body of a chunk workgroup; every wave of the workgroup runs it).
-// SHAPE: 1 biased and masked scores, 2 capped ones as well; bf16 rows out.
+// SHAPE (bf16 rows out): SHAPE_MASK masks alone; SHAPE_BIAS a bias by the distance; SHAPE_CAP a cap
+// of at most CAP_FAST, no bias; SHAPE_ALL any of them.  SHAPE_CAP: with r = 1 / (e^(2x / cap) + 1) a
+// capped score is cap - 2 cap r, so the smallest r has the largest score, and a weight is exp2 of one
+// FMA of r: two exponentials, a reciprocal and two instructions a score in place of one exponential
+// and the sixteen more of an exact tanh.  It is off by 2^-22 cap, 2^-15 at CAP_FAST, as much as the
+// rotated query's terms leave of a score of one, and bf16 rows have 2^-9.  (Four chunks of 512
+// queries after 12 to 16 K tokens, 24/4 heads, d = 256: 1,864 us, without a cap 1,714, with the
+// exact tanh 2,326.)
 template <int D, int SHAPE>
 __device__ __forceinline__ void chunk_block(const ChunkArgs& a, int4 it0, int4 it1, int h, uint8_t* smem) {
   constexpr int NDW = 3 * D / 128, CL = D / 16, QQ = D / 4;
@@ -576,10 +587,17 @@ __device__ __forceinline__ void chunk_block(const ChunkArgs& a, int4 it0, int4 i
     lo_max = __builtin_amdgcn_readfirstlane(lo_max);
   }
   // score v (base 2) of token t shaped; t0f the token's number less u
+  constexpr bool EARLY = SHAPE == SHAPE_BIAS || SHAPE == SHAPE_ALL;  // the row's factor before the max
+  constexpr bool RCP = SHAPE == SHAPE_CAP;                            // sc holds r, -inf's place taken by inf
   [[maybe_unused]] auto shaped = [&](float v, float t0f, int u) {
-    if constexpr (SHAPE == 2) v = shape_cap(a.shape, v);
+    if constexpr (SHAPE == SHAPE_ALL)
+      if (a.shape.cap != 0.0f) v = shape_cap(a.shape, v);
     return fmaf(slope, fabsf(t0f + (float)u - posf), v);
   };
+  // RCP: x times this is log2 of e^(2x / cap), x in base-2 units; weights are exp2(n2c r + c - m)
+  [[maybe_unused]] const float cap_k = 2.0f * LOG2E_F * a.shape.icap, n2c = -2.0f * a.shape.cap;
+  [[maybe_unused]] auto cap_r = [&](float v) { return __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(v) + 1.0f); };
+  constexpr float HIDDEN = RCP ? INFINITY : -INFINITY;
   auto sees = [&](int t) { return t <= lim && (!SHAPE || t >= lo); };
   float* const part = slot_out < 0 ? nullptr : a.parts + ((int64_t)slot_out * H + h) * chunk_part_floats(D);
   uint8_t* const kbuf = smem + LY::KB0;
@@ -994,7 +1012,8 @@ __device__ __forceinline__ void chunk_block(const ChunkArgs& a, int4 it0, int4 i
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
           float v = st[4 * e4 + u] * qinv * (float)reinterpret_cast<const _Float16*>(&gw[e4])[u];
-          if constexpr (SHAPE) v = shaped(v, (float)t0, u);
+          if constexpr (RCP) v = fmaf(n2c, cap_r(v * cap_k), a.shape.cap);
+          if constexpr (EARLY) v = shaped(v, (float)t0, u);
           if constexpr (decltype(masked)::value)
             sc[4 * e4 + u] = sees(t0 + u) ? v : -INFINITY;
           else
@@ -1064,20 +1083,24 @@ __device__ __forceinline__ void chunk_block(const ChunkArgs& a, int4 it0, int4 i
         for (int u = 0; u < 4; ++u) {
           // st * gamma as one mixed-precision FMA; the power-of-two row
           // factor qinv enters with the max and the exponent (exact)
-          // (SHAPE: here already, as cap and bias need the score itself)
+          // (here already where cap or bias need the score itself)
           float v = __builtin_fmaf((float)reinterpret_cast<const _Float16*>(&gw[e4])[u], st_prev[4 * e4 + u], 0.0f);
-          if constexpr (SHAPE) v = shaped(v * qinv, (float)t0, u);
+          if constexpr (EARLY) v = shaped(v * qinv, (float)t0, u);
+          if constexpr (RCP) v = cap_r(v * (qinv * cap_k));
           if constexpr (decltype(masked)::value)
-            sc[4 * e4 + u] = sees(t0 + u) ? v : -INFINITY;
+            sc[4 * e4 + u] = sees(t0 + u) ? v : HIDDEN;
           else
             sc[4 * e4 + u] = v;
         }
       };
       float m_new, alpha, lsum = 0.0f;
       auto ex = [&](int k0, int k1) {
+        [[maybe_unused]] const float cm = RCP ? a.shape.cap - m_new : 0.0f;
 #pragma unroll
         for (int k = k0; k < k1; ++k) {
-          sc[k] = __builtin_amdgcn_exp2f(SHAPE ? sc[k] - m_new : __builtin_fmaf(sc[k], qinv, -m_new));  // -inf -> 0
+          sc[k] = __builtin_amdgcn_exp2f(RCP     ? __builtin_fmaf(sc[k], n2c, cm)
+                                         : EARLY ? sc[k] - m_new
+                                                 : __builtin_fmaf(sc[k], qinv, -m_new));  // -inf -> 0
           lsum += sc[k];
         }
       };
@@ -1094,8 +1117,10 @@ __device__ __forceinline__ void chunk_block(const ChunkArgs& a, int4 it0, int4 i
       {
         float mx = sc[0];
 #pragma unroll
-        for (int k = 1; k < 16; ++k) mx = fmaxf(mx, sc[k]);
-        mx = fmaxf(mx, lane_xor<32>(mx, lane)) * (SHAPE ? 1.0f : qinv);
+        for (int k = 1; k < 16; ++k) mx = RCP ? fminf(mx, sc[k]) : fmaxf(mx, sc[k]);
+        const float other = lane_xor<32>(mx, lane);
+        if constexpr (RCP) mx = fmaf(n2c, fminf(mx, other), a.shape.cap);
+        else mx = fmaxf(mx, other) * (EARLY ? 1.0f : qinv);
         m_new = mx > m_run + 8.0f ? mx : m_run;
         alpha = __builtin_amdgcn_exp2f(m_run - m_new);
         m_run = m_new;
@@ -1253,18 +1278,20 @@ __device__ __forceinline__ void chunk_block(const ChunkArgs& a, int4 it0, int4 i
           float sc[16], alpha, lsum = 0.0f, m_new;
           auto scores = [&](int e4) {
             const int t0 = (e4 < 2 ? e_prev.x : e_prev.z) * PAGE + 8 * (e4 & 1) + 4 * lg;
-            const float kk = (e4 < 2 ? ksa_prev.x : ksb_prev.x) * smk;
+            const float kk = (e4 < 2 ? ksa_prev.x : ksb_prev.x) * (RCP ? smk * cap_k : smk);
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
               float v = st_prev[4 * e4 + u] * kk;
-              if constexpr (SHAPE) v = shaped(v, (float)t0, u);
-              sc[4 * e4 + u] = sees(t0 + u) ? v : -INFINITY;
+              if constexpr (EARLY) v = shaped(v, (float)t0, u);
+              if constexpr (RCP) v = cap_r(v);
+              sc[4 * e4 + u] = sees(t0 + u) ? v : HIDDEN;
             }
           };
           auto ex = [&](int k0) {
+            [[maybe_unused]] const float cm = RCP ? a.shape.cap - m_new : 0.0f;
 #pragma unroll
             for (int k = k0; k < k0 + 4; ++k) {
-              sc[k] = __builtin_amdgcn_exp2f(sc[k] - m_new);  // -inf -> 0
+              sc[k] = __builtin_amdgcn_exp2f(RCP ? __builtin_fmaf(sc[k], n2c, cm) : sc[k] - m_new);  // -inf -> 0
               lsum += sc[k];
             }
           };
@@ -1286,8 +1313,9 @@ __device__ __forceinline__ void chunk_block(const ChunkArgs& a, int4 it0, int4 i
           {
             float mx = sc[0];
 #pragma unroll
-            for (int k = 1; k < 16; ++k) mx = fmaxf(mx, sc[k]);
-            mx = fmaxf(mx, lane_xor<32>(mx, lane));
+            for (int k = 1; k < 16; ++k) mx = RCP ? fminf(mx, sc[k]) : fmaxf(mx, sc[k]);
+            const float other = lane_xor<32>(mx, lane);
+            mx = RCP ? fmaf(n2c, fminf(mx, other), a.shape.cap) : fmaxf(mx, other);
             m_new = mx > m_run + 8.0f ? mx : m_run;
             alpha = __builtin_amdgcn_exp2f(m_run - m_new);
             m_run = m_new;
@@ -1697,9 +1725,18 @@ hipError_t launch_chunk(const PoolView& P, int layer, int n_req, const uint16_t*
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const size_t lds = P.d == 256 ? (size_t)ChunkLds<256>::TOTAL : (size_t)ChunkLds<128>::TOTAL;
-  const int kind = !shape ? 0 : shape->cap != 0.0f ? 2 : 1;
-  const void* kerns[2][3] = {{(const void*)chunk_kernel<128, 0>, (const void*)chunk_kernel<128, 1>, (const void*)chunk_kernel<128, 2>},
-                             {(const void*)chunk_kernel<256, 0>, (const void*)chunk_kernel<256, 1>, (const void*)chunk_kernel<256, 2>}};
+  const bool cap = shape && shape->cap != 0.0f, bias = shape && shape->slopes;
+  const int kind = !shape                                                    ? 0
+                   : cap && !bias && shape->cap <= CAP_FAST * LOG2E_F ? SHAPE_CAP
+                   : cap                                                     ? SHAPE_ALL
+                   : bias                                                    ? SHAPE_BIAS
+                                                                             : SHAPE_MASK;
+  const void* kerns[2][5] = {{(const void*)chunk_kernel<128, 0>, (const void*)chunk_kernel<128, SHAPE_MASK>,
+                              (const void*)chunk_kernel<128, SHAPE_BIAS>, (const void*)chunk_kernel<128, SHAPE_CAP>,
+                              (const void*)chunk_kernel<128, SHAPE_ALL>},
+                             {(const void*)chunk_kernel<256, 0>, (const void*)chunk_kernel<256, SHAPE_MASK>,
+                              (const void*)chunk_kernel<256, SHAPE_BIAS>, (const void*)chunk_kernel<256, SHAPE_CAP>,
+                              (const void*)chunk_kernel<256, SHAPE_ALL>}};
   const void* kern = kerns[P.d == 256][kind];
   // the dynamic-LDS limit is raised once per kernel instance and device
   static std::atomic<uint32_t> attr_done[64];

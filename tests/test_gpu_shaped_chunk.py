@@ -57,6 +57,7 @@ def _kinds(hq, cu):
         dict(window=50, cap=3.0, slopes=_slopes(hq)), dict(window=1000), dict(first_keys=docs), dict(first_keys=odd, sinks=sinks),
         dict(first_keys=odd, cap=4.0, window=60), dict(prefix_lens=[1, 9, 640, 10 ** 6, 0, 2001]),
         dict(prefix_lens=[0, 17, 700, 300, -4, 5], window=30, slopes=_slopes(hq)), dict(scale=0.02, cap=50.0, prefix_lens=[5] * 6),
+        dict(cap=128.0, scale=0.5), dict(cap=200.0, scale=0.5), dict(cap=1e6, scale=0.5), dict(cap=1e-6),
     ]
 
 
