@@ -486,25 +486,33 @@ def kv_rope_apply(rope: Rope, x, positions, out, stream=None):
 class HeadNorm:
     """Norm of query or key heads (kv_head_norm): rows times 1 / sqrt(mean x^2 + eps) and the weights,
     bf16 (or its bits in int16) [head_dim], [heads][head_dim] or [layers][heads][head_dim]; None: ones.
-    unit_offset: the weights are kept as differences from one.  The object holds the tensor."""
+    unit_offset: the weights are kept as differences from one.  The object holds the tensor, whose
+    values may change, and is otherwise fixed."""
 
     def __init__(self, head_dim, weight=None, eps=1e-6, unit_offset=False):
-        self.head_dim, self.weight, self.eps, self.add = head_dim, weight, float(eps), 1.0 if unit_offset else 0.0
-        self._desc()
+        self.head_dim = head_dim
+        self._weight, self._shape, self._dev = weight, (), None
+        head = layer = 0
+        if weight is not None:
+            s = self._shape = tuple(weight.shape)
+            if weight.dtype not in _types()[0] or not weight.is_contiguous() or not 1 <= len(s) <= 3 or s[-1] != head_dim:
+                raise ValueError("weights are contiguous bf16 (or its bits in int16), [..][head_dim]")
+            self._dev = weight.get_device()
+            head, layer = head_dim if len(s) > 1 else 0, s[-2] * head_dim if len(s) > 2 else 0
+        self._desc = HeadNormDesc(head_dim, float(eps), 1.0 if unit_offset else 0.0, _ptr(weight), head, layer)
+        self._ref = ctypes.byref(self._desc)
 
-    def _desc(self, heads=None, layers=1, dev=None):
-        """The description for rows of `heads` heads and `layers` layers on device dev."""
-        w, d = self.weight, self.head_dim
-        if w is None:
-            return HeadNormDesc(d, self.eps, self.add, None, 0, 0)
-        s = w.shape
-        if w.dtype not in _types()[0] or not w.is_contiguous() or not 1 <= len(s) <= 3 or s[-1] != d:
-            raise ValueError("weights are contiguous bf16 (or its bits in int16), [..][head_dim]")
-        if heads is not None and (w.get_device() != dev or (len(s) > 1 and s[-2] != heads)
-                                  or (len(s) > 2 and s[0] != layers)):
+    @property
+    def weight(self):
+        return self._weight
+
+    def _for(self, dev, heads, layers=1):
+        """The description, for rows of `heads` heads and `layers` layers on device dev."""
+        s = self._shape
+        if s and (self._dev != dev or len(s) > 1 and s[-2] != heads or len(s) > 2 and s[0] != layers):
             raise ValueError(f"weights are [head_dim], [{heads}][head_dim] or [{layers}][{heads}][head_dim] on the "
                              "current device")
-        return HeadNormDesc(d, self.eps, self.add, w.data_ptr(), d if len(s) > 1 else 0, s[-2] * d if len(s) > 2 else 0)
+        return self._ref
 
 
 def kv_norm_rope_apply(rope, norm: HeadNorm, x, positions, out, stream=None):
@@ -515,9 +523,8 @@ def kv_norm_rope_apply(rope, norm: HeadNorm, x, positions, out, stream=None):
     n, heads, d = shape
     if out.shape != shape or d != norm.head_dim or (rope is not None and d != rope.head_dim):
         raise ValueError("x and out are [n][heads][head_dim]")
-    desc = norm._desc(heads, 1, dev)
     _check("kv_norm_rope_apply", lib().kv_norm_rope_apply(
-        None if rope is None else rope.handle, ctypes.byref(desc), n, heads, x.data_ptr(), _rows(dev, x, shape),
+        None if rope is None else rope.handle, norm._for(dev, heads), n, heads, x.data_ptr(), _rows(dev, x, shape),
         None if rope is None else _positions(dev, rope, positions, n), out.data_ptr(), _rows(dev, out, shape),
         cur if stream is None else stream.cuda_stream))
 
@@ -561,9 +568,8 @@ def kv_append_fp8_norm_rope(pool: Pool, rope, norm: HeadNorm, layer, block_table
     dev, cur = _current()
     n_req, max_pages, shape = _append_rows(dev, pool, layer, block_table, tags, seq_lens_before, cu_new_tokens, k, v)
     n = shape[-3]
-    desc = norm._desc(pool.n_kv_heads, shape[0] if layer < 0 else 1, dev)
     _check("kv_append_fp8_norm_rope", lib().kv_append_fp8_norm_rope(
-        pool.handle, None if rope is None else rope.handle, ctypes.byref(desc), layer, n_req, block_table.data_ptr(),
+        pool.handle, None if rope is None else rope.handle, norm._for(dev, pool.n_kv_heads, shape[0] if layer < 0 else 1), layer, n_req, block_table.data_ptr(),
         tags.data_ptr(), max_pages, seq_lens_before.data_ptr(), cu_new_tokens.data_ptr(), n,
         None if rope is None else _positions(dev, rope, positions, n), k.data_ptr(), _rows(dev, k, shape), v.data_ptr(),
         _rows(dev, v, shape), cur if stream is None else stream.cuda_stream))
@@ -694,21 +700,35 @@ class Shaping:
     """Scores and masks of shaped attention (paged_attn_shaping): softmax scale (0: 1 / sqrt(head_dim)),
     cap of the scores by a tanh (0: none), window of visible tokens (0: all), and device tensors or None:
     slopes float32 [n_q_heads] (bias -slope * distance), sinks float32 [n_q_heads], first_keys int32 [rows]
-    (first token each query row sees), prefix_lens int32 [n_req] (tokens seen from both sides; chunks)."""
+    (first token each query row sees), prefix_lens int32 [n_req] (tokens seen from both sides; chunks).
+    The object holds the tensors, whose values may change, and is otherwise fixed."""
 
     def __init__(self, scale=0.0, cap=0.0, window=0, slopes=None, sinks=None, first_keys=None, prefix_lens=None):
-        self.scale, self.cap, self.window = scale, cap, window
-        self.slopes, self.sinks, self.first_keys, self.prefix_lens = slopes, sinks, first_keys, prefix_lens
-
-    def _desc(self, dev, n_q_heads, rows, n_req):
         _, i32, f32 = _types()
-        for t, n, types in ((self.slopes, n_q_heads, f32), (self.sinks, n_q_heads, f32), (self.first_keys, rows, i32),
-                            (self.prefix_lens, n_req, i32)):
-            if t is not None and (t.get_device() != dev or t.dtype not in types or t.numel() < n or not t.is_contiguous()):
-                raise ValueError("slopes and sinks are float32 [n_q_heads], first_keys int32 [rows], prefix_lens int32 "
-                                 "[n_req], contiguous and on the current device")
-        return ShapingDesc(self.scale, self.cap, self.window, _ptr(self.slopes), _ptr(self.sinks), _ptr(self.first_keys),
-                           _ptr(self.prefix_lens))
+        self._tensors, self._dev = (slopes, sinks, first_keys, prefix_lens), None
+        most = []  # heads, heads, rows, requests that the tensors serve
+        for t, types in zip(self._tensors, (f32, f32, i32, i32)):
+            if t is None:
+                most.append(1 << 62)
+                continue
+            if t.dtype not in types or not t.is_contiguous() or self._dev not in (None, t.get_device()):
+                raise ValueError("slopes and sinks are float32, first_keys and prefix_lens int32, contiguous and on one device")
+            self._dev = t.get_device()
+            most.append(t.numel())
+        self._heads, self._rows, self._reqs = min(most[:2]), most[2], most[3]
+        self._desc = ShapingDesc(scale, cap, window, *map(_ptr, self._tensors))
+        self._ref = ctypes.byref(self._desc)
+
+    slopes = property(lambda self: self._tensors[0])
+    sinks = property(lambda self: self._tensors[1])
+    first_keys = property(lambda self: self._tensors[2])
+    prefix_lens = property(lambda self: self._tensors[3])
+
+    def _for(self, dev, heads, rows, n_req):
+        """The description, for so many query heads, rows and requests on device dev."""
+        if self._heads < heads or self._rows < rows or self._reqs < n_req or self._dev not in (None, dev):
+            raise ValueError("slopes and sinks are [n_q_heads], first_keys [rows], prefix_lens [n_req], on the current device")
+        return self._ref
 
 
 def paged_attn_decode_shaped(pool: Pool, shaping: Shaping, layer, q, block_table, tags, seq_lens, out, lse, ws,
@@ -725,9 +745,9 @@ def paged_attn_decode_shaped(pool: Pool, shaping: Shaping, layer, q, block_table
         _sizes((q, qs), (out, qs))
     if seq_lens.numel() < n_req or (lse is not None and lse.numel() < qs[0] * qs[1]):
         raise ValueError("seq_lens is [n_req], lse [n_req][n_q_heads]")
-    desc = shaping._desc(dev, pool.n_q_heads, n_req, n_req)
+    desc = shaping._for(dev, pool.n_q_heads, n_req, n_req)
     _check("paged_attn_decode_shaped", lib().paged_attn_decode_shaped(
-        pool.handle, ctypes.byref(desc), layer, n_req, q.data_ptr(), block_table.data_ptr(), tags.data_ptr(), max_pages,
+        pool.handle, desc, layer, n_req, q.data_ptr(), block_table.data_ptr(), tags.data_ptr(), max_pages,
         seq_lens.data_ptr(), out.data_ptr(), _ptr(lse), ws.data_ptr(), ws.nbytes,
         cur if stream is None else stream.cuda_stream))
 
@@ -749,12 +769,11 @@ def paged_attn_decode_append_shaped(pool: Pool, shaping: Shaping, rope, q_norm, 
         _sizes((q, qs), (out, qs), (k_new, ks), (v_new, ks))
     if seq_lens_before.numel() < n_req or (lse is not None and lse.numel() < qs[0] * qs[1]):
         raise ValueError("seq_lens_before is [n_req], lse [n_req][n_q_heads]")
-    desc = shaping._desc(dev, pool.n_q_heads, n_req, n_req)
-    qd = None if q_norm is None else q_norm._desc(pool.n_q_heads, 1, dev)
-    kd = None if k_norm is None else k_norm._desc(pool.n_kv_heads, 1, dev)
+    desc = shaping._for(dev, pool.n_q_heads, n_req, n_req)
+    qd = None if q_norm is None else q_norm._for(dev, pool.n_q_heads)
+    kd = None if k_norm is None else k_norm._for(dev, pool.n_kv_heads)
     _check("paged_attn_decode_append_shaped", lib().paged_attn_decode_append_shaped(
-        pool.handle, ctypes.byref(desc), None if rope is None else rope.handle, None if qd is None else ctypes.byref(qd),
-        None if kd is None else ctypes.byref(kd), layer, n_req, q.data_ptr(), k_new.data_ptr(), v_new.data_ptr(),
+        pool.handle, desc, None if rope is None else rope.handle, qd, kd, layer, n_req, q.data_ptr(), k_new.data_ptr(), v_new.data_ptr(),
         None if rope is None else _positions(dev, rope, positions, n_req), block_table.data_ptr(), tags.data_ptr(),
         max_pages, seq_lens_before.data_ptr(), out.data_ptr(), _ptr(lse), ws.data_ptr(), ws.nbytes,
         cur if stream is None else stream.cuda_stream))
@@ -811,9 +830,9 @@ def paged_attn_chunk_shaped(pool: Pool, shaping: Shaping, layer, q, cu_q, block_
         raise ValueError("q and out are [n][n_q_heads][head_dim]")
     if cu_q.numel() <= n_req or seq_lens.numel() < n_req:
         raise ValueError("cu_q is [n_req + 1], seq_lens [n_req]")
-    desc = shaping._desc(dev, pool.n_q_heads, q.shape[0], n_req)
+    desc = shaping._for(dev, pool.n_q_heads, q.shape[0], n_req)
     _check("paged_attn_chunk_shaped", lib().paged_attn_chunk_shaped(
-        pool.handle, ctypes.byref(desc), layer, n_req, q.data_ptr(), cu_q.data_ptr(), q.shape[0], block_table.data_ptr(),
+        pool.handle, desc, layer, n_req, q.data_ptr(), cu_q.data_ptr(), q.shape[0], block_table.data_ptr(),
         tags.data_ptr(), max_pages, seq_lens.data_ptr(), out.data_ptr(), ws.data_ptr(), ws.nbytes,
         cur if stream is None else stream.cuda_stream))
 

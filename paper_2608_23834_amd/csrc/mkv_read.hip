@@ -326,7 +326,7 @@ hipError_t launch_read_tokens(const PoolView& P, int layer, int n_req, const int
   const int64_t tasks = read_tasks(P, layer, n_req, n_total);
   a.n_tasks = (uint32_t)tasks;
   const int64_t wg = (tasks + 3) / 4;
-  const dim3 grid((unsigned)(wg < 4096 ? wg : 4096), k && v ? 2 : 1);
+  const dim3 grid((unsigned)(wg < 65536 ? wg : 65536), k && v ? 2 : 1);
   if (P.d == 256)
     hipLaunchKernelGGL(read_tokens_kernel<256>, grid, dim3(256), 0, s, a);
   else

@@ -70,13 +70,13 @@ __global__ __launch_bounds__(256) void rope_apply_kernel(RopeView R, int64_t t0,
 
 // rope_apply_kernel with every head normed and weighted first.  The lanes of a row add up its
 // squares over lane exchanges; U = 2 where a row has more lanes than a wave (d = 256, pairs of
-// one): a lane then holds two of them.
+// one): a lane then holds two of them.  FIG_ROWS
 template <int D, int V, bool NEAR>
 __global__ __launch_bounds__(256, 4) void norm_rope_apply_kernel(RopeView R, NormView N, int64_t t0, int n_here, int n_tokens,
                                                               int n_heads, int hb, const uint16_t* x, int64_t xs,
                                                               const int32_t* pos, uint16_t* out, int64_t os) {
   typedef typename RopeGroup<V>::type group;
-  constexpr int U = D / (2 * V) > 64 ? 2 : 1, LT = D / (2 * V) / U, HU = 4 / U;
+  constexpr int U = D / (2 * V) > 64 ? 2 : 1, LT = D / (2 * V) / U, HU = 2;
   const int nb = (n_heads + hb - 1) / hb;
   const int64_t unit = (int64_t)blockIdx.x * (256 / LT) + threadIdx.x / LT;
   if (unit >= (int64_t)n_here * nb) return;  // (all lanes of a row, so exchanges stay among those that are here)
@@ -85,10 +85,44 @@ __global__ __launch_bounds__(256, 4) void norm_rope_apply_kernel(RopeView R, Nor
   const int h0 = (int)(unit - tu * nb) * hb, h1 = min(h0 + hb, n_heads);
   int ca[U], cb[U];
   bool turn[U];
-  double c[U][V], s[U][V];
+#pragma unroll
+  for (int u = 0; u < U; ++u) turn[u] = rope_lane<V>(R, j + u * LT, ca[u], cb[u]);
+  const uint16_t* xr = x + t * xs;
+  uint16_t* orow = out + t * os;
+  uint32_t w[HU][U][V], ww[HU][U][V];  // two heads' values and weights, loaded while the two before are in work
+  auto load = [&](int hu) {
+#pragma unroll
+    for (int k = 0; k < HU; ++k)
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int h = min(hu + k, h1 - 1);
+        const uint16_t* xh = xr + (int64_t)h * D;
+        rope_words(*reinterpret_cast<const group*>(xh + ca[u]), *reinterpret_cast<const group*>(xh + cb[u]), w[k][u]);
+        if (N.head) {
+          const uint16_t* wh = N.w + h * N.head;
+          rope_words(*reinterpret_cast<const group*>(wh + ca[u]), *reinterpret_cast<const group*>(wh + cb[u]), ww[k][u]);
+        }
+      }
+  };
+  load(h0);
+  double wd[U][2 * V];  // weights of the head in work, of every head where they are the same
+  auto weigh = [&](int u, const uint32_t (&a)[V]) {
+    float f[2 * V];
+    rope_unpack<V>(a, f);
+#pragma unroll
+    for (int i = 0; i < 2 * V; ++i) wd[u][i] = (double)f[i] + N.add;
+  };
 #pragma unroll
   for (int u = 0; u < U; ++u) {
-    turn[u] = rope_lane<V>(R, j + u * LT, ca[u], cb[u]);
+    uint32_t one[V];
+#pragma unroll
+    for (int q = 0; q < V; ++q) one[q] = 0x3F803F80u;
+    if (N.w && !N.head) rope_words(*reinterpret_cast<const group*>(N.w + ca[u]), *reinterpret_cast<const group*>(N.w + cb[u]), one);
+    weigh(u, one);
+  }
+  double c[U][V], s[U][V];
+#pragma unroll
+  for (int u = 0; u < U; ++u)
 #pragma unroll
     for (int i = 0; i < V; ++i) {
       c[u][i] = 1.0;
@@ -98,31 +132,8 @@ __global__ __launch_bounds__(256, 4) void norm_rope_apply_kernel(RopeView R, Nor
         rope_cos_sin((double)pos[(int64_t)e.axis * n_tokens + t] * e.freq, R.scale, c[u][i], s[u][i]);
       }
     }
-  }
-  const uint16_t* xr = x + t * xs;
-  uint16_t* orow = out + t * os;
-  uint32_t ww[U][V];  // the weights of a head, of every head where they are the same
-  auto load_w = [&](int h) {
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-#pragma unroll
-      for (int q = 0; q < V; ++q) ww[u][q] = 0x3F803F80u;  // ones
-      if (N.w)
-        rope_words(*reinterpret_cast<const group*>(N.w + h * N.head + ca[u]),
-                   *reinterpret_cast<const group*>(N.w + h * N.head + cb[u]), ww[u]);
-    }
-  };
-  if (!N.head) load_w(0);
   for (int hu = h0; hu < h1; hu += HU) {
-    uint32_t w[HU][U][V];
-#pragma unroll
-    for (int k = 0; k < HU; ++k)
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const uint16_t* xh = xr + (int64_t)min(hu + k, h1 - 1) * D;
-        rope_words(*reinterpret_cast<const group*>(xh + ca[u]), *reinterpret_cast<const group*>(xh + cb[u]), w[k][u]);
-      }
-    double rs[HU];
+    double y[HU][U][2 * V], rs[HU];
 #pragma unroll
     for (int k = 0; k < HU; ++k) {
       rs[k] = 0.0;
@@ -131,32 +142,45 @@ __global__ __launch_bounds__(256, 4) void norm_rope_apply_kernel(RopeView R, Nor
         float v[2 * V];
         rope_unpack<V>(w[k][u], v);
 #pragma unroll
-        for (int i = 0; i < 2 * V; ++i) rs[k] = __builtin_fma((double)v[i], (double)v[i], rs[k]);
-        // (the words are read again below: the values in fp64 would fill the registers)
-#pragma unroll
-        for (int q = 0; q < V; ++q) asm volatile("" : "+v"(w[k][u][q]));
+        for (int i = 0; i < 2 * V; ++i) {
+          y[k][u][i] = (double)v[i];
+          rs[k] = __builtin_fma(y[k][u][i], y[k][u][i], rs[k]);
+        }
       }
     }
+    uint32_t wt[HU][U][V];
+#pragma unroll
+    for (int k = 0; k < HU; ++k)
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int q = 0; q < V; ++q) wt[k][u][q] = ww[k][u][q];
+    if (hu + HU < h1) load(hu + HU);
 #pragma unroll
     for (int k = 0; k < HU; ++k) rs[k] = norm_rstd(row_sum<LT>(rs[k], lane), D, N.eps);
 #pragma unroll
     for (int k = 0; k < HU; ++k) {
       if (hu + k >= h1) break;
-      if (N.head) load_w(hu + k);
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        float v[2 * V], f[2 * V];
-        rope_unpack<V>(w[k][u], v);
+        if (N.head) weigh(u, wt[k][u]);
 #pragma unroll
-        for (int q = 0; q < V; ++q) asm volatile("" : "+v"(ww[u][q]));
-        rope_unpack<V>(ww[u], f);
-        double y[2 * V];
+        for (int i = 0; i < 2 * V; ++i) y[k][u][i] = y[k][u][i] * rs[k] * wd[u][i];
+        if (turn[u]) {
+          constexpr int step = NEAR ? 2 : 1, other = NEAR ? 1 : V;
 #pragma unroll
-        for (int i = 0; i < 2 * V; ++i) y[i] = (double)v[i] * rs[k] * ((double)f[i] + N.add);
-        rope_turn_f64<V, NEAR>(y, v, turn[u], [&](int i) { return make_double2(c[u][i], s[u][i]); });
-        rope_pack<V>(v, w[k][u]);
+          for (int q = 0; q < V; ++q) {
+            const double x0 = y[k][u][step * q], x1 = y[k][u][step * q + other];
+            rope_rotate(x0, x1, c[u][q], s[u][q], y[k][u][step * q], y[k][u][step * q + other]);
+          }
+        }
+        float v[2 * V];
+#pragma unroll
+        for (int i = 0; i < 2 * V; ++i) v[i] = f64_round_bf16(y[k][u][i]);
+        uint32_t o[V];
+        rope_pack<V>(v, o);
         group a, b;
-        rope_groups<V>(w[k][u], a, b);
+        rope_groups<V>(o, a, b);
         uint16_t* oh = orow + (int64_t)(hu + k) * D;
         *reinterpret_cast<group*>(oh + ca[u]) = a;
         *reinterpret_cast<group*>(oh + cb[u]) = b;
