@@ -21,7 +21,7 @@
 //    the 32 rows, K = 64 channels; three MFMAs per k-step, one per query term)
 //    and, between those MFMAs, finishes pair p - 1: the causal mask, the online
 //    softmax in base 2 (lazy rescale, threshold 2^8) and the weights as fp16
-//    hi + lo pairs, handed over in LDS;
+//    hi + lo pairs (SHAPE, whose rows are bf16: as fp16 once), handed over in LDS;
 //  * four PV waves, wave v owning the 32-channel blocks 2v, 2v + 1 of all
 //    128 rows, hold O^T accumulators (32 channels x 32 rows per block and
 //    score wave) and compute O^T += V^T P^T on v_mfma_f32_32x32x16_f16 (M =
@@ -31,7 +31,7 @@
 //    zero term as one rank-2 product of the pages' zeros and weight sums,
 //    applying the rescale the score waves passed along first.
 // The pages and the page lists are copied (direct HBM -> LDS copies into a ring) by
-// the score waves at d = 256, by the PV waves at d = 128 (see COPY_PV).
+// the score waves at d = 256, by the PV waves at d = 128 and with SHAPE (see COPY_PV).
 // Pass p (one barrier): the score waves issue pair p's product and finish
 // pair p - 1 while the PV waves take pair p - 2.  FP8 pairs: the score waves
 // score them on the f16 MFMA against the plain query (the fp8 MFMA keeps too
@@ -238,6 +238,11 @@ __global__ __launch_bounds__(LIST_NT) void chunk_lists_kernel(const int32_t* bt,
 // units: 4 per pass, of either format (2.02 us per TQ3 pair and 1.88 per FP8 pair at
 // d = 256, 1.31 and 1.54 at d = 128, one workgroup on every CU; with 3 per FP8 pair a
 // 6,001-token prefill's twelve calls took 2,738 us, with 4 2,688).
+// With more than `share` blocks, up to twice as many, the second round is not full: where the call
+// allows it (tail: the most items then) the dearest `share` blocks stay whole and come first, and the
+// others are cut, at one of sixteen sizes, into parts that fill the round behind them.  It is estimated
+// as the dearest block and the rounds of the parts.  (Four chunks of 512 queries after 12 to 16 K tokens,
+// 24 heads over four, 96 blocks for 64 CUs per KV head, cap and prefix: 1,452 us whole, 1,107 so.)
 // items: two int4 per work item, {request, block of the request, first TQ3 pair,
 // TQ3 pairs}, {first FP8 pair, FP8 pairs, part slot or -1, -}; splits: {request,
 // block of the request, first part slot, parts}.
@@ -248,12 +253,12 @@ __global__ __launch_bounds__(1024) void chunk_plan_kernel(int n_req, const int32
                                                           int group, int grid, int b0, int n_items, int share,
                                                           int may_cut, int max_slots, int stride, const int2* cum,
                                                           int32_t* rbo, int32_t* hdr, int4* items,
-                                                          int4* splits, int32_t* err, int window,
+                                                          int4* splits, int32_t* err, int tail, int window,
                                                           const int32_t* first, const int32_t* prefix) {
   __shared__ int scratch[32];
   __shared__ int s_rbo[1025];
   __shared__ int s_r[MAX_ITEMS], s_x[MAX_ITEMS], s_t3[MAX_ITEMS], s_f8[MAX_ITEMS], s_a3[MAX_ITEMS], s_a8[MAX_ITEMS];
-  __shared__ int s_max, s_est[16], s_u[16];
+  __shared__ int s_max, s_est[16], s_u[16], s_rest[MAX_ITEMS], s_rmax;
   const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
   const int per = (n_req + 1023) / 1024;
   const int ra = min(n_req, tid * per), rb = min(n_req, ra + per);
@@ -386,10 +391,47 @@ __global__ __launch_bounds__(1024) void chunk_plan_kernel(int n_req, const int32
       best = s_est[w];
       U = s_u[w];
     }
+  int top = 0;  // blocks left whole, in the first items
+  bool whole = false;
+  int rank = 0;
+  if (tail && nblk > share) {  // workgroup-uniform
+    // the block's place by cost; s_rest: its cost where it is not among the first `share`
+    for (int b = 0; b < nblk; ++b) {
+      const int c = COST3 * s_t3[b] + COST8 * s_f8[b];
+      rank += c > cost || (c == cost && b < tid);
+    }
+    if (tid == 0) s_rmax = 0;
+    __syncthreads();  // (also: s_est is read)
+    if (tid < nblk) {
+      s_rest[tid] = rank < share ? 0 : cost;
+      if (rank >= share) atomicMax(&s_rmax, cost);
+    }
+    __syncthreads();
+    const int Ut = max(max(MIN_PART, (s_rmax + MAX_PARTS - 1) / MAX_PARTS), s_rmax / (wv + 1) + 1);
+    int n = 0;
+    for (int b = lane; b < nblk; b += 64) n += (s_rest[b] + Ut - 1) / Ut;
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) n += __shfl_xor(n, o, 64);
+    if (lane == 0) {
+      s_est[wv] = n <= max_slots && share + max(n, nblk - share) <= tail
+                      ? cmax + (n + share - 1) / share * (min(Ut, s_rmax) + CUT_COST) : 0x7FFFFFFF;
+      s_u[wv] = Ut;
+    }
+    __syncthreads();
+    for (int w = 0; w < 16; ++w)
+      if (s_est[w] < best) {
+        best = s_est[w];
+        U = s_u[w];
+        top = share;
+      }
+    whole = rank < top;
+  }
   // item and part slots
-  const int ns = tid < nblk ? max(1, (cost + U - 1) / U) : 0;
+  const int ns = tid < nblk ? whole ? 1 : max(1, (cost + U - 1) / U) : 0;
   int n_used, n_slots, n_split;
-  const int it0 = block_excl_scan(ns, scratch, &n_used);
+  int it0 = block_excl_scan(whole ? 0 : ns, scratch, &n_used) + top;
+  if (whole) it0 = rank;
+  n_used += top;
   const int sl0 = block_excl_scan(ns > 1 ? ns : 0, scratch, &n_slots);
   const int sp0 = block_excl_scan(ns > 1 ? 1 : 0, scratch, &n_split);
   if (tid < nblk) {
@@ -506,8 +548,9 @@ __device__ __forceinline__ void store_out(void* out, int64_t i, const float* y) 
 // FMA of r: two exponentials, a reciprocal and two instructions a score in place of one exponential
 // and the sixteen more of an exact tanh.  It is off by 2^-22 cap, 2^-15 at CAP_FAST, as much as the
 // rotated query's terms leave of a score of one, and bf16 rows have 2^-9.  (Four chunks of 512
-// queries after 12 to 16 K tokens, 24/4 heads, d = 256: 1,864 us, without a cap 1,714, with the
-// exact tanh 2,326.)
+// queries after 12 to 16 K tokens, 24/4 heads, d = 256: 1,107 us, without a cap 1,032, with a bias
+// 1,146; before the single products below, with the score waves copying and the blocks whole, 1,864,
+// 1,714 and with the exact tanh 2,326.)
 template <int D, int SHAPE>
 __device__ __forceinline__ void chunk_block(const ChunkArgs& a, int4 it0, int4 it1, int h, uint8_t* smem) {
   constexpr int NDW = 3 * D / 128, CL = D / 16, QQ = D / 4;
@@ -604,6 +647,16 @@ __device__ __forceinline__ void chunk_block(const ChunkArgs& a, int4 it0, int4 i
   uint8_t* const vbuf = smem + LY::VB0;
   uint8_t* const wbuf = smem + LY::WB0;
   float* const lbuf = reinterpret_cast<float*>(smem + LY::LB0);
+  // ONE (bf16 rows): weights and values enter their product rounded to fp16 once, 2^-12 of each at
+  // most, where the fp32 rows take both as pairs of halves: one product in place of three (FP8
+  // pages: two).  A TQ3 value is zero + scale * code, with terms larger than itself, so the zeros'
+  // weights and the row's sum are those of the rounded weights: what a row is off by is
+  // sum w delta (v - out), whatever the deltas have in common, and the rounded products of scale and
+  // code (the same call 1,714 us with the pairs, 1,518 so; with the sums by dot products of the
+  // halves, capped, 1,513 to 1,452).  The reference moves to BELOW under the largest score, so that weights as small as 2^-28 of
+  // the largest still count; no weight passes 2^8 for that.
+  constexpr bool ONE = SHAPE != 0;
+  constexpr float BELOW = ONE ? 3.0f : 0.0f;
   auto barrier = [&]() {
     wait_lgkm0();  // this wave's LDS reads and writes are done
     __builtin_amdgcn_s_barrier();
@@ -675,8 +728,10 @@ __device__ __forceinline__ void chunk_block(const ChunkArgs& a, int4 it0, int4 i
   // chain of scores, softmax and weights bounds a pass, so the PV waves copy
   // (per TQ3 and FP8 pass, one workgroup on every CU: d = 256 2.02 and 1.88 us with
   // the score waves copying, 2.21 and 2.12 with the PV waves; d = 128 1.46 and 1.67,
-  // 1.31 and 1.54).
-  constexpr bool COPY_PV = D == 128;
+  // 1.31 and 1.54).  With ONE the PV waves have a third of the products at d = 256 too and
+  // copy (a call of four chunks of 512 queries after 12 to 16 K tokens, whole blocks:
+  // 1,518 us with the score waves copying, 1,375 so).
+  constexpr bool COPY_PV = D == 128 || ONE;
   const int cwv = wid % NSW;
   // This wave's share of a unit's copies: OPS_W whole KiB (TQ3: KiB w OPS_W ..
   // of the two pages laid end to end, so waves 0 and 1 copy page a and waves
@@ -755,6 +810,29 @@ __device__ __forceinline__ void chunk_block(const ChunkArgs& a, int4 it0, int4 i
       }
       if (i < 0 || (i & 1)) e_iss = stage_at(stage_of_unit(issued), rd_iss);
     }
+  };
+  // refill in the passes over the TQ3 pairs once the ring is full: one unit a pass, and neither it
+  // nor the next one is the last TQ3 pair (so no page b is masked).  A wave issues an instruction
+  // every four cycles at most, so the hundred of the general form, most of them choices, took 900 of
+  // a pass's 3,700 cycles (d = 256)
+  auto refill3 = [&](int pass) {
+    if (issued != pass + CSLOTS - 2 || issued + 1 >= st3) {
+      refill(pass);
+      return;
+    }
+    if ((issued & 63) == 0 && (issued >> 6) + 2 < n_blk) issue_list((issued >> 6) + 2);
+    issue3(__builtin_amdgcn_readfirstlane(hw ? e_iss.w : e_iss.y), pl.so);
+    pl.so = pl.so == (CSLOTS - 1) * STAGE ? 0 : pl.so + STAGE;
+    ++issued;
+    if ((issued >> 6) != rd_iss.k) {
+      rd_iss.k = issued >> 6;
+      rd_iss.v = *reinterpret_cast<const int4*>(lsb + (rd_iss.k % LY::LBUF) * 1024 + lane * 16);
+      wait_lgkm0();
+    }
+    const int l = issued & 63;
+    e_iss.y = __builtin_amdgcn_readlane(rd_iss.v.y, l);
+    e_iss.z = __builtin_amdgcn_readlane(rd_iss.v.z, l);
+    e_iss.w = __builtin_amdgcn_readlane(rd_iss.v.w, l);
   };
   // before the barrier of pass p: pair p + 1 of the TQ3 pairs (its keys are
   // unpacked in pass p), pair p of the FP8 pairs has landed; the copies after it
@@ -890,36 +968,58 @@ __device__ __forceinline__ void chunk_block(const ChunkArgs& a, int4 it0, int4 i
 #pragma unroll
       for (int k = 1; k < 16; ++k) mx = fmaxf(mx, sc[k]);
       mx = fmaxf(mx, lane_xor<32>(mx, lane));
-      const float m_new = mx > m_run + 8.0f ? mx : m_run;
+      const float m_new = mx > m_run + 8.0f ? mx - BELOW : m_run;
       alpha = __builtin_amdgcn_exp2f(m_run - m_new);
       m_run = m_new;
       float lsum = 0.0f;
 #pragma unroll
       for (int k = 0; k < 16; ++k) {
         sc[k] = __builtin_amdgcn_exp2f(sc[k] - m_new);  // -inf -> 0
-        lsum += sc[k];
+        if constexpr (!ONE) lsum += sc[k];
       }
-      l_run = fmaf(l_run, alpha, lsum);
+      l_run = fmaf(l_run, alpha, lsum);  // ONE: without this tile's, see page_sums
     };
     // weights p[0..7] as an fp16 hi + lo pair (one token can carry most of
     // a row's mass, and its weight, taken against a lagging reference max,
     // is then not a power of two; a single fp16 rounding of it moves the
     // output by up to 2^-12 of that token's value)
     auto split8 = [&](const float* p, half8& hi, half8& lo) {
+      if constexpr (ONE) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) hi[k] = (_Float16)p[k];
+        return;
+      }
       uint32_t hh4[4], ll4[4];
 #pragma unroll
       for (int k = 0; k < 4; ++k) split2(p[2 * k], p[2 * k + 1], neg1, hh4[k], ll4[k]);
       hi = h8u(hh4[0], hh4[1], hh4[2], hh4[3]);
       lo = h8u(ll4[0], ll4[1], ll4[2], ll4[3]);
     };
+    // sums of the weights of a TQ3 pair's pages a and b (ONE: of the rounded ones, exact but for the
+    // last bits of fp32; the row's sum takes them here)
+    auto page_sums = [&](const float* sc, const TqW& w, float& ra, float& rb) {
+      if constexpr (ONE) {
+        const half2v one = {(_Float16)1.0f, (_Float16)1.0f};
+        ra = rb = 0.0f;
+#pragma unroll
+        for (int k = 0; k < 8; k += 2) {
+          ra = __builtin_amdgcn_fdot2(half2v{w.ha[k], w.ha[k + 1]}, one, ra, false);
+          rb = __builtin_amdgcn_fdot2(half2v{w.hb[k], w.hb[k + 1]}, one, rb, false);
+        }
+        l_run += ra + rb;
+      } else {
+        ra = ((sc[0] + sc[1]) + (sc[2] + sc[3])) + ((sc[4] + sc[5]) + (sc[6] + sc[7]));
+        rb = ((sc[8] + sc[9]) + (sc[10] + sc[11])) + ((sc[12] + sc[13]) + (sc[14] + sc[15]));
+      }
+    };
     // hand the weights of stage j (and the rescale the PV accumulators owe
     // before them; a TQ3 pair's zero term) to the PV waves
     auto put_weights = [&](int j, const TqW& w, float alpha, auto zero) {
       uint8_t* ws = wslot(j);
       *reinterpret_cast<half8*>(ws + 0 * 1024 + 16 * lane) = w.ha;
-      *reinterpret_cast<half8*>(ws + 1 * 1024 + 16 * lane) = w.la;
+      if constexpr (!ONE) *reinterpret_cast<half8*>(ws + 1 * 1024 + 16 * lane) = w.la;
       *reinterpret_cast<half8*>(ws + 2 * 1024 + 16 * lane) = w.hb;
-      *reinterpret_cast<half8*>(ws + 3 * 1024 + 16 * lane) = w.lb;
+      if constexpr (!ONE) *reinterpret_cast<half8*>(ws + 3 * 1024 + 16 * lane) = w.lb;
       if constexpr (decltype(zero)::value) *reinterpret_cast<half8*>(ws + 4 * 1024 + 16 * lane) = w.z;
       reinterpret_cast<float*>(ws + LY::WF_ALPHA)[lane] = alpha;
     };
@@ -971,7 +1071,7 @@ __device__ __forceinline__ void chunk_block(const ChunkArgs& a, int4 it0, int4 i
         for (int p = 0; p < 2; ++p) {
           const half2v s1 = bcast(*reinterpret_cast<const _Float16*>(rs + p * R3 + 12 * D + 32 + 2 * ch));
           const half2v sh = hi8x2(s1);
-          const half2v sp = {sh[0], s1[0] - sh[0]};  // exact split
+          const half2v sp = {ONE ? s1[0] : sh[0], s1[0] - sh[0]};  // exact split (ONE: whole)
           *reinterpret_cast<half2v*>(vb + LY::VX + ((p * NMB + mb) * 32 + rr) * 4) = sp;
           *reinterpret_cast<_Float16*>(vb + LY::VX + LY::SX + ((p * NMB + mb) * 32 + rr) * 2) =
               *reinterpret_cast<const _Float16*>(rs + p * R3 + 14 * D + 32 + 2 * ch);
@@ -1023,8 +1123,8 @@ __device__ __forceinline__ void chunk_block(const ChunkArgs& a, int4 it0, int4 i
       softmax(sc, alpha);
       split8(sc, w.ha, w.la);
       split8(sc + 8, w.hb, w.lb);
-      const float ra_ = ((sc[0] + sc[1]) + (sc[2] + sc[3])) + ((sc[4] + sc[5]) + (sc[6] + sc[7]));
-      const float rb_ = ((sc[8] + sc[9]) + (sc[10] + sc[11])) + ((sc[12] + sc[13]) + (sc[14] + sc[15]));
+      float ra_, rb_;
+      page_sums(sc, w, ra_, rb_);
       uint32_t zh, zl;
       split2(ra_, rb_, neg1, zh, zl);
       w.z = h8u(zh, zl, 0u, 0u);  // (R_a, R_b) hi, then lo
@@ -1101,7 +1201,7 @@ __device__ __forceinline__ void chunk_block(const ChunkArgs& a, int4 it0, int4 i
           sc[k] = __builtin_amdgcn_exp2f(RCP     ? __builtin_fmaf(sc[k], n2c, cm)
                                          : EARLY ? sc[k] - m_new
                                                  : __builtin_fmaf(sc[k], qinv, -m_new));  // -inf -> 0
-          lsum += sc[k];
+          if constexpr (!ONE) lsum += sc[k];
         }
       };
       TqW w;
@@ -1121,7 +1221,7 @@ __device__ __forceinline__ void chunk_block(const ChunkArgs& a, int4 it0, int4 i
         const float other = lane_xor<32>(mx, lane);
         if constexpr (RCP) mx = fmaf(n2c, fminf(mx, other), a.shape.cap);
         else mx = fmaxf(mx, other) * (EARLY ? 1.0f : qinv);
-        m_new = mx > m_run + 8.0f ? mx : m_run;
+        m_new = mx > m_run + 8.0f ? mx - BELOW : m_run;
         alpha = __builtin_amdgcn_exp2f(m_run - m_new);
         m_run = m_new;
       }
@@ -1144,8 +1244,8 @@ __device__ __forceinline__ void chunk_block(const ChunkArgs& a, int4 it0, int4 i
       __builtin_amdgcn_sched_barrier(0);
       mf(8);
       {
-        const float ra_ = ((sc[0] + sc[1]) + (sc[2] + sc[3])) + ((sc[4] + sc[5]) + (sc[6] + sc[7]));
-        const float rb_ = ((sc[8] + sc[9]) + (sc[10] + sc[11])) + ((sc[12] + sc[13]) + (sc[14] + sc[15]));
+        float ra_, rb_;
+        page_sums(sc, w, ra_, rb_);
         uint32_t zh, zl;
         split2(ra_, rb_, neg1, zh, zl);
         w.z = h8u(zh, zl, 0u, 0u);  // (R_a, R_b) hi, then lo
@@ -1193,7 +1293,7 @@ __device__ __forceinline__ void chunk_block(const ChunkArgs& a, int4 it0, int4 i
         else
           tq3_pass(p, st, std::true_type{}, std::false_type{});
       }
-      if constexpr (!COPY_PV) refill(p);
+      if constexpr (!COPY_PV) refill3(p);
       st_prev = st;
       e_prev = stage_at(p, rd_prev);
     }
@@ -1316,7 +1416,7 @@ __device__ __forceinline__ void chunk_block(const ChunkArgs& a, int4 it0, int4 i
             for (int k = 1; k < 16; ++k) mx = RCP ? fminf(mx, sc[k]) : fmaxf(mx, sc[k]);
             const float other = lane_xor<32>(mx, lane);
             mx = RCP ? fmaf(n2c, fminf(mx, other), a.shape.cap) : fmaxf(mx, other);
-            m_new = mx > m_run + 8.0f ? mx : m_run;
+            m_new = mx > m_run + 8.0f ? mx - BELOW : m_run;
             alpha = __builtin_amdgcn_exp2f(m_run - m_new);
             m_run = m_new;
           }
@@ -1412,7 +1512,7 @@ __device__ __forceinline__ void chunk_block(const ChunkArgs& a, int4 it0, int4 i
     auto ld_w2 = [&](int j, int t, W2& w) {
       const uint8_t* ws = wsl(j, t % NSW) + 2 * (t / NSW) * 1024 + 16 * lane;
       w.h = *reinterpret_cast<const half8*>(ws);
-      w.l = *reinterpret_cast<const half8*>(ws + 1024);
+      if constexpr (!ONE) w.l = *reinterpret_cast<const half8*>(ws + 1024);
     };
     auto tq3_pv = [&](int j) {
       const uint8_t* vb = vbuf + (j & 1) * LY::VB;
@@ -1437,7 +1537,7 @@ __device__ __forceinline__ void chunk_block(const ChunkArgs& a, int4 it0, int4 i
         const uint32_t c4 = q < 2 ? cw[p][b].x : cw[p][b].y;
         const half2v c = q & 1 ? cvt_code<true>(c4) : cvt_code<false>(c4);
         o.h[q] = c * sh;
-        o.l[q] = c * sl;
+        if constexpr (!ONE) o.l[q] = c * sl;
       };
       VOp op[2][NBW];
 #pragma unroll
@@ -1462,7 +1562,7 @@ __device__ __forceinline__ void chunk_block(const ChunkArgs& a, int4 it0, int4 i
         if (t == 2 * NSW - 1) ld_z(1);
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int k = 0; k < 3; ++k)
+        for (int k = 0; k < (ONE ? 1 : 3); ++k)
 #pragma unroll
           for (int b = 0; b < NBW; ++b) {
             const VOp& o = op[p][b];
@@ -1472,7 +1572,7 @@ __device__ __forceinline__ void chunk_block(const ChunkArgs& a, int4 it0, int4 i
             __builtin_amdgcn_sched_barrier(0);
           }
         if constexpr (COPY_PV)
-          if (t == REFILL_AT) refill(j + 2);  // the slots this pass frees
+          if (t == REFILL_AT) refill3(j + 2);  // the slots this pass frees
       }
 #pragma unroll
       for (int g = 0; g < NSW; ++g) {
@@ -1536,7 +1636,7 @@ __device__ __forceinline__ void chunk_block(const ChunkArgs& a, int4 it0, int4 i
         if (t + 2 < 2 * NSW) ld_w2(j, t + 2, w[(t + 2) % 3]);
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int k = 0; k < 2; ++k)
+        for (int k = 0; k < (ONE ? 1 : 2); ++k)
 #pragma unroll
           for (int b = 0; b < NBW; ++b) {
             acc[b][g] = __builtin_amdgcn_mfma_f32_32x32x16_f16(A[p][b], k ? w[t % 3].l : w[t % 3].h, acc[b][g], 0, 0, 0);
@@ -1610,14 +1710,15 @@ __device__ __forceinline__ void chunk_block(const ChunkArgs& a, int4 it0, int4 i
   }
 }
 
-// Grid (work item, KV head).
+// Grid (work item, KV head); SHAPE: (KV head, work item), so that the items of all heads start in the
+// plan's order, the whole blocks before the parts that fill the last round.
 template <int D, int SHAPE>
 __global__ __launch_bounds__(64 * CW, 1) void chunk_kernel(ChunkArgs a) {
   extern __shared__ __align__(16) uint8_t smem[];
-  const int gb = blockIdx.x;
+  const int gb = SHAPE ? blockIdx.y : blockIdx.x;
   const int4 it0 = a.items[2 * gb], it1 = a.items[2 * gb + 1];  // (in the table whether planned or not)
   if (gb >= a.hdr[0]) return;
-  chunk_block<D, SHAPE>(a, it0, it1, blockIdx.y, smem);
+  chunk_block<D, SHAPE>(a, it0, it1, SHAPE ? blockIdx.x : blockIdx.y, smem);
 }
 
 // Merge of the parts of cut blocks (Eq. softmax-merge): grid (cut block, KV
@@ -1756,16 +1857,20 @@ hipError_t launch_chunk(const PoolView& P, int layer, int n_req, const uint16_t*
   // (where the cut falls depends on every request of the call; deterministic pools keep
   // a row's bits to its own request)
   const bool cut = !P.deterministic && wl.n_parts > 0 && chunk_may_cut(n_q_total, P.group, P.n_kv_heads);
-  for (int b0 = 0; b0 < blocks; b0 += wl.n_items) {  // one turn where the workspace holds the call's items
+  // (a grid's second axis ends at 65,535)
+  const int turn = shape && wl.n_items > 65535 ? 65535 : wl.n_items;
+  const int tail = !shape || blocks <= share ? 0 : turn < 3 * share ? turn : 3 * share;
+  for (int b0 = 0; b0 < blocks; b0 += turn) {  // one turn where the workspace holds the call's items
     hipLaunchKernelGGL(chunk_plan_kernel, dim3(1), dim3(1024), 0, s, n_req, cu_q, n_q_total, seq_lens, max_pages,
-                       P.group, blocks, b0, wl.n_items, share, cut ? 1 : 0, wl.n_parts, wl.stride, cum, rbo, hdr,
-                       items, splits, P.ctrl + CTRL_ERR, a.shape.window, a.shape.first, a.shape.prefix);
+                       P.group, blocks, b0, turn, share, cut ? 1 : 0, wl.n_parts, wl.stride, cum, rbo, hdr,
+                       items, splits, P.ctrl + CTRL_ERR, tail, a.shape.window, a.shape.first, a.shape.prefix);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
-    int n = blocks - b0 < wl.n_items ? blocks - b0 : wl.n_items;
+    int n = blocks - b0 < turn ? blocks - b0 : turn;
     if (cut && b0 == 0 && n < 2 * share) n = 2 * share;
+    if (cut && b0 == 0 && n < tail) n = tail;
     void* args[] = {&a};
-    e = hipLaunchKernel(kern, dim3(n, P.n_kv_heads), dim3(64 * CW), args, lds, s);
+    e = hipLaunchKernel(kern, shape ? dim3(P.n_kv_heads, n) : dim3(n, P.n_kv_heads), dim3(64 * CW), args, lds, s);
     if (e != hipSuccess) return e;
     if (!cut || b0 > 0) continue;
     const dim3 mgrid(blocks < share ? blocks : share, P.n_kv_heads, NSW);

@@ -83,7 +83,14 @@ def chunk(orc, layer, q, cu, bt, tags, lens, kw):
     scale; the cap, the bias and the exponent add 2^-20 (|s| + |bias|).  The output moves by
     sqrt(sum w^2 eta^2 |v - o|^2) rms, of which three times is never reached over a row's many signs; each
     entry then rounds to bf16, 2^-8 of it, and a few weights that share all of a row are few signs:
-    2^-13 max|v - o| on top."""
+    2^-13 max|v - o| on top.
+
+    Weights and values are halves in their product.  A weight's 2^-12 moves the output as eta does (and
+    by 2^-12 of itself where the row's sum keeps the unrounded weight), and below 2^-14 of the reference,
+    2^-17 of the largest weight, it is off by 2^-25 (2^-28) whatever its size: n 2^-28 max|v - o|.  A TQ3
+    value is its page's least value, added apart, and a product of scale and code, off by 2^-12 of itself;
+    the tokens of a page may share that sign, the pages and channels do not: 3 2^-12 sqrt(sum over pages
+    |sum over its tokens w (v - least)|^2)."""
     hq, d = q.shape[1:]
     g = hq // orc.n_kv_heads
     out, tol = np.zeros(q.shape), np.zeros(q.shape[:2])
@@ -92,6 +99,10 @@ def chunk(orc, layer, q, cu, bt, tags, lens, kw):
         pos = n - len(rows) + np.arange(len(rows))
         for h in range(orc.n_kv_heads):
             k, v = orc.reconstruct(layer, r, h, bt, tags, n)
+            whole = orc.reconstruct(layer, r, h, bt, tags, -(-n // PAGE) * PAGE)[1].reshape(-1, PAGE, d)
+            part = np.zeros_like(whole).reshape(-1, d)  # scale times code
+            part[:n] = v - np.repeat(whole.min(1), PAGE, 0)[:n]
+            part = part.reshape(whole.shape)
             for j in range(h * g, (h + 1) * g):
                 f = shape_of({**kw, "first_keys": None}, j, 0, r)
                 scale = float(np.float32(f["scale"])) if f["scale"] else 1 / np.sqrt(d)
@@ -116,6 +127,13 @@ def chunk(orc, layer, q, cu, bt, tags, lens, kw):
                 away2 = (v * v).sum(1) - 2 * o @ v.T + (o * o).sum(1)[:, None]  # |v - o|^2
                 out[rows, j] = o
                 far = np.sqrt(np.where(w > 0, away2, 0.0).max(1, initial=0.0).clip(min=0.0))
-                tol[rows, j] = (3 * np.sqrt((w * w * eta * eta * away2.clip(min=0.0)).sum(1)) + 2.0 ** -13 * far
-                                + 2.0 ** -8 * np.linalg.norm(o, axis=1))
+                eta = eta + 2.0 ** -12
+                by_page = np.zeros((len(rows), whole.shape[0] * PAGE))
+                by_page[:, :n] = w
+                coded = np.zeros(len(rows))  # sum over pages of the squared norms
+                for g0 in range(whole.shape[0]):
+                    coded += ((by_page[:, g0 * PAGE:(g0 + 1) * PAGE] @ part[g0]) ** 2).sum(1)
+                tol[rows, j] = (3 * np.sqrt((w * w * eta * eta * away2.clip(min=0.0)).sum(1))
+                                + (2.0 ** -13 + n * 2.0 ** -28) * far + 3 * 2.0 ** -12 * np.sqrt(coded)
+                                + (2.0 ** -8 + 2.0 ** -12) * np.linalg.norm(o, axis=1))
     return out, tol

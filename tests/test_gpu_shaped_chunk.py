@@ -95,6 +95,42 @@ def test_long_chunks_and_few_blocks():
     assert mk.kv_pool_check_errors(t.gpu) == 0
 
 
+@pytest.mark.parametrize("lens,nq", [([2100, 700], [1100, 300]), ([1200, 1200], [640, 640]), ([1300], [1300])])
+def test_second_round_in_parts(lens, nq):
+    """More row blocks than compute units per KV head: the cheapest are cut behind the others."""
+    import paper_2608_23834_amd as mk
+    rng = np.random.default_rng(len(lens) + nq[0])
+    t = _twin(_w(128, 32, 32, len(lens)), lens, recent=256)
+    cu = np.r_[0, np.cumsum(nq)]
+    q = wl.bf16_round((2 * rng.standard_normal((cu[-1], 32, 128))).astype(np.float32))
+    for kw in (dict(cap=6.0, sinks=np.ones(32)), dict(window=900, prefix_lens=[900] * len(lens))):
+        want = sref.chunk(t.orc, 0, ref.bf16_f64(q), cu, t.obt, t.otags, t.cur, kw)
+        for det in (False, True):
+            mk.paged_attn_set_deterministic(t.gpu, det)
+            _near(_chunk(t, q, cu, kw), want)
+    assert mk.kv_pool_check_errors(t.gpu) == 0
+
+
+def test_more_row_blocks_than_a_grid_axis_holds():
+    import paper_2608_23834_amd as mk
+    torch = _torch()
+    rng = np.random.default_rng(2)
+    t = _twin(_w(128, 16, 1, 1), [16])
+    kw, n, m = dict(window=9, sinks=np.ones(16)), 8, 40000
+    q = _bits(rng, 9 * n, 16, 128)  # nine queries of sixteen heads: two blocks a request
+
+    def call(k):
+        out = torch.zeros((9 * k, 16, 128), dtype=torch.int16, device="cuda")
+        mk.paged_attn_chunk_shaped(t.gpu, _shaping(kw), 0, _i16(q).repeat(k // n, 1, 1), _i32(9 * np.arange(k + 1)),
+                                   t.bt.repeat(k, 1), t.tags.repeat(k, 1), _i32([16] * k), out,
+                                   mk.workspace(t.gpu, k, t.max_pages, 9 * k))
+        return out
+
+    few, many = call(n), call(m)
+    assert few.any() and torch.equal(many, few.repeat(m // n, 1, 1))
+    assert mk.kv_pool_check_errors(t.gpu) == 0
+
+
 def test_pages_that_no_row_sees_are_not_read():
     """A page without a readable id is left out; wholly outside the window it is listed but never read."""
     import paper_2608_23834_amd as mk
