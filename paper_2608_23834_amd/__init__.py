@@ -495,7 +495,8 @@ class HeadNorm:
         head = layer = 0
         if weight is not None:
             s = self._shape = tuple(weight.shape)
-            if weight.dtype not in _types()[0] or not weight.is_contiguous() or not 1 <= len(s) <= 3 or s[-1] != head_dim:
+            if (weight.dtype not in _types()[0] or not weight.is_contiguous() or not 1 <= len(s) <= 3
+                    or s[-1] != head_dim):
                 raise ValueError("weights are contiguous bf16 (or its bits in int16), [..][head_dim]")
             self._dev = weight.get_device()
             head, layer = head_dim if len(s) > 1 else 0, s[-2] * head_dim if len(s) > 2 else 0
@@ -569,7 +570,8 @@ def kv_append_fp8_norm_rope(pool: Pool, rope, norm: HeadNorm, layer, block_table
     n_req, max_pages, shape = _append_rows(dev, pool, layer, block_table, tags, seq_lens_before, cu_new_tokens, k, v)
     n = shape[-3]
     _check("kv_append_fp8_norm_rope", lib().kv_append_fp8_norm_rope(
-        pool.handle, None if rope is None else rope.handle, norm._for(dev, pool.n_kv_heads, shape[0] if layer < 0 else 1), layer, n_req, block_table.data_ptr(),
+        pool.handle, None if rope is None else rope.handle,
+        norm._for(dev, pool.n_kv_heads, shape[0] if layer < 0 else 1), layer, n_req, block_table.data_ptr(),
         tags.data_ptr(), max_pages, seq_lens_before.data_ptr(), cu_new_tokens.data_ptr(), n,
         None if rope is None else _positions(dev, rope, positions, n), k.data_ptr(), _rows(dev, k, shape), v.data_ptr(),
         _rows(dev, v, shape), cur if stream is None else stream.cuda_stream))
@@ -712,7 +714,8 @@ class Shaping:
                 most.append(1 << 62)
                 continue
             if t.dtype not in types or not t.is_contiguous() or self._dev not in (None, t.get_device()):
-                raise ValueError("slopes and sinks are float32, first_keys and prefix_lens int32, contiguous and on one device")
+                raise ValueError("slopes and sinks are float32, first_keys and prefix_lens int32, contiguous and on "
+                                 "one device")
             self._dev = t.get_device()
             most.append(t.numel())
         self._heads, self._rows, self._reqs = min(most[:2]), most[2], most[3]
@@ -727,7 +730,8 @@ class Shaping:
     def _for(self, dev, heads, rows, n_req):
         """The description, for so many query heads, rows and requests on device dev."""
         if self._heads < heads or self._rows < rows or self._reqs < n_req or self._dev not in (None, dev):
-            raise ValueError("slopes and sinks are [n_q_heads], first_keys [rows], prefix_lens [n_req], on the current device")
+            raise ValueError("slopes and sinks are [n_q_heads], first_keys [rows], prefix_lens [n_req], on the "
+                             "current device")
         return self._ref
 
 
@@ -752,8 +756,8 @@ def paged_attn_decode_shaped(pool: Pool, shaping: Shaping, layer, q, block_table
         cur if stream is None else stream.cuda_stream))
 
 
-def paged_attn_decode_append_shaped(pool: Pool, shaping: Shaping, rope, q_norm, k_norm, layer, q, k_new, v_new, positions,
-                                    block_table, tags, seq_lens_before, out, lse, ws, stream=None):
+def paged_attn_decode_append_shaped(pool: Pool, shaping: Shaping, rope, q_norm, k_norm, layer, q, k_new, v_new,
+                                    positions, block_table, tags, seq_lens_before, out, lse, ws, stream=None):
     """A decode step of one layer: query and key heads normed (q_norm, k_norm: HeadNorm or None) and rotated
     (rope or None), the token appended, attention with shaped scores; positions as in
     paged_attn_decode_append_rope."""
@@ -773,7 +777,8 @@ def paged_attn_decode_append_shaped(pool: Pool, shaping: Shaping, rope, q_norm, 
     qd = None if q_norm is None else q_norm._for(dev, pool.n_q_heads)
     kd = None if k_norm is None else k_norm._for(dev, pool.n_kv_heads)
     _check("paged_attn_decode_append_shaped", lib().paged_attn_decode_append_shaped(
-        pool.handle, desc, None if rope is None else rope.handle, qd, kd, layer, n_req, q.data_ptr(), k_new.data_ptr(), v_new.data_ptr(),
+        pool.handle, desc, None if rope is None else rope.handle, qd, kd, layer, n_req, q.data_ptr(), k_new.data_ptr(),
+        v_new.data_ptr(),
         None if rope is None else _positions(dev, rope, positions, n_req), block_table.data_ptr(), tags.data_ptr(),
         max_pages, seq_lens_before.data_ptr(), out.data_ptr(), _ptr(lse), ws.data_ptr(), ws.nbytes,
         cur if stream is None else stream.cuda_stream))

@@ -614,6 +614,9 @@ static mkv_status check_shaping(const paged_attn_shaping* sh, ShapeView* v) {
   if (!sh || sh->window < 0) return MKV_EINVAL;
   auto in = [](float x) { return x == 0.0f || (x >= 1e-6f && x <= 1e6f); };
   if (!in(sh->cap) || !in(sh->scale)) return MKV_ERANGE;  // (NaN too)
+  if ((reinterpret_cast<uintptr_t>(sh->slopes) | reinterpret_cast<uintptr_t>(sh->sinks) |
+       reinterpret_cast<uintptr_t>(sh->first_keys) | reinterpret_cast<uintptr_t>(sh->prefix_lens)) & 3)
+    return MKV_EINVAL;
   v->cap = sh->cap * LOG2E_F;
   v->icap = sh->cap != 0.0f ? 1.0f / v->cap : 0.0f;
   v->scale = sh->scale;

@@ -67,7 +67,8 @@ def _near(out, lse, want):
     o, l, to, tl = want
     err = np.abs(out - o).max(2)
     assert np.all(err <= to), (np.argwhere(err > to)[:4], (err / np.maximum(to, 1e-30)).max())
-    same = (lse == l) | (np.abs(np.where(np.isfinite(l), lse - l, np.inf)) <= tl)
+    both = np.isfinite(l) & np.isfinite(lse)
+    same = (lse == l) | (both & (np.abs(np.where(both, lse, 0.0) - np.where(both, l, 0.0)) <= tl))
     assert same.all(), (np.argwhere(~same)[:4], lse[~same][:4], l[~same][:4])
 
 
