@@ -40,10 +40,12 @@
 // takes each KV head's pages from a list instead of the whole table; SHAPE caps
 // and biases the scores and hides the tokens outside a window or a document, whose
 // pages it does not read (with APP and ROPE: the query and key heads are normed,
-// too, where asked).  The last three answer with fp32's error (FINE, below).  24 / 4 heads, d = 256, window 1,024:
+// too, where asked).  The last three answer with fp32's error (FINE, below).  24 / 4 heads, d = 256,
+// the pages' window of 1,024 tokens in FP8:
 // ROPE, 8 requests of 12,001 to 20,011 tokens (144 MB, 27.8 us of a copy's bandwidth):
 // 40.0 us a call, 4 of them the merge; SPARSE, 256 pages of each of 32 longer ones (170 MB,
-// 33.0 us): 41.3.
+// 33.0 us): 41.3; SHAPE, 32 requests of 8 to 32 K tokens, 4,096 of them seen, and sinks (171 MB,
+// 33.6 us): 40.3, and the ROPE call with both norms and a cap 45.2.
 #include <hip/hip_ext.h>
 #include <hip/hip_runtime.h>
 
