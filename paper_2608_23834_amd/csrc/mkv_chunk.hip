@@ -258,7 +258,8 @@ __global__ __launch_bounds__(1024) void chunk_plan_kernel(int n_req, const int32
   __shared__ int scratch[32];
   __shared__ int s_rbo[1025];
   __shared__ int s_r[MAX_ITEMS], s_x[MAX_ITEMS], s_t3[MAX_ITEMS], s_f8[MAX_ITEMS], s_a3[MAX_ITEMS], s_a8[MAX_ITEMS];
-  __shared__ int s_max, s_est[16], s_u[16], s_rest[MAX_ITEMS], s_rmax;
+  __shared__ int s_max, s_est[16], s_u[16], s_rmax;
+  __shared__ __align__(16) int s_rest[MAX_ITEMS];
   const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
   const int per = (n_req + 1023) / 1024;
   const int ra = min(n_req, tid * per), rb = min(n_req, ra + per);
@@ -395,13 +396,17 @@ __global__ __launch_bounds__(1024) void chunk_plan_kernel(int n_req, const int32
   bool whole = false;
   int rank = 0;
   if (tail && nblk > share) {  // workgroup-uniform
-    // the block's place by cost; s_rest: its cost where it is not among the first `share`
-    for (int b = 0; b < nblk; ++b) {
-      const int c = COST3 * s_t3[b] + COST8 * s_f8[b];
-      rank += c > cost || (c == cost && b < tid);
-    }
+    // the block's place by cost; s_rest: the costs, then those that are not among the first `share`
+    if (tid < MAX_ITEMS) s_rest[tid] = tid < nblk ? cost : -1;
     if (tid == 0) s_rmax = 0;
     __syncthreads();  // (also: s_est is read)
+    if (tid < nblk)
+      for (int b = 0; b < nblk; b += 4) {
+        const int4 c = *reinterpret_cast<const int4*>(s_rest + b);
+        rank += (c.x > cost || (c.x == cost && b < tid)) + (c.y > cost || (c.y == cost && b + 1 < tid)) +
+                (c.z > cost || (c.z == cost && b + 2 < tid)) + (c.w > cost || (c.w == cost && b + 3 < tid));
+      }
+    __syncthreads();
     if (tid < nblk) {
       s_rest[tid] = rank < share ? 0 : cost;
       if (rank >= share) atomicMax(&s_rmax, cost);
