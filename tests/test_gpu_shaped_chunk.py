@@ -95,6 +95,33 @@ def test_long_chunks_and_few_blocks():
     assert mk.kv_pool_check_errors(t.gpu) == 0
 
 
+@pytest.mark.parametrize("d", [128, 256])
+@pytest.mark.parametrize("power,shift,gain", [(-8, 0.0, 1.0), (-5, 0.0, 1.0), (4, 0.0, 1.0), (11, 0.0, 1.0), (0, 5.0, 2.0 ** -9),
+                                              (0, -3.0, 2.0 ** -13), (0, 0.0, 2.0 ** -11), (0, 20.0, 1.0)])
+def test_values_of_every_size_and_nearly_equal_scores(d, power, shift, gain):
+    """Values times a power of two, or about a common one, and queries whose scores hardly differ: what the
+    rounded weights share then must not reach the rows."""
+    import paper_2608_23834_amd as mk
+    from _harness import Twin
+    rng = np.random.default_rng(d + power + 20)
+    nq, w = [150, 40], _w(d, 8, 2, 2)
+    t = Twin(w, n_layers=1, lens=[1500, 40], recent=256)
+    for counts in ([1350, 0], [150, 40]):
+        k, v = zip(*(wl.kv_layer(w, 0, n, token_offset=r * 1_000_000 + t.cur[r]) for r, n in enumerate(counts) if n))
+        v = wl.bf16_round((wl.bf16_to_f32(np.concatenate(v)) * np.float32(2.0 ** power) + np.float32(shift)).astype(np.float32))
+        t.append(counts, layer_kv=(np.concatenate(k)[None], v[None]))
+    t.migrate()
+    assert (t.otags == 2).any() and (t.otags != 2).any()
+    cu = np.r_[0, np.cumsum(nq)]
+    q = wl.bf16_round((gain * rng.standard_normal((cu[-1], 8, d))).astype(np.float32))
+    for kw in ({}, dict(cap=30.0, first_keys=np.ones(cu[-1], np.int32))):
+        want = sref.chunk(t.orc, 0, ref.bf16_f64(q), cu, t.obt, t.otags, t.cur, kw)
+        for det in (False, True):
+            mk.paged_attn_set_deterministic(t.gpu, det)
+            _near(_chunk(t, q, cu, kw), want)
+    assert mk.kv_pool_check_errors(t.gpu) == 0
+
+
 @pytest.mark.parametrize("lens,nq", [([2100, 700], [1100, 300]), ([1200, 1200], [640, 640]), ([1300], [1300])])
 def test_second_round_in_parts(lens, nq):
     """More row blocks than compute units per KV head: the cheapest are cut behind the others."""
