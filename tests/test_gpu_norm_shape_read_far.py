@@ -112,3 +112,24 @@ def test_two_streams_at_a_time():
             for n in NAMES:
                 assert torch.equal(b[n], want[n]), n
     assert mk.kv_pool_check_errors(f.pool) == 0
+
+
+def test_rows_far_apart():
+    """Normed rows at the largest stride, in and out, and a weight stride of many heads."""
+    import torch
+    import paper_2608_23834_amd as mk
+    rng = np.random.default_rng(4)
+    rows = _i16(wl.bf16_round(rng.standard_normal((3, 3, D)).astype(np.float32)))
+    norm, rope = mk.HeadNorm(D, _i16(wl.bf16_round(rng.standard_normal((3, D)).astype(np.float32)))), mk.Rope(D, np.ones(16))
+    pos, want = _i32([[3, 70000, 0]]), torch.zeros_like(rows)
+    mk.kv_norm_rope_apply(rope, norm, rows, pos, want)
+    memory = torch.zeros(2 * 2 ** 31 + 3 * D, dtype=torch.int16, device="cuda")
+    far = memory.as_strided((3, 3, D), (2 ** 31, D, 1))
+    far.copy_(rows)
+    got = torch.zeros_like(rows)
+    mk.kv_norm_rope_apply(rope, norm, far, pos, got)
+    assert want.any() and torch.equal(got, want)
+    mk.kv_norm_rope_apply(rope, norm, far, pos, far)  # in place
+    assert torch.equal(far, want)
+    del far, memory
+    torch.cuda.empty_cache()
