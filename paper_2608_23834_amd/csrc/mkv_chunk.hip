@@ -495,8 +495,6 @@ __device__ __forceinline__ float vscale_rest(float s) {  // s over its power of 
 }
 constexpr float CM_INIT = -1.0e30f;  // running max before the first score (finite: no inf - inf)
 
-// kinds of a chunk instance, see chunk_block
-enum { SHAPE_MASK = 1, SHAPE_BIAS = 2, SHAPE_CAP = 3, SHAPE_ALL = 4 };
 constexpr float CAP_FAST = 128.0f;  // largest cap of SHAPE_CAP
 
 // LDS of a chunk workgroup (bytes): the ring of raw stages, two buffers of

@@ -324,7 +324,7 @@ __device__ __forceinline__ void p_operand(const float* p, bool row_is_b, half8& 
 // (see head_of_col).
 // ROPE, SPARSE: see DecodeArgs.
 template <int D, bool PAIR, bool G6, bool APP, bool SCORE = false, bool ROPE = false, bool SPARSE = false,
-          bool SHAPE = false>
+          int SHAPE = 0>
 __global__ __launch_bounds__(DecodeCfg<PAIR>::NT, PAIR && D == 128 ? 4 : 2) void decode_kernel(DecodeArgs a) {
   static_assert(!(APP && SCORE), "the scoring instance has no fused append");
   static_assert(APP || !ROPE, "rotation comes with the append");
@@ -1028,23 +1028,23 @@ __global__ __launch_bounds__(DecodeCfg<PAIR>::NT, PAIR && D == 128 ? 4 : 2) void
     if (lg == 0 && col_valid && lp < (S + PAGE - 1) / PAGE)
       a.page_mass[((int64_t)r * mp + lp) * Hq + h * G + col_head] = make_float2(ms, st.m_run);
   };
-  // SHAPE: the scores of tokens 4 lg .. + 3 of page lp capped, biased by their distance (capped
-  // first) and hidden before the first token; bias: a padding column's -inf, which no cap may lift
+  // SHAPE_CAP, SHAPE_ALL: the scores of tokens 4 lg .. + 3 of page lp capped, then biased by their
+  // distance; bias: a padding column's -inf, which no cap may lift (without a cap it is in the score
+  // already).  An instance of masks alone has neither: the branches around them cost 1.3 of 41 us.
   [[maybe_unused]] float slope = 0.0f;
-  if constexpr (SHAPE)
+  const bool capped = SHAPE == SHAPE_CAP || (SHAPE == SHAPE_ALL && a.shape.cap != 0.0f);
+  if constexpr (SHAPE == SHAPE_ALL)
     if (a.shape.slopes && col_valid) slope = a.shape.slopes[h * G + col_head] * LOG2E_F;
   [[maybe_unused]] auto shape_scores = [&](float* s, int lp, float bias) {
-    const int t = lp * PAGE + 4 * lg;
-    if (a.shape.cap != 0.0f) {
+    if (capped) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) s[i] = shape_cap(a.shape, s[i]);
+      for (int i = 0; i < 4; ++i) s[i] = shape_cap(a.shape, s[i]) + bias;
     }
-    if (a.shape.slopes) {
+    if constexpr (SHAPE == SHAPE_ALL) {
+      const int t = lp * PAGE + 4 * lg - (S - 1);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) s[i] = fmaf(slope, (float)(t + i - (S - 1)), s[i]);
+      for (int i = 0; i < 4; ++i) s[i] = fmaf(slope, (float)(t + i), s[i]);
     }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) s[i] = t + i < lo ? -INFINITY : s[i] + bias;
   };
   int k_st = 0;  // stages begun by this wave; stage k sits in slot k % SLOTS
   while (jc < st3) {
@@ -1125,15 +1125,15 @@ __global__ __launch_bounds__(DecodeCfg<PAIR>::NT, PAIR && D == 128 ? 4 : 2) void
     {
       const _Float16* gh = reinterpret_cast<const _Float16*>(&gw);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) sc[i] = fmaf((col_b ? sb[i] : sa[i]) * qinv, (float)gh[i], SHAPE ? 0.0f : col_bias);
-      if constexpr (SHAPE) shape_scores(sc, col_b ? e.z : e.x, col_bias);
+      for (int i = 0; i < 4; ++i) sc[i] = fmaf((col_b ? sb[i] : sa[i]) * qinv, (float)gh[i], capped ? 0.0f : col_bias);
+      if constexpr (SHAPE >= SHAPE_CAP) shape_scores(sc, col_b ? e.z : e.x, col_bias);
       // tokens at or past the end: only in a stage that holds the request's
-      // last page or a masked page b
-      if ((e.x + 1) * PAGE > S || (pair && (e.z + 1) * PAGE > S)) {
-        const int vcnt = S - (col_b ? e.z : e.x) * PAGE;
+      // last page or a masked page b (SHAPE: or the page of the first token)
+      if ((e.x + 1) * PAGE > S || (pair && (e.z + 1) * PAGE > S) || (SHAPE && e.x * PAGE < lo)) {
+        const int at = (col_b ? e.z : e.x) * PAGE, vcnt = S - at;
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-          if (4 * lg + i >= vcnt) sc[i] = -INFINITY;
+          if (4 * lg + i >= vcnt || (SHAPE && at + 4 * lg + i < lo)) sc[i] = -INFINITY;
       }
     }
     STAGE_PRIO(2);
@@ -1224,13 +1224,13 @@ __global__ __launch_bounds__(DecodeCfg<PAIR>::NT, PAIR && D == 128 ? 4 : 2) void
     {
       const float kk = FINE ? ksv.x * smk * pinv : ksv.x * smk;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) sc[i] = fmaf(sa[i], kk, SHAPE ? 0.0f : fp8_bias);
-      if constexpr (SHAPE) shape_scores(sc, e.x, fp8_bias);
-      if ((e.x + 1) * PAGE > S) {
+      for (int i = 0; i < 4; ++i) sc[i] = fmaf(sa[i], kk, capped ? 0.0f : fp8_bias);
+      if constexpr (SHAPE >= SHAPE_CAP) shape_scores(sc, e.x, fp8_bias);
+      if ((e.x + 1) * PAGE > S || (SHAPE && e.x * PAGE < lo)) {
         const int vcnt = S - e.x * PAGE;
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-          if (4 * lg + i >= vcnt) sc[i] = -INFINITY;
+          if (4 * lg + i >= vcnt || (SHAPE && e.x * PAGE + 4 * lg + i < lo)) sc[i] = -INFINITY;
       }
     }
     STAGE_PRIO(2);
@@ -1559,7 +1559,7 @@ static constexpr size_t lds_limit() {
   return 160 * 1024 - sizeof(int4) * MAX_CHUNK_PAGES - 2 * 16 * NW_MAX * sizeof(float) - 256;
 }
 
-template <bool APP, bool SCORE = false, bool ROPE = false, bool SPARSE = false, bool SHAPE = false>
+template <bool APP, bool SCORE = false, bool ROPE = false, bool SPARSE = false, int SHAPE = 0>
 static const void* decode_instance(int d, bool pair, bool g6) {
   if (d == 256)
     return g6 ? (const void*)decode_kernel<256, true, true, APP, SCORE, ROPE, SPARSE, SHAPE>
@@ -1628,23 +1628,30 @@ hipError_t launch_decode(const PoolView& P, int layer, int n_req, const uint16_t
   const size_t lds = qop_b + ring_b;  // the epilogue reuses each wave's ring slot
   if (lds > lds_limit()) return hipErrorInvalidValue;
   const bool g6 = pair && P.group <= 6;
-  const void* kern = shaped  ? app ? decode_instance<true, false, true, false, true>(P.d, pair, g6)
-                                   : decode_instance<false, false, false, false, true>(P.d, pair, g6)
+  const int kind = !shaped ? 0 : shape->slopes ? SHAPE_ALL : shape->cap != 0.0f ? SHAPE_CAP : SHAPE_MASK;
+  auto shaped_instance = [&](auto K) {
+    return app ? decode_instance<true, false, true, false, decltype(K)::value>(P.d, pair, g6)
+               : decode_instance<false, false, false, false, decltype(K)::value>(P.d, pair, g6);
+  };
+  const void* kern = kind == SHAPE_MASK  ? shaped_instance(std::integral_constant<int, SHAPE_MASK>{})
+                     : kind == SHAPE_CAP ? shaped_instance(std::integral_constant<int, SHAPE_CAP>{})
+                     : kind              ? shaped_instance(std::integral_constant<int, SHAPE_ALL>{})
                      : sparse  ? decode_instance<false, false, false, true>(P.d, pair, g6)
                      : turn  ? decode_instance<true, false, true>(P.d, pair, g6)
                      : app   ? decode_instance<true>(P.d, pair, g6)
                      : score ? decode_instance<false, true>(P.d, pair, g6)
                              : decode_instance<false>(P.d, pair, g6);
   // the dynamic-LDS limit is raised once per kernel instance and device
-  static std::atomic<uint64_t> attr_done[64];
+  static std::atomic<uint64_t> attr_done[2][64];  // [shaped]
   int dev = 0;
   hipError_t e = hipGetDevice(&dev);
   if (e != hipSuccess) return e;
-  const uint64_t bit = 1ull << ((shaped ? app ? 36 : 30 : sparse ? 24 : turn ? 18 : app ? 6 : score ? 12 : 0) + (P.d == 256 ? 3 : 0) + (g6 ? 2 : pair ? 1 : 0));
-  if (dev < 0 || dev >= 64 || !(attr_done[dev].load() & bit)) {
+  const int set = shaped ? 12 * (kind - 1) + (app ? 6 : 0) : sparse ? 24 : turn ? 18 : app ? 6 : score ? 12 : 0;
+  const uint64_t bit = 1ull << (set + (P.d == 256 ? 3 : 0) + (g6 ? 2 : pair ? 1 : 0));
+  if (dev < 0 || dev >= 64 || !(attr_done[shaped][dev].load() & bit)) {
     e = hipFuncSetAttribute(kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds_limit());
     if (e != hipSuccess) return e;
-    if (dev >= 0 && dev < 64) attr_done[dev].fetch_or(bit);
+    if (dev >= 0 && dev < 64) attr_done[shaped][dev].fetch_or(bit);
   }
   const dim3 grid = decode_chunks_last(P.d, pair) ? dim3(P.n_kv_heads, n_req, sh.max_chunks)
                                                 : dim3(sh.max_chunks, P.n_kv_heads, n_req);

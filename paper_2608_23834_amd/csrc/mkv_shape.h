@@ -20,6 +20,9 @@ struct ShapeView {
 
 constexpr float LOG2E_F = 1.4426950408889634f;
 
+// kinds of shaped instances: masks alone; a bias by the distance; a cap; any of them
+enum { SHAPE_MASK = 1, SHAPE_BIAS = 2, SHAPE_CAP = 3, SHAPE_ALL = 4 };
+
 // tanh in fp32: an odd polynomial below 0.55 (least squares of the relative error: 1.1 2^-24),
 // 1 - 2 / (e^2x + 1) above, where the quotient is at most half of the result's size, so the
 // hardware's exponential and reciprocal (an ulp each) leave less than 2 ulp.
