@@ -45,7 +45,7 @@
 // ROPE, 8 requests of 12,001 to 20,011 tokens (144 MB, 27.8 us of a copy's bandwidth):
 // 40.0 us a call, 4 of them the merge; SPARSE, 256 pages of each of 32 longer ones (170 MB,
 // 33.0 us): 41.3; SHAPE, 32 requests of 8 to 32 K tokens, 4,096 of them seen, and sinks (171 MB,
-// 33.6 us): 40.3, and the ROPE call with both norms and a cap 45.2.
+// 33.6 us): 40.1, and the ROPE call with both norms and a cap 43.4.
 #include <hip/hip_ext.h>
 #include <hip/hip_runtime.h>
 
@@ -1031,15 +1031,14 @@ __global__ __launch_bounds__(DecodeCfg<PAIR>::NT, PAIR && D == 128 ? 4 : 2) void
   // SHAPE_CAP, SHAPE_ALL: the scores of tokens 4 lg .. + 3 of page lp capped, then biased by their
   // distance; bias: a padding column's -inf, which no cap may lift (without a cap it is in the score
   // already).  An instance of masks alone has neither: the branches around them cost 1.3 of 41 us.
+  // (Eight requests of 12,001 to 20,011 tokens, both norms: 41.2 us without a cap, 42.5 with one that
+  // no score comes near, 44.5 where scores pass it.)
   [[maybe_unused]] float slope = 0.0f;
   const bool capped = SHAPE == SHAPE_CAP || (SHAPE == SHAPE_ALL && a.shape.cap != 0.0f);
   if constexpr (SHAPE == SHAPE_ALL)
     if (a.shape.slopes && col_valid) slope = a.shape.slopes[h * G + col_head] * LOG2E_F;
   [[maybe_unused]] auto shape_scores = [&](float* s, int lp, float bias) {
-    if (capped) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) s[i] = shape_cap(a.shape, s[i]) + bias;
-    }
+    if (capped) shape_cap<4>(a.shape, s, bias);
     if constexpr (SHAPE == SHAPE_ALL) {
       const int t = lp * PAGE + 4 * lg - (S - 1);
 #pragma unroll
