@@ -93,6 +93,9 @@ constexpr int CUT_COST = 12 * COST3, MIN_PART = 4 * COST3;
 // parts is estimated at MIN_PART + CUT_COST, and whole blocks take one round of the
 // dearest where cut ones could take one, two where they take two.
 constexpr int CUT_FROM = MIN_PART + CUT_COST;
+// Work items of a block of that cost, cut at U units a part.  A block without pages is one, too (its
+// rows become zeros), so the plan's estimates and its table count with this alone.
+__device__ __forceinline__ int block_items(int cost, int U) { return max(1, (cost + U - 1) / U); }
 static int64_t chunk_blocks(int n_q_total, int group) { return ((int64_t)n_q_total * group + NSW * 32 - 1) / (NSW * 32); }
 // Blocks are cut only where at least that many of them (the query ranges not
 // overlapping) leave room in two rounds.
@@ -376,7 +379,7 @@ __global__ __launch_bounds__(1024) void chunk_plan_kernel(int n_req, const int32
     int n = 0;
     for (int b = lane; b < nblk; b += 64) {
       const int c = COST3 * s_t3[b] + COST8 * s_f8[b];
-      n += max(1, (c + U - 1) / U);
+      n += block_items(c, U);
     }
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) n += __shfl_xor(n, o, 64);
@@ -396,7 +399,8 @@ __global__ __launch_bounds__(1024) void chunk_plan_kernel(int n_req, const int32
   bool whole = false;
   int rank = 0;
   if (tail && nblk > share) {  // workgroup-uniform
-    // the block's place by cost; s_rest: the costs, then those that are not among the first `share`
+    // the block's place by cost; s_rest: the costs, then those of the blocks that are not among the first
+    // `share`, -1 for these
     if (tid < MAX_ITEMS) s_rest[tid] = tid < nblk ? cost : -1;
     if (tid == 0) s_rmax = 0;
     __syncthreads();  // (also: s_est is read)
@@ -408,17 +412,17 @@ __global__ __launch_bounds__(1024) void chunk_plan_kernel(int n_req, const int32
       }
     __syncthreads();
     if (tid < nblk) {
-      s_rest[tid] = rank < share ? 0 : cost;
+      s_rest[tid] = rank < share ? -1 : cost;
       if (rank >= share) atomicMax(&s_rmax, cost);
     }
     __syncthreads();
     const int Ut = max(max(MIN_PART, (s_rmax + MAX_PARTS - 1) / MAX_PARTS), s_rmax / (wv + 1) + 1);
     int n = 0;
-    for (int b = lane; b < nblk; b += 64) n += (s_rest[b] + Ut - 1) / Ut;
+    for (int b = lane; b < nblk; b += 64) n += s_rest[b] < 0 ? 0 : block_items(s_rest[b], Ut);
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) n += __shfl_xor(n, o, 64);
     if (lane == 0) {
-      s_est[wv] = n <= max_slots && share + max(n, nblk - share) <= tail
+      s_est[wv] = n <= max_slots && share + n <= tail
                       ? cmax + (n + share - 1) / share * (min(Ut, s_rmax) + CUT_COST) : 0x7FFFFFFF;
       s_u[wv] = Ut;
     }
@@ -432,7 +436,7 @@ __global__ __launch_bounds__(1024) void chunk_plan_kernel(int n_req, const int32
     whole = rank < top;
   }
   // item and part slots
-  const int ns = tid < nblk ? whole ? 1 : max(1, (cost + U - 1) / U) : 0;
+  const int ns = tid < nblk ? whole ? 1 : block_items(cost, U) : 0;
   int n_used, n_slots, n_split;
   int it0 = block_excl_scan(whole ? 0 : ns, scratch, &n_used) + top;
   if (whole) it0 = rank;
