@@ -448,7 +448,8 @@ mkv_status paged_attn_decode_sparse(mkv_pool* pool, int32_t layer, int32_t n_req
  *    sees it.  State afterwards as by kv_append_fp8_norm_rope.
  *  - paged_attn_chunk_shaped is paged_attn_chunk with them, rows = queries, and with rows of
  *    bf16 out ([n_q_total][n_q_heads][d], what the next matrix product takes).  A block of 128
- *    rows reads the pages from the first to the last that any of its rows sees.  Weights and
+ *    rows reads the pages from the first to the last that any of its rows sees; the pages of a
+ *    request before the first that any of its rows sees are not read (nor checked).  Weights and
  *    values are rounded to fp16 for their product (sums in fp32), 2^-12 of each at most.
  * Errors also: EINVAL (shaping NULL, window negative), ERANGE (cap neither 0 nor in [1e-6, 1e6],
  * scale neither 0 nor in [1e-6, 1e6]).  Slopes and sinks are finite, or a sink -inf. */

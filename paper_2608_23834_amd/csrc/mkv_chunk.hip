@@ -159,15 +159,20 @@ size_t chunk_ws_least(int n_req, int max_pages) {
 // (an odd list ends with a masked page), and per logical page the counts of both
 // formats up to and including it.  Pages whose id lies outside their pool are left out
 // (a pool without TQ3 pages has no memory that could stand in), and set the range error
-// bit.  Four consecutive pages per thread, one scan of both counts per 4,096 pages: the
-// cost is round trips.
+// bit.  With a window or first keys the lists begin at the first page that any row of the
+// request sees: the pages before it may be gone, and would be read where one is the partner of
+// a page that is seen (its weights are zero, but its values need not be numbers).  Four
+// consecutive pages per thread, one scan of both counts per 4,096 pages: the cost is round
+// trips.
 constexpr int LIST_NT = 1024, LIST_KB = 4;
 __global__ __launch_bounds__(LIST_NT) void chunk_lists_kernel(const int32_t* bt, const uint8_t* tags,
                                                               int max_pages, int stride,
                                                               const int32_t* seq_lens, int n_fp8,
                                                               int n_tq3, int2* list8, int2* list3,
-                                                              int2* cum, int32_t* err) {
+                                                              int2* cum, int32_t* err, const int32_t* cu_q,
+                                                              int n_q_total, int window, const int32_t* first) {
   __shared__ int scratch[32];
+  __shared__ int s_first;
   const int r = blockIdx.x, tid = threadIdx.x;
   const int S = seq_lens[r];
   const int np = S >= 1 ? (S - 1) / PAGE + 1 : 0;
@@ -178,8 +183,27 @@ __global__ __launch_bounds__(LIST_NT) void chunk_lists_kernel(const int32_t* bt,
   int2* l8 = list8 + (int64_t)r * stride;
   int2* l3 = list3 + (int64_t)r * stride;
   int2* cm = cum + (int64_t)r * stride;
-  int b8 = 0, b3 = 0, bad = 0;
-  for (int c0 = 0; c0 < np; c0 += LIST_NT * LIST_KB) {
+  int b8 = 0, b3 = 0, bad = 0, pf = 0;  // pf: the lists' first page
+  if (window || first) {  // (a request whose queries are invalid is listed whole, and not read)
+    const int q0 = cu_q[r], q1 = cu_q[r + 1];
+    if (q0 >= 0 && q1 > q0 && q1 <= n_q_total && q1 - q0 <= S) {  // workgroup-uniform
+      const int p0 = S - (q1 - q0);  // position of the first query
+      int from = 0;
+      if (first) {
+        from = 0x7FFFFFFF;
+        for (int i = q0 + tid; i < q1; i += LIST_NT) from = min(from, first[i]);
+        if (tid == 0) s_first = 0x7FFFFFFF;
+        __syncthreads();
+        atomicMin(&s_first, from);
+        __syncthreads();
+        from = s_first;
+      }
+      if (window) from = max(from, p0 - window + 1);
+      pf = min(max(from, 0), p0) / PAGE;  // (no block's pages begin before it, see chunk_plan_kernel)
+      if (pf > 0 && tid == 0) cm[pf - 1] = make_int2(0, 0);
+    }
+  }
+  for (int c0 = pf; c0 < np; c0 += LIST_NT * LIST_KB) {
     int tg[LIST_KB], id[LIST_KB];
 #pragma unroll
     for (int j = 0; j < LIST_KB; ++j) {
@@ -1829,7 +1853,8 @@ hipError_t launch_chunk(const PoolView& P, int layer, int n_req, const uint16_t*
   a.sm_log2 = shape && shape->scale > 0.0f ? shape->scale * LOG2E_F : 1.4426950408889634f / sqrtf((float)P.d);
   a.shape = shape ? *shape : ShapeView{};
   hipLaunchKernelGGL(chunk_lists_kernel, dim3(n_req), dim3(LIST_NT), 0, s, bt, tags, max_pages, wl.stride,
-                     seq_lens, P.n_fp8, P.n_tq3, list8, list3, cum, P.ctrl + CTRL_ERR);
+                     seq_lens, P.n_fp8, P.n_tq3, list8, list3, cum, P.ctrl + CTRL_ERR, cu_q, n_q_total,
+                     a.shape.window, a.shape.first);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const size_t lds = P.d == 256 ? (size_t)ChunkLds<256>::TOTAL : (size_t)ChunkLds<128>::TOTAL;
