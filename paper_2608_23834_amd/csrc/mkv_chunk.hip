@@ -678,14 +678,16 @@ __device__ __forceinline__ void chunk_block(const ChunkArgs& a, int4 it0, int4 i
   uint8_t* const vbuf = smem + LY::VB0;
   uint8_t* const wbuf = smem + LY::WB0;
   float* const lbuf = reinterpret_cast<float*>(smem + LY::LB0);
-  // ONE (bf16 rows): weights and values enter their product rounded to fp16 once, 2^-12 of each at
-  // most, where the fp32 rows take both as pairs of halves: one product in place of three (FP8
-  // pages: two).  A TQ3 value is zero + scale * code, with terms larger than itself, so the zeros'
-  // weights and the row's sum are those of the rounded weights: what a row is off by is
-  // sum w delta (v - out), whatever the deltas have in common, and the rounded products of scale and
-  // code (the same call 1,714 us with the pairs, 1,518 so; with the sums by dot products of the
-  // halves, capped, 1,513 to 1,452).  The reference moves to BELOW under the largest score, so that weights as small as 2^-28 of
-  // the largest still count; no weight passes 2^8 for that.
+  // ONE (bf16 rows): weights and values enter their product rounded to fp16 once, 2^-11 of each at
+  // most (2^-25 of a weight below 2^-14), where the fp32 rows take both as pairs of halves: one product
+  // in place of three (FP8 pages: two).  The row's sum, and the weights of the zeros that a TQ3 value's
+  // scale * code is added to, are those of the rounded weights: what a row is off by is
+  // sum w delta (v - out), whatever the deltas have in common (equal scores: all of them), and the
+  // rounded products of scale and code.  (Four chunks of 512 queries after 12 to 16 K tokens, a cap, the
+  // blocks whole: 1,714 us with the pairs, 1,518 so; with the sums by dot products of the halves 1,513
+  // to 1,452.  The sums of FP8 pages, 1,102 to 1,112 of the present call.)  The reference moves to BELOW
+  // under the largest score, so that weights as small as 2^-28 of the largest still count; no weight
+  // passes 2^8 for that.
   constexpr bool ONE = SHAPE != 0;
   constexpr float BELOW = ONE ? 3.0f : 0.0f;
   auto barrier = [&]() {
@@ -1026,17 +1028,19 @@ __device__ __forceinline__ void chunk_block(const ChunkArgs& a, int4 it0, int4 i
       hi = h8u(hh4[0], hh4[1], hh4[2], hh4[3]);
       lo = h8u(ll4[0], ll4[1], ll4[2], ll4[3]);
     };
-    // sums of the weights of a TQ3 pair's pages a and b (ONE: of the rounded ones, exact but for the
-    // last bits of fp32; the row's sum takes them here)
+    // ONE: the sum of eight rounded weights, exact but for the last bits of fp32
+    auto half_sum = [&](const half8& w) {
+      const half2v one = {(_Float16)1.0f, (_Float16)1.0f};
+      float s = 0.0f;
+#pragma unroll
+      for (int k = 0; k < 8; k += 2) s = __builtin_amdgcn_fdot2(half2v{w[k], w[k + 1]}, one, s, false);
+      return s;
+    };
+    // sums of the weights of a TQ3 pair's pages a and b (ONE: the row's sum takes them here)
     auto page_sums = [&](const float* sc, const TqW& w, float& ra, float& rb) {
       if constexpr (ONE) {
-        const half2v one = {(_Float16)1.0f, (_Float16)1.0f};
-        ra = rb = 0.0f;
-#pragma unroll
-        for (int k = 0; k < 8; k += 2) {
-          ra = __builtin_amdgcn_fdot2(half2v{w.ha[k], w.ha[k + 1]}, one, ra, false);
-          rb = __builtin_amdgcn_fdot2(half2v{w.hb[k], w.hb[k + 1]}, one, rb, false);
-        }
+        ra = half_sum(w.ha);
+        rb = half_sum(w.hb);
         l_run += ra + rb;
       } else {
         ra = ((sc[0] + sc[1]) + (sc[2] + sc[3])) + ((sc[4] + sc[5]) + (sc[6] + sc[7]));
@@ -1423,16 +1427,27 @@ __device__ __forceinline__ void chunk_block(const ChunkArgs& a, int4 it0, int4 i
 #pragma unroll
             for (int k = k0; k < k0 + 4; ++k) {
               sc[k] = __builtin_amdgcn_exp2f(RCP ? __builtin_fmaf(sc[k], n2c, cm) : sc[k] - m_new);  // -inf -> 0
-              lsum += sc[k];
+              if constexpr (!ONE) lsum += sc[k];
             }
           };
-          // weights of page a (k0 = 0) or b (k0 = 8), the rest of the page's V scale folded in
+          // weights of page a (k0 = 0) or b (k0 = 8), the rest of the page's V scale folded in.
+          // ONE: the row's sum takes the rounded ones, less that rest, which is 1 to 2; of a page
+          // whose scale lies outside vscale_pow2's range (no values at all among them) the others
           auto split = [&](int k0, float vs, half8& hi, half8& lo) {
             const float vr = REST_EARLY ? vs : vscale_rest(vs);
             float pw[8];
 #pragma unroll
             for (int k = 0; k < 8; ++k) pw[k] = sc[k0 + k] * vr;
             split8(pw, hi, lo);
+            if constexpr (ONE) {
+              const float vu = __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(vr)));  // the page's
+              if (vu >= 1.0f && vu < 2.0f) {
+                lsum = __builtin_fmaf(half_sum(hi), __builtin_amdgcn_rcpf(vu), lsum);
+              } else {
+#pragma unroll
+                for (int k = 0; k < 8; ++k) lsum += sc[k0 + k];
+              }
+            }
           };
           mf(0);
           scores(0);
@@ -1461,9 +1476,10 @@ __device__ __forceinline__ void chunk_block(const ChunkArgs& a, int4 it0, int4 i
           ex(8);
           mf(7);
           ex(12);
-          l_run = fmaf(l_run, alpha, lsum);
+          if constexpr (!ONE) l_run = fmaf(l_run, alpha, lsum);
           mf(8);
           split(8, ksb_prev.y, w.hb, w.lb);
+          if constexpr (ONE) l_run = fmaf(l_run, alpha, lsum);
           mf(9);
           put_weights(p - 1, w, alpha, std::false_type{});
           rest_early();
