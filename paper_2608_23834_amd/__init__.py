@@ -487,21 +487,27 @@ class HeadNorm:
     """Norm of query or key heads (kv_head_norm): rows times 1 / sqrt(mean x^2 + eps) and the weights,
     bf16 (or its bits in int16) [head_dim], [heads][head_dim] or [layers][heads][head_dim]; None: ones.
     unit_offset: the weights are kept as differences from one.  The object holds the tensor, whose
-    values may change, and is otherwise fixed."""
+    values may change and whose memory may be replaced (as moving a module's parameters does), and is
+    otherwise fixed."""
 
     def __init__(self, head_dim, weight=None, eps=1e-6, unit_offset=False):
         self.head_dim = head_dim
         self._weight, self._shape, self._dev = weight, (), None
-        head = layer = 0
-        if weight is not None:
-            s = self._shape = tuple(weight.shape)
-            if (weight.dtype not in _types()[0] or not weight.is_contiguous() or not 1 <= len(s) <= 3
-                    or s[-1] != head_dim):
-                raise ValueError("weights are contiguous bf16 (or its bits in int16), [..][head_dim]")
-            self._dev = weight.get_device()
-            head, layer = head_dim if len(s) > 1 else 0, s[-2] * head_dim if len(s) > 2 else 0
-        self._desc = HeadNormDesc(head_dim, float(eps), 1.0 if unit_offset else 0.0, _ptr(weight), head, layer)
+        self._desc = HeadNormDesc(head_dim, float(eps), 1.0 if unit_offset else 0.0, None, 0, 0)
         self._ref = ctypes.byref(self._desc)
+        if weight is not None:
+            self._take()
+
+    def _take(self):
+        """The weights as they lie now, into the description."""
+        w, d = self._weight, self.head_dim
+        s = tuple(w.shape)
+        if w.dtype not in _types()[0] or not w.is_contiguous() or not 1 <= len(s) <= 3 or s[-1] != d:
+            raise ValueError("weights are contiguous bf16 (or its bits in int16), [..][head_dim]")
+        self._shape, self._dev = s, w.get_device()
+        desc = self._desc
+        desc.head_stride, desc.layer_stride = d if len(s) > 1 else 0, s[-2] * d if len(s) > 2 else 0
+        desc.weight = w.data_ptr()
 
     @property
     def weight(self):
@@ -509,6 +515,9 @@ class HeadNorm:
 
     def _for(self, dev, heads, layers=1):
         """The description, for rows of `heads` heads and `layers` layers on device dev."""
+        w = self._weight
+        if w is not None and w.data_ptr() != self._desc.weight:
+            self._take()
         s = self._shape
         if s and (self._dev != dev or len(s) > 1 and s[-2] != heads or len(s) > 2 and s[0] != layers):
             raise ValueError(f"weights are [head_dim], [{heads}][head_dim] or [{layers}][{heads}][head_dim] on the "
@@ -703,24 +712,33 @@ class Shaping:
     cap of the scores by a tanh (0: none), window of visible tokens (0: all), and device tensors or None:
     slopes float32 [n_q_heads] (bias -slope * distance), sinks float32 [n_q_heads], first_keys int32 [rows]
     (first token each query row sees), prefix_lens int32 [n_req] (tokens seen from both sides; chunks).
-    The object holds the tensors, whose values may change, and is otherwise fixed."""
+    The object holds the tensors, whose values may change and whose memory may be replaced, and is
+    otherwise fixed."""
 
     def __init__(self, scale=0.0, cap=0.0, window=0, slopes=None, sinks=None, first_keys=None, prefix_lens=None):
+        self._tensors = slopes, sinks, first_keys, prefix_lens
+        self._where = [t.data_ptr for t in self._tensors if t is not None]
+        self._desc = ShapingDesc(scale, cap, window)
+        self._ref = ctypes.byref(self._desc)
+        self._take()
+
+    def _take(self):
+        """The tensors as they lie now, into the description."""
         _, i32, f32 = _types()
-        self._tensors, self._dev = (slopes, sinks, first_keys, prefix_lens), None
-        most = []  # heads, heads, rows, requests that the tensors serve
+        dev, most = None, []  # most: heads, heads, rows, requests that the tensors serve
         for t, types in zip(self._tensors, (f32, f32, i32, i32)):
             if t is None:
                 most.append(1 << 62)
                 continue
-            if t.dtype not in types or not t.is_contiguous() or self._dev not in (None, t.get_device()):
+            if t.dtype not in types or not t.is_contiguous() or dev not in (None, t.get_device()):
                 raise ValueError("slopes and sinks are float32, first_keys and prefix_lens int32, contiguous and on "
                                  "one device")
-            self._dev = t.get_device()
+            dev = t.get_device()
             most.append(t.numel())
-        self._heads, self._rows, self._reqs = min(most[:2]), most[2], most[3]
-        self._desc = ShapingDesc(scale, cap, window, *map(_ptr, self._tensors))
-        self._ref = ctypes.byref(self._desc)
+        self._dev, self._heads, self._rows, self._reqs = dev, min(most[:2]), most[2], most[3]
+        d = self._desc
+        d.slopes, d.sinks, d.first_keys, d.prefix_lens = map(_ptr, self._tensors)
+        self._at = [p() for p in self._where]
 
     slopes = property(lambda self: self._tensors[0])
     sinks = property(lambda self: self._tensors[1])
@@ -729,6 +747,8 @@ class Shaping:
 
     def _for(self, dev, heads, rows, n_req):
         """The description, for so many query heads, rows and requests on device dev."""
+        if self._at != [p() for p in self._where]:
+            self._take()
         if self._heads < heads or self._rows < rows or self._reqs < n_req or self._dev not in (None, dev):
             raise ValueError("slopes and sinks are [n_q_heads], first_keys [rows], prefix_lens [n_req], on the "
                              "current device")
