@@ -963,6 +963,7 @@ __device__ __forceinline__ void chunk_block(const ChunkArgs& a, int4 it0, int4 i
       int ex = 0;
       (void)frexpf(amax, &ex);  // amax in [2^(ex-1), 2^ex)
       const bool ok = rho_l < rows_r && amax > 0.0f;
+      ex = max(ex, 8 - 100);  // (this factor and those of the plain query are fp32 numbers)
       const float qsc = ok ? ldexpf(1.0f, 8 - ex) : 0.0f;
       qinv = ok ? ldexpf(1.0f, ex - 8) : 1.0f;  // (the terms of such a row are all zero)
 #pragma unroll
@@ -1333,14 +1334,21 @@ __device__ __forceinline__ void chunk_block(const ChunkArgs& a, int4 it0, int4 i
       e_prev = stage_at(p, rd_prev);
     }
     // ---- passes over the FP8 pairs: pass p scores pair p with plain queries as
-    // fp16 (bf16 -> fp16 is exact for the query range) against its FP8 keys,
-    // straight from the ring, and between those MFMAs finishes the weights of
+    // fp16, times a power of two of each row that puts its largest entry between 2^5 and
+    // 2^15 (so what matters of a bf16 row is exact there, whatever its size), against its
+    // FP8 keys, straight from the ring, and between those MFMAs finishes the weights of
     // stage p - 1 (for p = st3 the last TQ3 pair, whose values it also unpacks);
     // the last pass only finishes.  Score rows 0-15 are page a's tokens, 16-31
     // page b's; lane (li, lg) holds, for k-step s, channels (D/2) lg + 8 s + b
     // (b < 8) of its row.
     {
       half8 qop[NKS];
+      // that power of two, from the rotated query's, which has the same 2-norm: smk times its
+      // largest entry over qinv lies in [2^7, 2^8), and the largest entries of the two are
+      // within a factor of sqrt(d) <= 2^4
+      const float smp = __uint_as_float(__float_as_uint(smk) & 0x7F800000u);
+      const float psc = 8.0f * smp * __int_as_float(0x7F000000 - __float_as_int(qinv));  // (1 / qinv)
+      const float smk8 = smk * __int_as_float(0x7F000000 - __float_as_int(smp)) * qinv * 0.125f;  // smk / psc
       if (n_f8 > 0) {
         const uint16_t* qrow = qrow_ptr + (D / 2) * lg;
 #pragma unroll
@@ -1348,7 +1356,7 @@ __device__ __forceinline__ void chunk_block(const ChunkArgs& a, int4 it0, int4 i
           const uint4 raw = *reinterpret_cast<const uint4*>(qrow + 8 * s);
           const uint16_t* hb = reinterpret_cast<const uint16_t*>(&raw);
 #pragma unroll
-          for (int j = 0; j < 8; ++j) qop[s][j] = (_Float16)bf16_to_f32(hb[j]);
+          for (int j = 0; j < 8; ++j) qop[s][j] = (_Float16)(bf16_to_f32(hb[j]) * psc);
         }
       }
       // key and value scales of the pages of FP8 stage p - 1, of the value scales the rest
@@ -1413,7 +1421,7 @@ __device__ __forceinline__ void chunk_block(const ChunkArgs& a, int4 it0, int4 i
           float sc[16], alpha, lsum = 0.0f, m_new;
           auto scores = [&](int e4) {
             const int t0 = (e4 < 2 ? e_prev.x : e_prev.z) * PAGE + 8 * (e4 & 1) + 4 * lg;
-            const float kk = (e4 < 2 ? ksa_prev.x : ksb_prev.x) * (RCP ? smk * cap_k : smk);
+            const float kk = (e4 < 2 ? ksa_prev.x : ksb_prev.x) * (RCP ? smk8 * cap_k : smk8);
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
               float v = st_prev[4 * e4 + u] * kk;
