@@ -440,7 +440,8 @@ mkv_status paged_attn_decode_sparse(mkv_pool* pool, int32_t layer, int32_t n_req
  * the device arrays when the kernels run (a captured call bakes in the rest of the struct).
  *  - paged_attn_decode_shaped is paged_attn_decode with them, rows = requests; prefix_lens is
  *    not read (a query at the end sees the whole prefix).  Pages wholly outside the window, or
- *    before first_keys, are not read (nor checked).  Outputs carry the error of fp32 arithmetic, as
+ *    before first_keys, are not read (nor checked).  The work is spread over the chip by the
+ *    table's width or the window, so documents go with a window as long as the longest.  Outputs carry the error of fp32 arithmetic, as
  *    paged_attn_decode_append_rope's do.  Buffers, workspace and errors as paged_attn_decode.
  *  - paged_attn_decode_append_shaped is paged_attn_decode_append_rope with them, and with the
  *    query and key heads normed before the rotation (q_norm, k_norm, each may be NULL: not
@@ -449,8 +450,10 @@ mkv_status paged_attn_decode_sparse(mkv_pool* pool, int32_t layer, int32_t n_req
  *  - paged_attn_chunk_shaped is paged_attn_chunk with them, rows = queries, and with rows of
  *    bf16 out ([n_q_total][n_q_heads][d], what the next matrix product takes).  A block of 128
  *    rows reads the pages from the first to the last that any of its rows sees; the pages of a
- *    request before the first that any of its rows sees are not read (nor checked).  Weights and
- *    values are rounded to fp16 for their product (sums in fp32), 2^-12 of each at most.
+ *    request before the first that any of its rows sees are not read (nor checked).  Those that
+ *    are read hold finite values, also where a row does not see them.  Weights and values are
+ *    rounded to fp16 for their product (sums in fp32): 2^-11 of each at most, or 2^-28 of the
+ *    row's largest weight where that is more.
  * Errors also: EINVAL (shaping NULL, window negative), ERANGE (cap neither 0 nor in [1e-6, 1e6],
  * scale neither 0 nor in [1e-6, 1e6]).  Slopes and sinks are finite, or a sink -inf. */
 typedef struct paged_attn_shaping {

@@ -269,7 +269,7 @@ __global__ __launch_bounds__(LIST_NT) void chunk_lists_kernel(const int32_t* bt,
 // allows it (tail: the most items then) the dearest `share` blocks stay whole and come first, and the
 // others are cut, at one of sixteen sizes, into parts that fill the round behind them.  It is estimated
 // as the dearest block and the rounds of the parts.  (Four chunks of 512 queries after 12 to 16 K tokens,
-// 24 heads over four, 96 blocks for 64 CUs per KV head, cap and prefix: 1,452 us whole, 1,107 so.)
+// 24 heads over four, 96 blocks for 64 CUs per KV head, cap and prefix: 1,452 us whole, 1,107 so, then.)
 // items: two int4 per work item, {request, block of the request, first TQ3 pair,
 // TQ3 pairs}, {first FP8 pair, FP8 pairs, part slot or -1, -}; splits: {request,
 // block of the request, first part slot, parts}.
@@ -578,10 +578,11 @@ __device__ __forceinline__ void store_out(void* out, int64_t i, const float* y) 
 // capped score is cap - 2 cap r, so the smallest r has the largest score, and a weight is exp2 of one
 // FMA of r: two exponentials, a reciprocal and two instructions a score in place of one exponential
 // and the sixteen more of an exact tanh.  It is off by 2^-22 cap, 2^-15 at CAP_FAST, as much as the
-// rotated query's terms leave of a score of one, and bf16 rows have 2^-9.  (Four chunks of 512
-// queries after 12 to 16 K tokens, 24/4 heads, d = 256: 1,107 us, without a cap 1,032, with a bias
-// 1,146; before the single products below, with the score waves copying and the blocks whole, 1,864,
-// 1,714 and with the exact tanh 2,326.)
+// rotated query's terms leave of a score of one, and bf16 rows have 2^-8.  (Four chunks of 512
+// queries after 12 to 16 K tokens, 24/4 heads, d = 256: 1,111 us, without a cap 1,020, with a bias
+// 1,157, with both 1,447; before the single products below, with the score waves copying and the blocks
+// whole, 1,864, 1,714 and with the exact tanh 2,326.  Six chunks of 1 to 300 queries, d = 128: cap 178,
+// masks 171, bias 180, both 242.)
 template <int D, int SHAPE>
 __device__ __forceinline__ void chunk_block(const ChunkArgs& a, int4 it0, int4 it1, int h, uint8_t* smem) {
   constexpr int NDW = 3 * D / 128, CL = D / 16, QQ = D / 4;
@@ -683,9 +684,9 @@ __device__ __forceinline__ void chunk_block(const ChunkArgs& a, int4 it0, int4 i
   // in place of three (FP8 pages: two).  The row's sum, and the weights of the zeros that a TQ3 value's
   // scale * code is added to, are those of the rounded weights: what a row is off by is
   // sum w delta (v - out), whatever the deltas have in common (equal scores: all of them), and the
-  // rounded products of scale and code.  (Four chunks of 512 queries after 12 to 16 K tokens, a cap, the
-  // blocks whole: 1,714 us with the pairs, 1,518 so; with the sums by dot products of the halves 1,513
-  // to 1,452.  The sums of FP8 pages, 1,102 to 1,112 of the present call.)  The reference moves to BELOW
+  // rounded products of scale and code.  (Four chunks of 512 queries after 12 to 16 K tokens, the blocks
+  // whole: without a cap 1,714 us with the pairs, 1,518 so; capped, with the sums by dot products of
+  // the halves, 1,513 to 1,452.  The sums over FP8 pages, blocks cut: 1,102 to 1,112.)  The reference moves to BELOW
   // under the largest score, so that weights as small as 2^-28 of the largest still count; no weight
   // passes 2^8 for that.
   constexpr bool ONE = SHAPE != 0;
@@ -1016,7 +1017,7 @@ __device__ __forceinline__ void chunk_block(const ChunkArgs& a, int4 it0, int4 i
     // weights p[0..7] as an fp16 hi + lo pair (one token can carry most of
     // a row's mass, and its weight, taken against a lagging reference max,
     // is then not a power of two; a single fp16 rounding of it moves the
-    // output by up to 2^-12 of that token's value)
+    // output by up to 2^-11 of that token's value)
     auto split8 = [&](const float* p, half8& hi, half8& lo) {
       if constexpr (ONE) {
 #pragma unroll
