@@ -494,8 +494,9 @@ mkv_status paged_attn_chunk_shaped(mkv_pool* pool, const paged_attn_shaping* sha
  * Either of k and v may be NULL, not both; they may not be the same.  A range that does not
  * lie in [0, 16 * max_pages]: RANGE, and its rows become zeros; so do the rows of a page that
  * is not mapped or has another tag (BAD_TAG) or an id out of range (RANGE).  cu_tokens that do
- * not begin with 0 or end with n_total: RANGE, and nothing is written; rows that no request's
- * entries cover stay as they are.  n_total = 0 does nothing. */
+ * not begin with 0 or end with n_total: RANGE, and nothing is written; entries that fall: RANGE, and
+ * rows that more than one request's entries cover, or none's, hold either's or stay as they are.
+ * n_total = 0 does nothing. */
 mkv_status kv_read_tokens(mkv_pool* pool, int32_t layer, int32_t n_req, const int32_t* block_table,
                           const uint8_t* tags, int32_t max_pages, const int32_t* from,
                           const int32_t* cu_tokens, int32_t n_total, uint16_t* k, int64_t k_stride,

@@ -296,6 +296,10 @@ __device__ __forceinline__ void read_rows(const ReadArgs& a) {
       }
     }
   }
+  // entries that fall (and so all that leave [0, n_total]): the waves above see those that a slot leads to
+  if (blockIdx.x == 0 && blockIdx.y == 0)
+    for (int r = threadIdx.x; r < a.n_req; r += 256)
+      if (a.cu[r + 1] < a.cu[r]) atomicOr(&P.ctrl[CTRL_ERR], (int)MKV_DEVERR_RANGE);
 }
 
 // blockIdx.y: keys or values, where both are asked for
