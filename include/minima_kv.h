@@ -436,13 +436,16 @@ mkv_status paged_attn_decode_sparse(mkv_pool* pool, int32_t layer, int32_t n_req
  *     p < prefix_lens[r] (a prefix seen from both sides),
  * and below the sequence's end; every head's sink logit takes its share of the softmax as a
  * token without a value: out = sum e^s v / (e^sink + sum e^s).  A query that sees no token has
- * zero outputs, its lse is the sink (-inf without one).  The struct is read during the call,
- * the device arrays when the kernels run (a captured call bakes in the rest of the struct).
+ * zero outputs, its lse is the sink (-inf without one).  The values in pages that are read are
+ * finite, also those of tokens that a query does not see (their weight is zero, and a product of
+ * zero and NaN is NaN).  The struct is read during the call, the device arrays when the kernels
+ * run (a captured call bakes in the rest of the struct).
  *  - paged_attn_decode_shaped is paged_attn_decode with them, rows = requests; prefix_lens is
  *    not read (a query at the end sees the whole prefix).  Pages wholly outside the window, or
  *    before first_keys, are not read (nor checked).  The work is spread over the chip by the
- *    table's width or the window, so documents go with a window as long as the longest.  Outputs carry the error of fp32 arithmetic, as
- *    paged_attn_decode_append_rope's do.  Buffers, workspace and errors as paged_attn_decode.
+ *    table's width or the window, so documents go with a window as long as the longest.
+ *    Outputs carry the error of fp32 arithmetic, as paged_attn_decode_append_rope's do.
+ *    Buffers, workspace and errors as paged_attn_decode.
  *  - paged_attn_decode_append_shaped is paged_attn_decode_append_rope with them, and with the
  *    query and key heads normed before the rotation (q_norm, k_norm, each may be NULL: not
  *    normed; rope NULL: not rotated).  The appended token is stored whether or not its query
@@ -450,10 +453,9 @@ mkv_status paged_attn_decode_sparse(mkv_pool* pool, int32_t layer, int32_t n_req
  *  - paged_attn_chunk_shaped is paged_attn_chunk with them, rows = queries, and with rows of
  *    bf16 out ([n_q_total][n_q_heads][d], what the next matrix product takes).  A block of 128
  *    rows reads the pages from the first to the last that any of its rows sees; the pages of a
- *    request before the first that any of its rows sees are not read (nor checked).  Those that
- *    are read hold finite values, also where a row does not see them.  Weights and values are
- *    rounded to fp16 for their product (sums in fp32): 2^-11 of each at most, or 2^-28 of the
- *    row's largest weight where that is more.
+ *    request before the first that any of its rows sees are not read (nor checked).  Weights and
+ *    values are rounded to fp16 for their product (sums in fp32): 2^-11 of each at most, or 2^-28
+ *    of the row's largest weight where that is more.
  * Errors also: EINVAL (shaping NULL, window negative), ERANGE (cap neither 0 nor in [1e-6, 1e6],
  * scale neither 0 nor in [1e-6, 1e6]).  Slopes and sinks are finite, or a sink -inf. */
 typedef struct paged_attn_shaping {
