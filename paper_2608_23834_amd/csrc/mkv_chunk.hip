@@ -686,9 +686,9 @@ __device__ __forceinline__ void chunk_block(const ChunkArgs& a, int4 it0, int4 i
   // sum w delta (v - out), whatever the deltas have in common (equal scores: all of them), and the
   // rounded products of scale and code.  (Four chunks of 512 queries after 12 to 16 K tokens, the blocks
   // whole: without a cap 1,714 us with the pairs, 1,518 so; capped, with the sums by dot products of
-  // the halves, 1,513 to 1,452.  The sums over FP8 pages, blocks cut: 1,102 to 1,112.)  The reference moves to BELOW
-  // under the largest score, so that weights as small as 2^-28 of the largest still count; no weight
-  // passes 2^8 for that.
+  // the halves, 1,513 to 1,452.  The sums over FP8 pages, blocks cut: 1,102 to 1,112.)  The reference
+  // moves to BELOW under the largest score, so that weights as small as 2^-28 of the largest still
+  // count; no weight passes 2^8 for that.
   constexpr bool ONE = SHAPE != 0;
   constexpr float BELOW = ONE ? 3.0f : 0.0f;
   auto barrier = [&]() {
